@@ -385,7 +385,7 @@ typedef struct {
     uint32_t             y_dtype;        /* ANSZP_OUT_F32, or ANSZP_OUT_BF16 (the fp32 result rounded
                                             to nearest even)                                      */
     uint32_t             x_layout;       /* ANSZP_ACT_*; ANSZP_ACT_C8 needs cin to be a multiple of 8 */
-    uint32_t             y_layout;       /* ANSZP_ACT_*                                            */
+    uint32_t             y_layout;       /* ANSZP_FN_*                                           */
     uint32_t*            status;         /* [device] 2 words, as for anszp_decode                 */
 } anszp_conv_args_t;
 
@@ -406,6 +406,124 @@ typedef struct {
  * 1 x 1 (no padding) or three wide, whatever their batch; for others one per kind of layer.  Later
  * calls may be captured into a graph and replayed. */
 int anszp_conv_fused(const anszp_conv_args_t* args, void* hip_stream);
+
+/* ---- operators that run decoded layers as a model: norm, product, quantised cache, attention ----
+ * All four return before the GPU is done, allocate nothing, keep nothing and may be captured into a graph.  Element
+ * types are ANSZP_OUT_F32, ANSZP_OUT_BF16 and, where said, ANSZP_I8; strides count elements, the innermost dimension is
+ * contiguous, and rows may begin at any element. */
+#define ANSZP_I8              3     /* signed bytes, a value is a scale times them                      */
+
+/* Root-mean-square norm with the residual's addition: h = x + residual, y = h * (mean(h^2) + eps)^(-1/2) * weight; out is y
+ * rounded to its type, or with ANSZP_I8 round(y / s) with s = max|y| / 127 of the row in out_scales (0 for a row of zeros; a row
+ * that holds an infinity or a NaN has NaN for a scale and zeros).  Sums in 32 bits, from h before it is rounded. */
+typedef struct {
+    const void* x;                /* [device] rows x cols of dtype                                   */
+    const void* residual;         /* [device] the same, or NULL for none                             */
+    void*       total;            /* [device] h rounded to dtype, or NULL; may be x or residual (same stride) */
+    const void* weight;           /* [device] cols of weight_dtype                                   */
+    void*       out;              /* [device] rows x cols of out_dtype; apart from the inputs        */
+    float*      out_scales;       /* [device] rows; with ANSZP_I8 only                               */
+    uint64_t    rows;             /* < 2^31, may be 0                                                */
+    uint64_t    x_stride, residual_stride, total_stride, out_stride;
+    uint32_t    cols;             /* 1 .. 2^31 - 1                                                   */
+    uint32_t    dtype;            /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    uint32_t    weight_dtype;     /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    uint32_t    out_dtype;        /* ANSZP_OUT_F32, ANSZP_OUT_BF16 or ANSZP_I8                       */
+    uint32_t    normalise;        /* 0: y = h (weight and eps are not read)                          */
+    float       eps;
+} anszp_norm_args_t;
+/* Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_rms_norm(const anszp_norm_args_t* args, void* hip_stream);
+
+/* activations of anszp_linear */
+#define ANSZP_FN_NONE        0
+#define ANSZP_FN_RELU        1
+#define ANSZP_FN_GELU        2     /* v / 2 * (1 + erf(v / sqrt 2))                                    */
+#define ANSZP_FN_SILU        3     /* v / (1 + exp(-v))                                                */
+
+/* Matrix product with its epilogue: out = act(scale * x_scales[r] * channel_scales[c] * sum_k x[r, k] w[c, k] + bias[c]) * mul[r, c]
+ * + residual[r, c].  x in bf16 with weights in bf16, or x in 8 bits (as anszp_rms_norm leaves it) with weights as symbols (as
+ * anszp_decode leaves them with ANSZP_OUT_U8), where w = symbol - zero_point (Sec. II-B), whatever the symbols' bitwidth.
+ * Sums of bf16 products in fp32, of 8-bit ones exact. */
+typedef struct {
+    const void*  x;               /* [device] rows x k                                               */
+    const void*  weight;          /* [device] cols x k: bf16, or with x in ANSZP_I8 symbols          */
+    const float* x_scales;        /* [device] rows, or NULL                                          */
+    const float* channel_scales;  /* [device] cols, or NULL                                          */
+    const float* bias;            /* [device] cols, or NULL                                          */
+    const void*  mul;             /* [device] rows x cols of out_dtype, or NULL                      */
+    const void*  residual;        /* [device] rows x cols of out_dtype, or NULL                      */
+    void*        out;             /* [device] rows x cols of out_dtype; may be mul or residual (same stride), apart from x and weight */
+    uint64_t     rows, cols;      /* each < 2^31, may be 0                                           */
+    uint64_t     x_stride, weight_stride, mul_stride, residual_stride, out_stride;
+    uint32_t     k;               /* 1 .. 2^30 (x in 8 bits: 65536, so that sums fit 32 bits)        */
+    uint32_t     x_dtype;         /* ANSZP_OUT_BF16 or ANSZP_I8                                      */
+    uint32_t     out_dtype;       /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    uint32_t     zero_point;      /* 0 .. 255; with x in ANSZP_I8 only                               */
+    uint32_t     activation;      /* ANSZP_FN_*                                                    */
+    float        scale;
+} anszp_linear_args_t;
+/* Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_linear(const anszp_linear_args_t* args, void* hip_stream);
+
+/* A paged cache of keys and values in 8 or 4 bits.  A slot is a token's place: page * page_size + token in page.  A vector (one
+ * head's key or value of one token) has symbols and a pair (scale, zero-point), value = scale * (symbol - zero_point): in 4 bits
+ * element 2i is the low and element 2i + 1 the high half of byte i.  The arrays are [page][head][token in page][...]. */
+typedef struct {
+    uint8_t* k;                   /* [device] n_pages x heads x page_size x head_dim * bits / 8 bytes, 16-byte aligned */
+    float*   k_params;            /* [device] n_pages x heads x page_size x 2, 16-byte aligned; zero-points are whole, 0 .. 2^bits - 1 */
+    uint8_t* v;
+    float*   v_params;
+    uint64_t n_pages;             /* < 2^31                                                          */
+    uint32_t page_size;           /* a power of two from 16 to 65536                                 */
+    uint32_t heads;               /* of keys and values, 1 .. 65535                                  */
+    uint32_t head_dim;            /* 64, 128 or 256                                                  */
+    uint32_t bits;                /* 8 or 4                                                          */
+} anszp_cache_t;
+/* [host only] What every call with a cache checks first: E_NULL, E_RANGE. */
+int anszp_cache_check(const anszp_cache_t* cache);
+
+/* Keys and values quantised into their slots, a scale and a zero-point for each vector (Sec. II-B): lo = min(0, min x), hi = max(0, max x),
+ * scale = (hi - lo) * (1 / (2^bits - 1)), zero_point = round(-lo / scale), symbol = clamp(round(x / scale) + zero_point), every operation
+ * rounded to binary32.  A vector that holds an infinity or a NaN, or whose range no binary32 holds, has NaN for a scale.
+ * k, v: [device] n_tokens x heads x head_dim of dtype (F32 or BF16); slots: [device] n_tokens, all different; a negative one: the token is
+ * not written.  status: [device] 2 words as for anszp_decode, or NULL: a slot beyond the cache is not written (ANSZP_ST_BAD_DESC,
+ * counted).  Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_cache_write(const anszp_cache_t* cache, const void* k, const void* v, uint32_t dtype, uint64_t k_token_stride, uint64_t k_head_stride,
+                      uint64_t v_token_stride, uint64_t v_head_stride, const int64_t* slots, uint64_t n_tokens, uint32_t* status, void* hip_stream);
+/* What the slots hold, as values: k, v [device] n_tokens x heads x head_dim, contiguous, of dtype (F32 or BF16), 16-byte aligned; zeros for
+ * a negative slot and one beyond the cache (ANSZP_ST_BAD_DESC).  Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_cache_read(const anszp_cache_t* cache, void* k, void* v, uint32_t dtype, const int64_t* slots, uint64_t n_tokens, uint32_t* status, void* hip_stream);
+
+/* Attention of new tokens over the cache.  Sequence s has the queries starts[s] .. starts[s + 1] - 1, its last tokens: with n of them
+ * and lengths[s] tokens in all (the new ones written already), number i is at position lengths[s] - n + i and sees the positions up to its own.
+ *   out = sum_t softmax_t(scale * q . k_t) v_t        a query that sees nothing (a position below 0): zeros
+ * Query head h reads the cache's head h / group.  Position t of sequence s is in page pages[s * table_width + t / page_size].
+ * Sums and statistics in fp32; queries go into the matrix instructions in fp16 scaled by a power of two per row, keys and values
+ * exactly, weights in fp16 scaled to 2^15. */
+typedef struct {
+    anszp_cache_t  cache;
+    const void*    q;             /* [device] n_tokens x (heads * group) x head_dim, bf16            */
+    void*          out;           /* [device] the same shape, of out_dtype, contiguous in head_dim   */
+    const int32_t* pages;         /* [device] n_seqs x table_width                                   */
+    const int32_t* lengths;       /* [device] n_seqs, 0 .. table_width * page_size                   */
+    const int32_t* starts;        /* [device] n_seqs + 1, from 0 to n_tokens, never falling; what is out of range is
+                                     clamped, as lengths are; queries of no sequence are left unwritten */
+    uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for a page beyond the cache that a query would
+                                     have seen; its positions are not seen, [1] grows                 */
+    void*          workspace;     /* [device] anszp_attend_workspace_bytes, 16-byte aligned, in use until the call is done */
+    uint64_t       workspace_bytes;
+    uint64_t       n_tokens, n_seqs;                      /* each < 2^24, may be 0                    */
+    uint64_t       q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    uint32_t       table_width;   /* >= 1; table_width * page_size <= 2^30                           */
+    uint32_t       group;         /* query heads per head of the cache, 1 .. 256                     */
+    uint32_t       out_dtype;     /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    float          scale;
+} anszp_attend_args_t;
+/* [host only] Bytes of workspace a call takes (0: none); reads sizes only, no pointers. */
+uint64_t anszp_attend_workspace_bytes(const anszp_attend_args_t* args);
+/* Errors: E_NULL, E_RANGE (also for a workspace that is too small), E_HIP. */
+int anszp_attend(const anszp_attend_args_t* args, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -70,6 +70,34 @@ class PackSet(C.Structure):
                 ("payload_words_used", C.c_void_p), ("status", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
 
 
+class NormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("total", C.c_void_p), ("weight", C.c_void_p), ("out", C.c_void_p),
+                ("out_scales", C.c_void_p), ("rows", C.c_uint64), ("x_stride", C.c_uint64), ("residual_stride", C.c_uint64),
+                ("total_stride", C.c_uint64), ("out_stride", C.c_uint64), ("cols", C.c_uint32), ("dtype", C.c_uint32),
+                ("weight_dtype", C.c_uint32), ("out_dtype", C.c_uint32), ("normalise", C.c_uint32), ("eps", C.c_float)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("weight", C.c_void_p), ("x_scales", C.c_void_p), ("channel_scales", C.c_void_p), ("bias", C.c_void_p),
+                ("mul", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("x_stride", C.c_uint64), ("weight_stride", C.c_uint64), ("mul_stride", C.c_uint64), ("residual_stride", C.c_uint64),
+                ("out_stride", C.c_uint64), ("k", C.c_uint32), ("x_dtype", C.c_uint32), ("out_dtype", C.c_uint32), ("zero_point", C.c_uint32),
+                ("activation", C.c_uint32), ("scale", C.c_float)]
+
+
+class CacheArg(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("k_params", C.c_void_p), ("v", C.c_void_p), ("v_params", C.c_void_p), ("n_pages", C.c_uint64),
+                ("page_size", C.c_uint32), ("heads", C.c_uint32), ("head_dim", C.c_uint32), ("bits", C.c_uint32)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("cache", CacheArg), ("q", C.c_void_p), ("out", C.c_void_p), ("pages", C.c_void_p), ("lengths", C.c_void_p),
+                ("starts", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("n_tokens", C.c_uint64), ("n_seqs", C.c_uint64), ("q_token_stride", C.c_uint64), ("q_head_stride", C.c_uint64),
+                ("out_token_stride", C.c_uint64), ("out_head_stride", C.c_uint64), ("table_width", C.c_uint32), ("group", C.c_uint32),
+                ("out_dtype", C.c_uint32), ("scale", C.c_float)]
+
+
 class AnszpError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -81,7 +109,8 @@ EXPORTS = ["anszp_version", "anszp_strerror", "anszp_normalize_freqs", "anszp_bu
            "anszp_build_tables", "anszp_build_tables_device", "anszp_pack_bound", "anszp_pack_layer", "anszp_decode", "anszp_decode_variant",
            "anszp_dequant_zp", "anszp_conv_fused", "anszp_pack_layer_device",
            "anszp_plan_bytes", "anszp_plan_decode", "anszp_decode_planned", "anszp_decode_static_plan",
-           "anszp_pack_layers_device", "anszp_pack_scratch_bytes", "anszp_pack_set_device", "anszp_test_set_spin_limit"]
+           "anszp_pack_layers_device", "anszp_pack_scratch_bytes", "anszp_pack_set_device", "anszp_test_set_spin_limit",
+           "anszp_rms_norm", "anszp_linear", "anszp_cache_check", "anszp_cache_write", "anszp_cache_read", "anszp_attend_workspace_bytes", "anszp_attend"]
 
 
 def lib():
@@ -127,6 +156,15 @@ def lib():
         L.anszp_pack_set_device.argtypes = [C.c_void_p, C.c_void_p]
         L.anszp_test_set_spin_limit.argtypes = [C.c_uint32]
         L.anszp_test_set_spin_limit.restype = None
+        L.anszp_rms_norm.argtypes = [C.c_void_p, C.c_void_p]
+        L.anszp_linear.argtypes = [C.c_void_p, C.c_void_p]
+        L.anszp_cache_check.argtypes = [C.c_void_p]
+        L.anszp_cache_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint64,
+                                        C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]
+        L.anszp_cache_read.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]
+        L.anszp_attend_workspace_bytes.argtypes = [C.c_void_p]
+        L.anszp_attend_workspace_bytes.restype = C.c_uint64
+        L.anszp_attend.argtypes = [C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -773,3 +811,218 @@ def pack_layers_device(symbols_dev, layer_sizes: Sequence[int], freqs_dev, table
     for t in (symbols_dev, freqs_dev) if out is None else (symbols_dev, freqs_dev, *out):
         t.record_stream(stream)
     return results
+
+
+# --------------------------------------------------------------------------- operators that run decoded layers as a model
+I8 = 3
+_CODE_OF = {"torch.float32": OUT_F32, "torch.bfloat16": OUT_BF16, "torch.int8": I8}
+FN_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+CACHE_BITS, CACHE_HEAD_DIMS = (8, 4), (64, 128, 256)
+
+
+def _want(t, name: str, device, shape: tuple, *dtypes):
+    """A tensor on `device` of the given shape (None: any size) and one of the dtypes, its last dimension contiguous; raises ValueError."""
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, but is on {t.device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be of {' or '.join(map(str, dtypes))}, but is of {t.dtype}")
+    if t.dim() != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must have the shape {shape}, but has {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return t.data_ptr()
+
+
+def _out_type(torch, out_dtype: str, *others):
+    if out_dtype not in ("f32", "bf16", *others):
+        raise ValueError(f"out_dtype must be one of {('f32', 'bf16', *others)}, but is {out_dtype!r}")
+    return torch.int8 if out_dtype == "i8" else torch.float32 if out_dtype == "f32" else torch.bfloat16
+
+
+def _norm(where: str, x, weight, eps: float, residual, total, out_dtype: str, normalise: int):
+    torch = _torch()
+    dev = x.device
+    _device_index(torch, dev)
+    floats = (torch.float32, torch.bfloat16)
+    a = NormArgs()
+    a.x = _want(x, "x", dev, (None, None), *floats)
+    rows, cols = x.shape
+    if normalise:
+        a.weight, a.weight_dtype = _want(weight, "weight", dev, (cols,), *floats), _CODE_OF[str(weight.dtype)]
+    if residual is not None:
+        a.residual, a.residual_stride = _want(residual, "residual", dev, (rows, cols), x.dtype), residual.stride(0)
+        if total is None:
+            total = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    if total is not None:
+        a.total, a.total_stride = _want(total, "total", dev, (rows, cols), x.dtype), total.stride(0)
+    out = torch.empty((rows, cols), dtype=_out_type(torch, out_dtype, "i8"), device=dev)
+    scales = torch.empty(rows, dtype=torch.float32, device=dev) if out_dtype == "i8" else None
+    a.out, a.out_scales = out.data_ptr(), scales.data_ptr() if scales is not None else None
+    a.rows, a.cols, a.x_stride, a.out_stride = rows, cols, x.stride(0), cols
+    a.dtype, a.out_dtype, a.normalise, a.eps = _CODE_OF[str(x.dtype)], _CODE_OF[str(out.dtype)], normalise, eps
+    _enqueue(where, lib().anszp_rms_norm, dev, C.addressof(a))
+    return out, scales, total
+
+
+def rms_norm(x, weight, eps: float = 1e-6, residual=None, out_dtype: str = "bf16", total=None):
+    """anszp_rms_norm on torch's current stream: x [rows, cols] fp32 or bf16, weight [cols], residual like x.  Returns (out, scales,
+    total): out "bf16", "f32" or "i8", scales a number per row with "i8" (else None), total = x + residual (None without a residual; written
+    to `total` where that is given, which may be x or residual itself)."""
+    return _norm("anszp_rms_norm", x, weight, eps, residual, total, out_dtype, 1)
+
+
+def quantise_rows(x):
+    """Rows of fp32 or bf16 in 8 bits with a scale each, as rms_norm's "i8" output: (symbols int8, scales fp32)."""
+    out, scales, _ = _norm("anszp_rms_norm", x, None, 0.0, None, None, "i8", 0)
+    return out, scales
+
+
+def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, channel_scales=None, bias=None, activation: str = "none",
+           mul=None, residual=None, out_dtype: str = "bf16", out=None):
+    """anszp_linear on torch's current stream: act(scale * x_scales[r] * channel_scales[c] * (x @ w^T) + bias) * mul + residual.
+    x [rows, k] and weight [cols, k] in bf16, or x int8 and weight uint8 symbols, w = symbol - zero_point; x_scales [rows],
+    channel_scales and bias [cols] fp32; mul and residual [rows, cols] of the output's type.  activation: "none", "relu",
+    "gelu" or "silu".  Returns out (which may be mul or residual itself)."""
+    torch = _torch()
+    dev = x.device
+    _device_index(torch, dev)
+    a = LinearArgs()
+    a.x = _want(x, "x", dev, (None, None), torch.bfloat16, torch.int8)
+    rows, k = x.shape
+    a.weight = _want(weight, "weight", dev, (None, k), torch.uint8 if x.dtype == torch.int8 else torch.bfloat16)
+    cols = weight.shape[0]
+    if activation not in FN_CODES:
+        raise ValueError(f"activation must be one of {tuple(FN_CODES)}, but is {activation!r}")
+    if not 0 <= zero_point <= 255 or (zero_point and x.dtype != torch.int8):
+        raise ValueError("zero_point is the symbols' own: 0 to 255, and 0 for weights in bf16")
+    if out is None:
+        out = torch.empty((rows, cols), dtype=_out_type(torch, out_dtype), device=dev)
+    a.out = _want(out, "out", dev, (rows, cols), torch.float32, torch.bfloat16)
+    if x_scales is not None:
+        a.x_scales = _want(x_scales, "x_scales", dev, (rows,), torch.float32)
+    if channel_scales is not None:
+        a.channel_scales = _want(channel_scales, "channel_scales", dev, (cols,), torch.float32)
+    if bias is not None:
+        a.bias = _want(bias, "bias", dev, (cols,), torch.float32)
+    if mul is not None:
+        a.mul, a.mul_stride = _want(mul, "mul", dev, (rows, cols), out.dtype), mul.stride(0)
+    if residual is not None:
+        a.residual, a.residual_stride = _want(residual, "residual", dev, (rows, cols), out.dtype), residual.stride(0)
+    a.rows, a.cols, a.k, a.x_stride, a.weight_stride, a.out_stride = rows, cols, k, x.stride(0), weight.stride(0), out.stride(0)
+    a.x_dtype, a.out_dtype, a.zero_point, a.activation, a.scale = _CODE_OF[str(x.dtype)], _CODE_OF[str(out.dtype)], zero_point, FN_CODES[activation], scale
+    _enqueue("anszp_linear", lib().anszp_linear, dev, C.addressof(a))
+    return out
+
+
+@dataclass
+class KvCache:
+    """A paged cache of keys and values in 8 or 4 bits (anszp_cache_t): k, v uint8 [pages, heads, page_size, head_dim * bits / 8],
+    k_params, v_params fp32 [pages, heads, page_size, 2], a scale and a zero-point for each vector.  status: two int32 words that collect
+    ANSZP_ST_* bits, or None."""
+    k: object
+    k_params: object
+    v: object
+    v_params: object
+    bits: int = 8
+    status: object = None
+
+    @property
+    def page_size(self) -> int:
+        return self.k.shape[2]
+
+    @property
+    def head_dim(self) -> int:
+        return self.k.shape[3] * 8 // self.bits
+
+
+def new_kv_cache(n_pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8, device="cuda:0") -> KvCache:
+    """An empty cache: every vector reads as zeros."""
+    torch = _torch()
+    if bits not in CACHE_BITS or head_dim not in CACHE_HEAD_DIMS:
+        raise ValueError(f"a cache has {CACHE_BITS} bits and heads of {CACHE_HEAD_DIMS} elements")
+    symbols, params = [[torch.zeros((n_pages, heads, page_size, n), dtype=t, device=device) for _ in range(2)]
+                       for n, t in ((head_dim * bits // 8, torch.uint8), (2, torch.float32))]
+    return KvCache(symbols[0], params[0], symbols[1], params[1], bits, torch.zeros(2, dtype=torch.int32, device=device))
+
+
+def _cache_arg(torch, cache: KvCache, a=None) -> CacheArg:
+    if cache.bits not in CACHE_BITS:
+        raise ValueError(f"a cache has {CACHE_BITS} bits, not {cache.bits}")
+    k, dev = cache.k, cache.k.device
+    a = CacheArg() if a is None else a
+    a.k = _want(k, "the cache's k", dev, (None, None, None, None), torch.uint8)
+    a.v = _want(cache.v, "the cache's v", dev, tuple(k.shape), torch.uint8)
+    pages, heads, page_size, _ = k.shape
+    a.k_params = _want(cache.k_params, "the cache's k_params", dev, (pages, heads, page_size, 2), torch.float32)
+    a.v_params = _want(cache.v_params, "the cache's v_params", dev, (pages, heads, page_size, 2), torch.float32)
+    if not (k.is_contiguous() and cache.v.is_contiguous() and cache.k_params.is_contiguous() and cache.v_params.is_contiguous()):
+        raise ValueError("a cache's tensors must be contiguous")
+    a.n_pages, a.page_size, a.heads, a.head_dim, a.bits = pages, page_size, heads, cache.head_dim, cache.bits
+    return a
+
+
+def _status_ptr(torch, cache: KvCache):
+    return None if cache.status is None else _want(cache.status, "the cache's status", cache.k.device, (2,), torch.int32)
+
+
+def cache_write(cache: KvCache, k, v, slots):
+    """anszp_cache_write on torch's current stream: k, v [tokens, heads, head_dim] fp32 or bf16 (contiguous in the last dimension) into
+    the slots [tokens] int64, page * page_size + place in the page; tokens with a negative slot are not written."""
+    torch = _torch()
+    dev = cache.k.device
+    _device_index(torch, dev)
+    a = _cache_arg(torch, cache)
+    shape = (None, a.heads, a.head_dim)
+    kp = _want(k, "k", dev, shape, torch.float32, torch.bfloat16)
+    n = k.shape[0]
+    vp = _want(v, "v", dev, (n, *shape[1:]), k.dtype)
+    sp = _want(slots, "slots", dev, (n,), torch.int64)
+    _enqueue("anszp_cache_write", lib().anszp_cache_write, dev, C.addressof(a), kp, vp, _CODE_OF[str(k.dtype)], k.stride(0), k.stride(1),
+             v.stride(0), v.stride(1), sp, n, _status_ptr(torch, cache))
+
+
+def cache_read(cache: KvCache, slots, out_dtype: str = "bf16"):
+    """anszp_cache_read on torch's current stream: (k, v), each [tokens, heads, head_dim]; zeros for a negative slot."""
+    torch = _torch()
+    dev = cache.k.device
+    _device_index(torch, dev)
+    a = _cache_arg(torch, cache)
+    sp = _want(slots, "slots", dev, (None,), torch.int64)
+    n, t = slots.shape[0], _out_type(torch, out_dtype)
+    k, v = (torch.empty((n, a.heads, a.head_dim), dtype=t, device=dev) for _ in range(2))
+    _enqueue("anszp_cache_read", lib().anszp_cache_read, dev, C.addressof(a), k.data_ptr(), v.data_ptr(), _CODE_OF[str(t)], sp, n, _status_ptr(torch, cache))
+    return k, v
+
+
+def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = None, out_dtype: str = "bf16", out=None):
+    """anszp_attend on torch's current stream: q [tokens, heads * group, head_dim] bf16, the new tokens of all sequences one sequence
+    behind the other, their keys and values in the cache already; pages [sequences, width] int32, lengths [sequences] int32 (new tokens
+    included), starts [sequences + 1] int32.  scale: 1 / sqrt(head_dim) if not given.  Returns out, q's shape."""
+    torch = _torch()
+    dev = q.device
+    _device_index(torch, dev)
+    a = AttendArgs()
+    c = _cache_arg(torch, cache, a.cache)
+    if q.dim() != 3 or q.shape[1] == 0 or q.shape[1] % max(c.heads, 1):
+        raise ValueError(f"q must be [tokens, a multiple of {c.heads} heads, {c.head_dim}], but has the shape {tuple(q.shape)}")
+    a.q = _want(q, "q", cache.k.device, (None, None, c.head_dim), torch.bfloat16)
+    a.pages = _want(pages, "pages", dev, (None, None), torch.int32)
+    n_seqs, width = pages.shape
+    if width > 1 and pages.stride(0) != width and n_seqs > 1:
+        raise ValueError("pages must be contiguous")
+    a.lengths = _want(lengths, "lengths", dev, (n_seqs,), torch.int32)
+    a.starts = _want(starts, "starts", dev, (n_seqs + 1,), torch.int32)
+    if out is None:
+        out = torch.empty(q.shape, dtype=_out_type(torch, out_dtype), device=dev)
+    a.out = _want(out, "out", dev, tuple(q.shape), torch.float32, torch.bfloat16)
+    a.status = _status_ptr(torch, cache)
+    a.n_tokens, a.n_seqs, a.table_width, a.group = q.shape[0], n_seqs, width, q.shape[1] // c.heads
+    a.q_token_stride, a.q_head_stride, a.out_token_stride, a.out_head_stride = q.stride(0), q.stride(1), out.stride(0), out.stride(1)
+    a.out_dtype, a.scale = _CODE_OF[str(out.dtype)], c.head_dim ** -0.5 if scale is None else scale
+    L = lib()
+    need = L.anszp_attend_workspace_bytes(C.addressof(a))
+    if need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+    _enqueue("anszp_attend", L.anszp_attend, dev, C.addressof(a))
+    return out

@@ -1,0 +1,212 @@
+"""GPU: attention over the quantised cache against the formula in 64 bits: one token and chunks, ragged sequences, shared heads, every
+head width, pages that end inside a step, sequences that are split, and what must not be seen."""
+import pytest
+import torch
+
+import operators_plain as P
+from paper_2406_06237_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _filled(pages, page, heads, dim, bits, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    most = (1 << bits) - 1
+    cache = B.new_kv_cache(pages, page, heads, dim, bits)
+    for symbols, params in ((cache.k, cache.k_params), (cache.v, cache.v_params)):
+        symbols.copy_(torch.randint(0, 256, symbols.shape, device=DEV, generator=g))
+        params[..., 0] = (torch.rand(params.shape[:-1], device=DEV, generator=g) + 0.1) * 4.0 / most
+        params[..., 1] = torch.randint(0, most + 1, params.shape[:-1], device=DEV, generator=g).float()
+    return cache
+
+
+def _case(lengths, news, heads=2, group=2, dim=64, page=16, bits=8, seed=0, spare=2, width=None):
+    g = torch.Generator().manual_seed(seed)
+    counts = [-(-n // page) for n in lengths]
+    cache = _filled(sum(counts) + spare, page, heads, dim, bits, seed)
+    order = torch.randperm(sum(counts) + spare, generator=g).to(torch.int32)
+    table, at = torch.full((len(lengths), width or max(1, max(counts))), -7, dtype=torch.int32), 0      # places that no token has name no page
+    for i, n in enumerate(counts):
+        table[i, :n] = order[at:at + n]
+        at += n
+    starts = torch.tensor([0] + news).cumsum(0).to(torch.int32)
+    q = torch.randn(int(starts[-1]), heads * group, dim, generator=g).to(torch.bfloat16)
+    return cache, q.to(DEV), table.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV), starts.to(DEV)
+
+
+def _check(case, out_dtype="bf16", scale=None, what=""):
+    cache, q, table, lengths, starts = case
+    d = q.shape[2]
+    want, error = P.attend(q, P.values(cache.k, cache.k_params, cache.bits), P.values(cache.v, cache.v_params, cache.bits), table, lengths, starts, cache.page_size,
+                           d ** -0.5 if scale is None else scale)
+    got = B.attend(q, cache, table, lengths, starts, scale=scale, out_dtype=out_dtype)
+    P.assert_within(got, want, error + want.abs() * P.HALF_ULP[got.dtype], what)
+    return got
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 64])
+def test_single_tokens_of_all_lengths(page, dim, bits):
+    lengths = [1, 2, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129, 300, 513]
+    for heads, group in ((1, 1), (2, 4), (1, 16), (3, 5)):
+        _check(_case(lengths, [1] * len(lengths), heads, group, dim, page, bits), what=(heads, group))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group", [1, 3, 8])
+def test_chunks(group, dim, bits):
+    for lengths, news in (([40, 7, 65], [40, 7, 3]), ([150, 200, 33], [33, 100, 32]), ([17], [16])):
+        _check(_case(lengths, news, 2, group, dim, 16, bits), what=news)
+        _check(_case(lengths, news, 1, group, dim, 32, bits), "f32", what=news)
+
+
+def test_long_chunks():
+    _check(_case([300, 261], [260, 131], 1, 2, 128, 64))
+    _check(_case([300, 261], [260, 131], 1, 1, 64, 16, 4))
+    _check(_case([300, 261], [260, 131], 1, 1, 256, 16))
+
+
+def test_sequences_split_over_workgroups():
+    for bits in (8, 4):
+        _check(_case([5000], [1], 1, 2, 128, 64, bits))
+        _check(_case([3001, 40], [2, 1], 1, 4, 64, 16, bits, width=400))
+        _check(_case([2049], [5], 1, 8, 256, 32, bits), "f32")
+
+
+def test_sequences_of_nothing():
+    """No new tokens, no tokens at all, and new tokens before the first position: zeros."""
+    for group in (1, 8):
+        got = _check(_case([0, 20, 0, 5, 3, 64], [2, 0, 0, 8, 3, 40], 2, group))
+        assert (got[:2] == 0).all() and (got[2:5] == 0).all()
+    cache, q, table, lengths, starts = _case([40], [1])
+    assert B.attend(q[:0], cache, table, lengths, torch.zeros_like(starts)).shape == (0, 4, 64)
+    empty = B.new_kv_cache(0, 16, 2, 64)
+    assert (B.attend(q, empty, table, lengths, starts) == 0).all()
+
+
+def test_many_sequences():
+    lengths = [1 + (7 * i) % 50 for i in range(150)]
+    _check(_case(lengths, [min(n, 1 + i % 3) for i, n in enumerate(lengths)], 1, 2))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_what_is_not_seen_may_be_anything(new):
+    """Vectors behind a sequence's end, and, for a query, those of later tokens: NaN, infinities, scales of any size."""
+    case = _case([70, 45], [new, new], 2, 4, 128, 32)
+    cache, q, table, lengths, starts = case
+    want = B.attend(q, cache, table, lengths, starts)
+    used = torch.zeros(cache.k.shape[0], cache.page_size, dtype=torch.bool, device=DEV)
+    for s, n in enumerate((70, 45)):
+        for t in range(n):
+            used[table[s, t // 32], t % 32] = True
+    for params in (cache.k_params, cache.v_params):
+        params.masked_fill_(~used[:, None, :, None], float("nan"))
+    assert torch.equal(B.attend(q, cache, table, lengths, starts), want)
+    for params in (cache.k_params, cache.v_params):
+        params[..., 0].masked_fill_(~used[:, None, :], float("inf"))
+        params[..., 1].masked_fill_(~used[:, None, :], -3e38)
+    assert torch.equal(B.attend(q, cache, table, lengths, starts), want)
+    if new > 1:                                                        # a later token without a scale
+        cache.v_params[table[0, 65 // 32], :, 65 % 32, 0] = float("nan")
+        cache.k_params[table[0, 66 // 32], :, 66 % 32, 0] = float("nan")
+        got = B.attend(q, cache, table, lengths, starts)
+        first = 65 - (70 - new)
+        assert torch.equal(got[:first], want[:first]) and torch.equal(got[new:], want[new:])
+        assert torch.isnan(got[first:new]).all()
+
+
+def test_queries_of_all_sizes_and_bad_ones():
+    case = _case([50, 60, 70, 80, 90], [1, 1, 1, 1, 1], 1, 2, 64)
+    q = case[1]
+    q[0] *= 2.0 ** 100
+    q[1] *= 2.0 ** -100
+    q[2] = 0
+    q[3, 0, 5] = float("nan")
+    _check((case[0], torch.cat([q[1:3], q[2:3]]), case[2][:3], case[3][:3], case[4][:4]), "f32")
+    got = B.attend(q, *((case[0],) + case[2:]))
+    assert torch.isnan(got[3, 0]).all() and torch.isfinite(got[3, 1]).all() and torch.isfinite(got[[1, 2, 4]]).all()
+
+
+@pytest.mark.parametrize("by", [1e-30, 1e-6, 1e6, 1e30])
+def test_value_scales_of_all_sizes(by):
+    """Some values a million times larger than others, and all of them small or large; zeros."""
+    case = _case([150, 90], [1, 12], 1, 2, 128, 16)
+    v = case[0].v_params
+    v[..., 0] *= by
+    v[::2, :, 3:9, 0] *= 1e-6
+    v[1::2, :, 9:12, 0] = 0
+    _check(case, "f32")
+    v[..., 0] = 0
+    assert (B.attend(case[1], *((case[0],) + case[2:])) == 0).all()
+
+
+def test_weights_of_a_peaked_softmax():
+    """One token with nearly all the weight and no value to speak of, so that the small weights make the result."""
+    case = _case([400], [1], 1, 1, 64, 16)
+    cache, q, table = case[0], case[1], case[2]
+    sink = (int(table[0, 0]), 0, 0)
+    values = P.values(cache.k, cache.k_params, 8)
+    cache.k_params[..., 0] *= 0.05
+    cache.k[sink] = torch.where(q[0, 0] > 0, 255, 0).to(torch.uint8)
+    cache.k_params[sink] = torch.tensor([0.02, 128.0], device=DEV)
+    cache.v_params[sink] = torch.tensor([0.0, 0.0], device=DEV)
+    del values
+    _check(case, "f32", scale=0.05)
+
+
+def test_pages_that_are_not_there():
+    case = _case([100, 100], [1, 20], 2, 2, 64)
+    cache, q, table, lengths, starts = case
+    table[0, 2], table[1, 0], table[1, 1] = -1, cache.k.shape[0], 2 ** 31 - 1
+    _check(case)
+    assert cache.status[0].item() == B.ST_BAD_DESC and cache.status[1].item() > 0
+    table[0] = -1
+    assert (_check(case)[0] == 0).all()
+
+
+def test_views_of_queries_and_outputs():
+    cache, q, table, lengths, starts = _case([60, 33], [20, 1], 2, 2, 128)
+    want = B.attend(q, cache, table, lengths, starts)
+    wide = torch.zeros(21, 12, 128, dtype=torch.bfloat16, device=DEV)
+    wide[:, 4:8] = q
+    out = torch.zeros(21, 4, 136, dtype=torch.bfloat16, device=DEV)[:, :, 3:131]
+    assert torch.equal(B.attend(wide[:, 4:8], cache, table, lengths, starts, out=out), want)
+    assert torch.equal(out, want)
+
+
+def test_a_cache_of_more_than_4_gib():
+    heads, dim, page = 8, 128, 64
+    pages = (5 << 30) // (heads * dim * page)
+    big = B.KvCache(torch.empty(pages, heads, page, dim, dtype=torch.uint8, device=DEV), torch.empty(pages, heads, page, 2, device=DEV),
+                    torch.empty(pages, heads, page, dim, dtype=torch.uint8, device=DEV), torch.empty(pages, heads, page, 2, device=DEV))
+    for new in (1, 60):
+        cache, q, table, lengths, starts = _case([200], [new], heads, 1, dim, page)
+        far = torch.tensor([[pages - 1, 0, pages - 2, pages - 4]], dtype=torch.int32, device=DEV)
+        for a, b in ((big.k, cache.k), (big.k_params, cache.k_params), (big.v, cache.v), (big.v_params, cache.v_params)):
+            a[far[0].long()] = b[table[0].long()]
+        assert torch.equal(B.attend(q, big, far, lengths, starts), B.attend(q, cache, table, lengths, starts))
+
+
+def test_a_captured_step_and_other_streams():
+    cache, q, table, lengths, starts = _case([700, 90], [1, 1], 2, 2, 128, 16)
+    want = B.attend(q, cache, table, lengths, starts)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = B.attend(q, cache, table, lengths, starts)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(other, want)
+    graph = torch.cuda.CUDAGraph()
+    static = torch.empty_like(want)
+    with torch.cuda.graph(graph):
+        B.attend(q, cache, table, lengths, starts, out=static)
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, device=DEV).to(torch.bfloat16))
+        lengths[0] = 650 + i
+        static.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(static, B.attend(q, cache, table, lengths, starts)), i

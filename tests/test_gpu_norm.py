@@ -1,0 +1,95 @@
+"""GPU: the root-mean-square norm against the formula in 64 bits, at every width class of its kernels, from rows that begin at any
+element, with and without a residual, in fp32, bf16 and 8 bits."""
+import pytest
+import torch
+
+import operators_plain as P
+from paper_2406_06237_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 1e-5
+# sums over 32 elements a thread, 6 exchanges in a wavefront and 15 more
+SUM = 2.0 ** -24 * 64
+
+
+def _inputs(rows, cols, dtype, seed=0, pad=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(rows, cols + pad, device=DEV, generator=g).to(dtype)[:, pad:]
+    r = (3 * torch.randn(rows, cols + pad, device=DEV, generator=g)).to(dtype)[:, :cols]
+    return x, r, (1 + 0.3 * torch.randn(cols, device=DEV, generator=g)).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [1, 7, 8, 64, 512, 513, 1000, 1024, 1025, 2048, 4096, 4099, 8192, 11008, 16384, 16391, 40000])
+def test_widths(cols, dtype):
+    for rows, pad, residual in ((1, 0, True), (3, 0, False), (5, 1, True), (66, 0, True)):
+        x, r, w = _inputs(rows, cols, dtype, cols + rows, pad)
+        r = r if residual else None
+        y, h = P.rms_norm(x, w, EPS, r)
+        for out_dtype in ("f32", "bf16", "i8"):
+            out, scales, total = B.rms_norm(x, w, EPS, residual=r, out_dtype=out_dtype)
+            if residual:
+                assert torch.equal(total, (x.float() + r.float()).to(dtype))
+            else:
+                assert total is None
+            if out_dtype == "i8":
+                most = y.abs().amax(-1)
+                P.assert_within(scales, most / 127, most / 127 * SUM)
+                P.assert_within(out.double() * scales.double()[:, None], y, (most / 127 * (0.5 + 127 * 2 * SUM))[:, None].expand_as(y))
+                assert out.abs().max().item() == 127 and (out >= -127).all()
+            else:
+                assert scales is None
+                P.assert_within(out, y, y.abs() * (SUM + P.HALF_ULP[out.dtype]))
+
+
+@pytest.mark.parametrize("cols", [64, 4096, 40000])
+def test_the_sum_may_replace_its_inputs(cols):
+    x, r, w = _inputs(9, cols, torch.bfloat16)
+    want, _, total = B.rms_norm(x, w, EPS, residual=r)
+    for which in (0, 1):
+        a, b = x.clone(), r.clone()
+        out, _, same = B.rms_norm(a, w, EPS, residual=b, total=(a, b)[which])
+        assert same.data_ptr() == (a, b)[which].data_ptr()
+        assert torch.equal(same, total) and torch.equal(out, want)
+
+
+def test_rows_without_a_number_and_rows_of_zeros():
+    for cols in (64, 4096, 40000):
+        x, _, w = _inputs(6, cols, torch.float32)
+        x[1] = 0
+        x[2, 5] = float("nan")
+        x[3, cols - 1] = float("inf")
+        x[4] = 1e-30
+        out, scales, _ = B.rms_norm(x, w, EPS, out_dtype="i8")
+        q, by = B.quantise_rows(x)
+        for symbols, s in ((out, scales), (q, by)):
+            assert torch.isnan(s[[2, 3]]).all() and torch.isfinite(s[[0, 1, 4, 5]]).all()
+            assert (symbols[1:4] == 0).all() and s[1] == 0 and s[4] > 0 and symbols[4].abs().max() == 127
+        out, _, _ = B.rms_norm(x, w, EPS, out_dtype="f32")
+        assert (out[1] == 0).all() and torch.isnan(out[2]).all()
+        assert torch.isnan(out[3, cols - 1]) and (out[3, : cols - 1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [1, 100, 4096, 11008, 20000])
+def test_rows_in_eight_bits_without_a_norm(cols, dtype):
+    x, _, _ = _inputs(7, cols, dtype, pad=3)
+    q, scales = B.quantise_rows(x)
+    most = P.wide(x).abs().amax(-1)
+    P.assert_within(scales, most / 127, most / 127 * 2.0 ** -22)
+    P.assert_within(q.double() * scales.double()[:, None], P.wide(x), (most / 127 * (0.5 + 2.0 ** -14))[:, None].expand_as(x.cpu()))
+
+
+def test_weights_of_the_other_type_and_rows_many():
+    x, r, w = _inputs(70001, 64, torch.bfloat16)
+    want, _, _ = B.rms_norm(x, w, EPS, residual=r)
+    got, _, _ = B.rms_norm(x, w.float(), EPS, residual=r)
+    assert torch.equal(got, want)
+    y, _ = P.rms_norm(x, w, EPS, r)
+    P.assert_within(want, y, y.abs() * (SUM + P.HALF_ULP[torch.bfloat16]))
+
+
+def test_no_rows():
+    out, scales, total = B.rms_norm(torch.zeros(0, 64, device=DEV), torch.ones(64, device=DEV), residual=torch.zeros(0, 64, device=DEV), out_dtype="i8")
+    assert out.shape == (0, 64) and scales.shape == (0,) and total.shape == (0, 64)

@@ -1,0 +1,208 @@
+"""What the operators beside the decoded weights refuse: the library by an error code before anything is enqueued (no GPU needed), the binding by
+a ValueError before the library is called."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2406_06237_amd import binding as B
+
+E_NULL, E_RANGE = -1, -2
+PTR = 1 << 20                                          # never followed: every call here is refused first
+
+
+def _norm(**change):
+    a = B.NormArgs(x=PTR, residual=None, total=None, weight=PTR, out=PTR, out_scales=PTR, rows=4, x_stride=64, out_stride=64, cols=64, dtype=B.OUT_BF16,
+                   weight_dtype=B.OUT_BF16, out_dtype=B.I8, normalise=1, eps=1e-6)
+    for name, value in change.items():
+        setattr(a, name, value)
+    return B.lib().anszp_rms_norm(C.addressof(a), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), E_NULL), (dict(weight=None), E_NULL), (dict(out=None), E_NULL), (dict(out_scales=None), E_NULL),
+    (dict(cols=0), E_RANGE), (dict(cols=1 << 31), E_RANGE), (dict(rows=1 << 31), E_RANGE), (dict(dtype=B.OUT_U8), E_RANGE), (dict(dtype=B.I8), E_RANGE),
+    (dict(out_dtype=B.OUT_U8), E_RANGE), (dict(out_dtype=4), E_RANGE), (dict(weight_dtype=B.I8), E_RANGE), (dict(out_stride=63), E_RANGE),
+    (dict(total=PTR, total_stride=10), E_RANGE), (dict(rows=0, x=None, out=None), 0)])
+def test_norm(change, code):
+    assert _norm(**change) == code
+    assert B.lib().anszp_rms_norm(None, None) == E_NULL
+
+
+def _linear(**change):
+    a = B.LinearArgs(x=PTR, weight=PTR, out=PTR, rows=4, cols=64, x_stride=64, weight_stride=64, out_stride=64, k=64, x_dtype=B.I8, out_dtype=B.OUT_BF16, scale=1.0)
+    for name, value in change.items():
+        setattr(a, name, value)
+    return B.lib().anszp_linear(C.addressof(a), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(x=None), E_NULL), (dict(weight=None), E_NULL), (dict(out=None), E_NULL), (dict(k=0), E_RANGE), (dict(k=65537), E_RANGE),
+    (dict(k=(1 << 30) + 1, x_dtype=B.OUT_BF16), E_RANGE), (dict(rows=1 << 31), E_RANGE), (dict(cols=1 << 31), E_RANGE), (dict(x_dtype=B.OUT_F32), E_RANGE),
+    (dict(x_dtype=B.OUT_U8), E_RANGE), (dict(out_dtype=B.I8), E_RANGE), (dict(zero_point=256), E_RANGE), (dict(activation=4), E_RANGE), (dict(out_stride=60), E_RANGE),
+    (dict(rows=0, x=None), 0), (dict(cols=0, weight=None), 0)])
+def test_linear(change, code):
+    assert _linear(**change) == code
+    assert B.lib().anszp_linear(None, None) == E_NULL
+
+
+def _cache(**change):
+    a = B.CacheArg(k=PTR, k_params=PTR, v=PTR, v_params=PTR, n_pages=4, page_size=16, heads=2, head_dim=64, bits=8)
+    for name, value in change.items():
+        setattr(a, name, value)
+    return a
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(), 0), (dict(bits=2), E_RANGE), (dict(head_dim=96), E_RANGE), (dict(page_size=8), E_RANGE), (dict(page_size=48), E_RANGE), (dict(page_size=1 << 17), E_RANGE),
+    (dict(heads=0), E_RANGE), (dict(heads=1 << 16), E_RANGE), (dict(n_pages=1 << 31), E_RANGE), (dict(k=None), E_NULL), (dict(v_params=None), E_NULL),
+    (dict(k=PTR + 8), E_RANGE), (dict(v_params=PTR + 4), E_RANGE), (dict(n_pages=0, k=None, v=None, k_params=None, v_params=None), 0)])
+def test_cache(change, code):
+    a, L = _cache(**change), B.lib()
+    assert L.anszp_cache_check(C.addressof(a)) == code
+    if code:
+        assert L.anszp_cache_write(C.addressof(a), PTR, PTR, B.OUT_F32, 1, 1, 1, 1, PTR, 1, None, None) == code
+        assert L.anszp_cache_read(C.addressof(a), PTR, PTR, B.OUT_F32, PTR, 1, None, None) == code
+
+
+def test_cache_calls():
+    a, L = _cache(), B.lib()
+    write = lambda k=PTR, v=PTR, dtype=B.OUT_BF16, slots=PTR, n=1, cache=C.addressof(a): L.anszp_cache_write(cache, k, v, dtype, 1, 1, 1, 1, slots, n, None, None)  # noqa: E731
+    read = lambda k=PTR, v=PTR, dtype=B.OUT_BF16, slots=PTR, n=1, cache=C.addressof(a): L.anszp_cache_read(cache, k, v, dtype, slots, n, None, None)  # noqa: E731
+    for call in (write, read):
+        assert call(cache=None) == call(k=None) == call(v=None) == call(slots=None) == E_NULL
+        assert call(dtype=B.I8) == call(dtype=B.OUT_U8) == call(n=1 << 31) == E_RANGE
+        assert call(n=0, slots=None) == 0
+
+
+def _attend(cache=None, **change):
+    a = B.AttendArgs(q=PTR, out=PTR, pages=PTR, lengths=PTR, starts=PTR, n_tokens=1, n_seqs=1, q_token_stride=128, q_head_stride=64, out_token_stride=128,
+                     out_head_stride=64, table_width=4, group=1, out_dtype=B.OUT_BF16, scale=0.1)
+    for name, value in change.items():
+        setattr(a, name, value)
+    a.cache = _cache(**(cache or {}))
+    return a
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(q=None), E_NULL), (dict(out=None), E_NULL), (dict(pages=None), E_NULL), (dict(lengths=None), E_NULL), (dict(starts=None), E_NULL),
+    (dict(table_width=0), E_RANGE), (dict(table_width=1 << 27), E_RANGE), (dict(group=0), E_RANGE), (dict(group=257), E_RANGE), (dict(out_dtype=B.I8), E_RANGE),
+    (dict(n_tokens=1 << 24), E_RANGE), (dict(n_seqs=1 << 24), E_RANGE), (dict(cache=dict(head_dim=32)), E_RANGE), (dict(cache=dict(v=None)), E_NULL),
+    (dict(n_tokens=0, q=None), 0), (dict(n_seqs=0, pages=None), 0)])
+def test_attend(change, code):
+    a = _attend(**change)
+    assert B.lib().anszp_attend(C.addressof(a), None) == code
+
+
+def test_attend_workspace():
+    L = B.lib()
+    a = _attend(table_width=4096)
+    need = L.anszp_attend_workspace_bytes(C.addressof(a))
+    assert need > 0
+    a.workspace, a.workspace_bytes = None, need
+    assert L.anszp_attend(C.addressof(a), None) == E_NULL
+    a.workspace, a.workspace_bytes = PTR, need - 1
+    assert L.anszp_attend(C.addressof(a), None) == E_RANGE
+    a.workspace, a.workspace_bytes = PTR + 4, need
+    assert L.anszp_attend(C.addressof(a), None) == E_RANGE
+    for nothing in (_attend(n_tokens=0), _attend(group=0), _attend(table_width=1)):
+        assert L.anszp_attend_workspace_bytes(C.addressof(nothing)) == 0
+    assert L.anszp_attend_workspace_bytes(None) == 0 and L.anszp_attend(None, None) == E_NULL
+
+
+# ------------------------------------------------------------------------------------------------ the binding
+@pytest.fixture
+def calls(monkeypatch):
+    """The binding with host tensors taken for a GPU's and the library's device calls only counted."""
+    seen, real = [], B.lib()
+
+    class Stub:
+        def __getattr__(self, name):
+            if name == "anszp_attend_workspace_bytes":
+                return getattr(real, name)
+            return lambda *args: seen.append(name) or 0
+
+    stub = Stub()
+    monkeypatch.setattr(B, "lib", lambda: stub)
+    monkeypatch.setattr(B, "_torch_with_gpu", torch)
+    monkeypatch.setattr(B, "_host", False)
+    monkeypatch.setattr(B, "_device_index", lambda torch_, device: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    return seen
+
+
+BF16 = torch.bfloat16
+
+
+def _operands():
+    cache = B.KvCache(torch.zeros(3, 2, 16, 64, dtype=torch.uint8), torch.zeros(3, 2, 16, 2), torch.zeros(3, 2, 16, 64, dtype=torch.uint8), torch.zeros(3, 2, 16, 2),
+                      8, torch.zeros(2, dtype=torch.int32))
+    return {
+        "norm": (B.rms_norm, dict(x=torch.zeros(3, 64, dtype=BF16), weight=torch.ones(64, dtype=BF16), residual=torch.zeros(3, 64, dtype=BF16))),
+        "linear": (B.linear, dict(x=torch.zeros(3, 64, dtype=torch.int8), weight=torch.zeros(32, 64, dtype=torch.uint8), x_scales=torch.ones(3), channel_scales=torch.ones(32),
+                                  bias=torch.zeros(32), mul=torch.zeros(3, 32, dtype=BF16), residual=torch.zeros(3, 32, dtype=BF16))),
+        "write": (B.cache_write, dict(cache=cache, k=torch.zeros(5, 2, 64), v=torch.zeros(5, 2, 64), slots=torch.zeros(5, dtype=torch.int64))),
+        "read": (B.cache_read, dict(cache=cache, slots=torch.zeros(5, dtype=torch.int64))),
+        "attend": (B.attend, dict(q=torch.zeros(4, 6, 64, dtype=BF16), cache=cache, pages=torch.zeros(2, 3, dtype=torch.int32), lengths=torch.zeros(2, dtype=torch.int32),
+                                  starts=torch.zeros(3, dtype=torch.int32))),
+    }
+
+
+def _cache_with(**change):
+    cache = _operands()["read"][1]["cache"]
+    for name, value in change.items():
+        setattr(cache, name, value)
+    return dict(cache=cache)
+
+
+def test_operands_as_they_should_be(calls):
+    for function, operands in _operands().values():
+        function(**operands)
+    assert calls == ["anszp_rms_norm", "anszp_linear", "anszp_cache_write", "anszp_cache_read", "anszp_attend"]
+
+
+@pytest.mark.parametrize("which,change", [
+    ("norm", dict(x=torch.zeros(3, 64, dtype=torch.float16))), ("norm", dict(x=torch.zeros(64, dtype=BF16))), ("norm", dict(x=torch.zeros(64, 3, dtype=BF16).t())),
+    ("norm", dict(weight=torch.ones(63, dtype=BF16))), ("norm", dict(weight=torch.ones(64, dtype=torch.float16))), ("norm", dict(residual=torch.zeros(3, 64))),
+    ("norm", dict(residual=torch.zeros(2, 64, dtype=BF16))), ("norm", dict(out_dtype="u8")), ("norm", dict(total=torch.zeros(3, 64))),
+    ("linear", dict(x=torch.zeros(3, 64))), ("linear", dict(x=torch.zeros(3, 64, dtype=BF16))), ("linear", dict(weight=torch.zeros(32, 64, dtype=BF16))),
+    ("linear", dict(weight=torch.zeros(32, 63, dtype=torch.uint8))), ("linear", dict(weight=torch.zeros(64, 32, dtype=torch.uint8).t())), ("linear", dict(x_scales=torch.ones(4))),
+    ("linear", dict(channel_scales=torch.ones(32, dtype=BF16))), ("linear", dict(channel_scales=torch.ones(64)[::2])), ("linear", dict(bias=torch.zeros(32, 1))),
+    ("linear", dict(mul=torch.zeros(3, 32))), ("linear", dict(residual=torch.zeros(3, 33, dtype=BF16))), ("linear", dict(activation="tanh")), ("linear", dict(out_dtype="i8")),
+    ("linear", dict(zero_point=256)), ("linear", dict(zero_point=-1)), ("linear", dict(out=torch.zeros(3, 31, dtype=BF16))), ("linear", dict(out=torch.zeros(3, 32, dtype=torch.float16))),
+    ("linear", dict(x=torch.zeros(3, 64, dtype=BF16), weight=torch.zeros(32, 64, dtype=BF16), zero_point=1)),
+    ("write", dict(k=torch.zeros(5, 3, 64))), ("write", dict(v=torch.zeros(5, 2, 64, dtype=BF16))), ("write", dict(v=torch.zeros(4, 2, 64))),
+    ("write", dict(slots=torch.zeros(5, dtype=torch.int32))), ("write", dict(slots=torch.zeros(4, dtype=torch.int64))), ("write", dict(k=torch.zeros(5, 64, 2).transpose(1, 2))),
+    ("read", dict(slots=torch.zeros(5, 1, dtype=torch.int64))), ("read", dict(out_dtype="i8")), ("read", _cache_with(bits=5)),
+    ("read", _cache_with(k=torch.zeros(3, 2, 16, 64))), ("read", _cache_with(v=torch.zeros(2, 2, 16, 64, dtype=torch.uint8))), ("read", _cache_with(k_params=torch.zeros(3, 2, 16, 1))),
+    ("read", _cache_with(v_params=torch.zeros(3, 2, 16, 4)[..., ::2])), ("read", _cache_with(status=torch.zeros(1, dtype=torch.int32))),
+    ("read", _cache_with(k=torch.zeros(3, 16, 2, 64, dtype=torch.uint8).transpose(1, 2))),
+    ("attend", dict(q=torch.zeros(4, 5, 64, dtype=BF16))), ("attend", dict(q=torch.zeros(4, 6, 64))), ("attend", dict(q=torch.zeros(4, 6, 32, dtype=BF16))),
+    ("attend", dict(q=torch.zeros(4, 0, 64, dtype=BF16))), ("attend", dict(q=torch.zeros(4, 384, dtype=BF16))), ("attend", dict(pages=torch.zeros(2, 3, dtype=torch.int64))),
+    ("attend", dict(pages=torch.zeros(2, 6, dtype=torch.int32)[:, :3])), ("attend", dict(lengths=torch.zeros(3, dtype=torch.int32))), ("attend", dict(starts=torch.zeros(2, dtype=torch.int32))),
+    ("attend", dict(out_dtype="i8")), ("attend", dict(out=torch.zeros(4, 6, 32, dtype=BF16))),
+])
+def test_operands_that_are_refused(calls, which, change):
+    function, operands = _operands()[which]
+    with pytest.raises(ValueError):
+        function(**{**operands, **change})
+    assert calls == []
+
+
+@pytest.mark.parametrize("which", ["norm", "linear", "write", "read", "attend"])
+def test_memory_that_is_no_gpus(monkeypatch, which):
+    monkeypatch.setattr(B, "_torch_with_gpu", torch)
+    function, operands = _operands()[which]
+    with pytest.raises(ValueError, match="Expected a cuda device"):
+        function(**operands)
+
+
+def test_new_cache():
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(B, "_torch_with_gpu", torch)
+        for bad in (dict(bits=3), dict(head_dim=80)):
+            with pytest.raises(ValueError):
+                B.new_kv_cache(**{**dict(n_pages=2, page_size=16, heads=2, head_dim=64, bits=4, device="cpu"), **bad})
+        cache = B.new_kv_cache(2, 16, 3, 128, 4, "cpu")
+        assert cache.k.shape == (2, 3, 16, 64) and cache.head_dim == 128 and cache.page_size == 16
