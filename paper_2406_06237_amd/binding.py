@@ -373,9 +373,28 @@ def _host_calls():
     return _host
 
 
-def _call(where: str, name: str, device, *args):
-    """_enqueue for a native call: its result, or None where the binding's own path has to take over."""
-    function = getattr(_host_calls(), name, None)
+_operators = None
+
+
+def _operator_calls():
+    """The operators' native calls (csrc/anszp_torch_operators.cpp), or False where there are no native calls."""
+    global _operators
+    if not _host_calls():
+        return False
+    if _operators is None:
+        try:
+            from paper_2406_06237_amd import _anszp_operators
+            _operators = _anszp_operators
+        except ImportError as e:
+            import warnings
+            warnings.warn(f"the operators' native calls cannot be loaded, the binding's Python path is used ({e}); run __graft_entry__.build()")
+            _operators = False
+    return _operators
+
+
+def _call(where: str, name: str, device, *args, calls=_host_calls):
+    """_enqueue for a native call: its result (no plain int, which is an error code), or None where the binding's own path has to take over."""
+    function = getattr(calls(), name, None)
     if function is None:
         return None
     torch = _torch()
@@ -816,6 +835,8 @@ def pack_layers_device(symbols_dev, layer_sizes: Sequence[int], freqs_dev, table
 # --------------------------------------------------------------------------- operators that run decoded layers as a model
 I8 = 3
 _CODE_OF = {"torch.float32": OUT_F32, "torch.bfloat16": OUT_BF16, "torch.int8": I8}
+_FLOATS = {"f32": OUT_F32, "bf16": OUT_BF16}
+_OUT_AND_I8 = {**_FLOATS, "i8": I8}
 FN_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 CACHE_BITS, CACHE_HEAD_DIMS = (8, 4), (64, 128, 256)
 
@@ -842,6 +863,10 @@ def _out_type(torch, out_dtype: str, *others):
 def _norm(where: str, x, weight, eps: float, residual, total, out_dtype: str, normalise: int):
     torch = _torch()
     dev = x.device
+    if out_dtype in _OUT_AND_I8 and (weight is not None) == bool(normalise):
+        results = _call(where, "rms_norm", dev, x, weight, eps, residual, total, _OUT_AND_I8[out_dtype], calls=_operator_calls)
+        if results is not None:
+            return results
     _device_index(torch, dev)
     floats = (torch.float32, torch.bfloat16)
     a = NormArgs()
@@ -885,6 +910,11 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
     "gelu" or "silu".  Returns out (which may be mul or residual itself)."""
     torch = _torch()
     dev = x.device
+    if out_dtype in _FLOATS and activation in FN_CODES:
+        result = _call("anszp_linear", "linear", dev, x, weight, x_scales, zero_point, scale, channel_scales, bias, FN_CODES[activation], mul, residual,
+                       _FLOATS[out_dtype], out, calls=_operator_calls)
+        if result is not None:
+            return result
     _device_index(torch, dev)
     a = LinearArgs()
     a.x = _want(x, "x", dev, (None, None), torch.bfloat16, torch.int8)
@@ -970,6 +1000,8 @@ def cache_write(cache: KvCache, k, v, slots):
     the slots [tokens] int64, page * page_size + place in the page; tokens with a negative slot are not written."""
     torch = _torch()
     dev = cache.k.device
+    if _call("anszp_cache_write", "cache_write", dev, cache.k, cache.k_params, cache.v, cache.v_params, cache.bits, cache.status, k, v, slots, calls=_operator_calls) is not None:
+        return
     _device_index(torch, dev)
     a = _cache_arg(torch, cache)
     shape = (None, a.heads, a.head_dim)
@@ -985,6 +1017,10 @@ def cache_read(cache: KvCache, slots, out_dtype: str = "bf16"):
     """anszp_cache_read on torch's current stream: (k, v), each [tokens, heads, head_dim]; zeros for a negative slot."""
     torch = _torch()
     dev = cache.k.device
+    if out_dtype in _FLOATS:
+        results = _call("anszp_cache_read", "cache_read", dev, cache.k, cache.k_params, cache.v, cache.v_params, cache.bits, cache.status, slots, _FLOATS[out_dtype], calls=_operator_calls)
+        if results is not None:
+            return results
     _device_index(torch, dev)
     a = _cache_arg(torch, cache)
     sp = _want(slots, "slots", dev, (None,), torch.int64)
@@ -1000,6 +1036,11 @@ def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = N
     included), starts [sequences + 1] int32.  scale: 1 / sqrt(head_dim) if not given.  Returns out, q's shape."""
     torch = _torch()
     dev = q.device
+    if out_dtype in _FLOATS:
+        result = _call("anszp_attend", "attend", dev, q, cache.k, cache.k_params, cache.v, cache.v_params, cache.bits, cache.status, pages, lengths, starts, scale,
+                       _FLOATS[out_dtype], out, calls=_operator_calls)
+        if result is not None:
+            return result
     _device_index(torch, dev)
     a = AttendArgs()
     c = _cache_arg(torch, cache, a.cache)

@@ -32,6 +32,8 @@ def build_test_helpers(verbose: bool = False) -> str:
 
 HOST_SRC = os.path.join(CSRC, "anszp_torch.cpp")
 HOST_LIB = os.path.join(HERE, "_anszp_torch.so")
+OPERATORS_SRC = os.path.join(CSRC, "anszp_torch_operators.cpp")
+OPERATORS_LIB = os.path.join(HERE, "_anszp_operators.so")
 
 
 def build_host_calls(verbose: bool = False) -> str:
@@ -41,12 +43,17 @@ def build_host_calls(verbose: bool = False) -> str:
     import torch
     from torch.utils.cpp_extension import include_paths
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-I", os.path.join(ROOT, "include"), *[f for d in include_paths() + [sysconfig.get_paths()["include"]] for f in ("-isystem", d)],
-           "-o", HOST_LIB, HOST_SRC, "-L", HERE, "-l:" + os.path.basename(LIB), "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    builds = []
+    for src, to in ((HOST_SRC, HOST_LIB), (OPERATORS_SRC, OPERATORS_LIB)):
+        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+               "-I", os.path.join(ROOT, "include"), *[f for d in include_paths() + [sysconfig.get_paths()["include"]] for f in ("-isystem", d)],
+               "-o", to, src, "-L", HERE, "-l:" + os.path.basename(LIB), "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        builds.append((cmd, subprocess.Popen(cmd)))
+    for cmd, build in builds:
+        if build.wait():
+            raise subprocess.CalledProcessError(build.returncode, cmd)
     return HOST_LIB
 
 
