@@ -172,6 +172,96 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p) {
         }
 }
 
+// Few rows: the weights are read once, straight into the matrix instructions' registers, and memory is what bounds it.  A workgroup has
+// 16 * CH channels and all rows (16 * TOK at most); its wavefronts share k, 256 bytes of a row at a time each, and their sums meet in LDS.
+// Lane (c, g), c = lane % 16, g = lane / 16, feeds bytes [64 u + 16 g, 64 u + 16 g + 16) of weight row c and of activation row c.
+// Rows of either that do not exist are the last one again; their sums are not stored.
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p) {
+    constexpr uint32_t kPieces = 4u, kChunk = 64u * kPieces;
+    typedef typename Sums<BYTES>::type sums;
+    __shared__ sums joined[WAVES][(CH + (BYTES ? 1u : 0u)) * TOK][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
+    const uint64_t c0 = uint64_t(blockIdx.x) * (16u * CH), r0 = uint64_t(blockIdx.y) * (16u * TOK);
+    const uint8_t *w_row[CH], *x_row[TOK];
+    for (uint32_t a = 0; a < CH; ++a) w_row[a] = p.w + least(c0 + 16u * a + c, p.cols - 1u) * p.w_stride;
+    for (uint32_t b = 0; b < TOK; ++b) x_row[b] = p.x + least(r0 + 16u * b + c, p.rows - 1u) * p.x_stride;
+    const words4 all_one = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
+    sums acc[CH][TOK] = {}, ones[TOK] = {};
+    words4 w[2][CH][kPieces], x[2][TOK][kPieces];
+    const auto load = [&](uint32_t slot, uint32_t k0) {
+        if (k0 + kChunk <= p.k_bytes) {
+            for (uint32_t u = 0; u < kPieces; ++u) {
+                for (uint32_t a = 0; a < CH; ++a) w[slot][a][u] = *reinterpret_cast<const words4_any*>(w_row[a] + k0 + 64u * u + 16u * g);
+                for (uint32_t b = 0; b < TOK; ++b) x[slot][b][u] = *reinterpret_cast<const words4_any*>(x_row[b] + k0 + 64u * u + 16u * g);
+            }
+        } else {
+            for (uint32_t u = 0; u < kPieces; ++u) {
+                const uint32_t at = k0 + 64u * u + 16u * g;
+                const bool there = at < p.k_bytes;
+                for (uint32_t a = 0; a < CH; ++a) w[slot][a][u] = there ? piece_of(w_row[a], at, p.k_bytes) : words4{0u, 0u, 0u, 0u};
+                for (uint32_t b = 0; b < TOK; ++b) x[slot][b][u] = there ? piece_of(x_row[b], at, p.k_bytes) : words4{0u, 0u, 0u, 0u};
+            }
+        }
+    };
+    const auto multiply = [&](uint32_t slot) {
+        for (uint32_t u = 0; u < kPieces; ++u) {
+            if constexpr (BYTES)
+                for (uint32_t a = 0; a < CH; ++a)
+                    for (uint32_t e = 0; e < 4u; ++e) w[slot][a][u][e] ^= 0x80808080u;
+            for (uint32_t b = 0; b < TOK; ++b) {
+                for (uint32_t a = 0; a < CH; ++a) acc[a][b] = Sums<BYTES>::step(w[slot][a][u], x[slot][b][u], acc[a][b]);
+                if constexpr (BYTES) ones[b] = Sums<BYTES>::step(all_one, x[slot][b][u], ones[b]);
+            }
+        }
+    };
+    uint32_t k0 = wave * kChunk;
+    if (k0 < p.k_bytes) load(0u, k0);
+    while (k0 < p.k_bytes) {                              // (one piece of k on its way while the other is multiplied)
+        k0 += WAVES * kChunk;
+        if (k0 < p.k_bytes) load(1u, k0);
+        multiply(0u);
+        if (k0 >= p.k_bytes) break;
+        k0 += WAVES * kChunk;
+        if (k0 < p.k_bytes) load(0u, k0);
+        multiply(1u);
+    }
+    for (uint32_t b = 0; b < TOK; ++b) {
+        for (uint32_t a = 0; a < CH; ++a) joined[wave][a * TOK + b][lane] = acc[a][b];
+        if constexpr (BYTES) joined[wave][CH * TOK + b][lane] = ones[b];
+    }
+    __syncthreads();
+    for (uint32_t tile = wave; tile < CH * TOK; tile += WAVES) {
+        const uint32_t a = tile / TOK, b = tile % TOK;
+        sums all = joined[0][tile][lane];
+        for (uint32_t v = 1; v < WAVES; ++v) all += joined[v][tile][lane];
+        float sum[4];
+        if constexpr (BYTES) {
+            sums one = joined[0][CH * TOK + b][lane];
+            for (uint32_t v = 1; v < WAVES; ++v) one += joined[v][CH * TOK + b][lane];
+            for (uint32_t i = 0; i < 4u; ++i) sum[i] = float(all[i] + p.offset * one[i]);
+        } else {
+            for (uint32_t i = 0; i < 4u; ++i) sum[i] = all[i];
+        }
+        finish_four(p, r0 + b * 16u + c, c0 + a * 16u + g * 4u, sum);
+    }
+}
+
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WAVES>
+void launch_few(const LinearParams& p, hipStream_t s) {
+    const dim3 grid(static_cast<uint32_t>((p.cols + 16u * CH - 1u) / (16u * CH)), static_cast<uint32_t>((p.rows + 16u * TOK - 1u) / (16u * TOK)));
+    hipLaunchKernelGGL((linear_few_kernel<BYTES, TOK, CH, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
+}
+
+template <bool BYTES>
+bool take_few(const LinearParams& p, hipStream_t s) {
+    if (p.rows <= 16u) launch_few<BYTES, 1u, 1u, 8u>(p, s);
+    else if (p.rows <= 32u) launch_few<BYTES, 2u, 1u, 8u>(p, s);
+    else if (p.rows <= 64u) launch_few<BYTES, 4u, 1u, 8u>(p, s);
+    else return false;
+    return true;
+}
+
 }  // namespace
 
 extern "C" int anszp_linear(const anszp_linear_args_t* a, void* hip_stream) {
@@ -190,6 +280,7 @@ extern "C" int anszp_linear(const anszp_linear_args_t* a, void* hip_stream) {
     const dim3 grid(static_cast<uint32_t>((p.cols + 63u) / 64u), static_cast<uint32_t>((p.rows + 63u) / 64u));
     if (grid.y > 65535u) return ANSZP_E_RANGE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (bytes ? take_few<true>(p, s) : take_few<false>(p, s)) return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
     if (bytes) hipLaunchKernelGGL(linear_any_kernel<true>, grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(linear_any_kernel<false>, grid, dim3(256), 0, s, p);
     return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
