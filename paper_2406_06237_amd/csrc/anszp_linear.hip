@@ -9,6 +9,9 @@
 // with four consecutive output channels of one row of activations.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "anszp_numbers.h"
 
 namespace {
@@ -39,61 +42,90 @@ __device__ __forceinline__ float activated(float v, uint32_t activation) {
     }
 }
 
-__device__ __forceinline__ void load_four(const void* base, uint32_t dtype, uint64_t at, uint32_t there, float (&v)[4]) {
+// N = 4 or 8 consecutive elements of the output's type.
+template <uint32_t N>
+__device__ __forceinline__ void load_some(const void* base, uint32_t dtype, uint64_t at, uint32_t there, float (&v)[N]) {
     if (dtype == ANSZP_OUT_BF16) {
         const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-        if (there >= 4u) {
-            const words2 w = *reinterpret_cast<const words2_any*>(p);
-            v[0] = bf16_low(w[0]); v[1] = bf16_high(w[0]); v[2] = bf16_low(w[1]); v[3] = bf16_high(w[1]);
+        if (there >= N) {
+#pragma unroll
+            for (uint32_t i = 0; i < N / 4u; ++i) {
+                const words2 w = reinterpret_cast<const words2_any*>(p)[i];
+                v[4u * i] = bf16_low(w[0]); v[4u * i + 1u] = bf16_high(w[0]); v[4u * i + 2u] = bf16_low(w[1]); v[4u * i + 3u] = bf16_high(w[1]);
+            }
         } else {
-            for (uint32_t i = 0; i < 4u; ++i) v[i] = i < there ? bf16_low(p[i]) : 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) v[i] = i < there ? bf16_low(p[i]) : 0.0f;
         }
     } else {
         const float* p = static_cast<const float*>(base) + at;
-        if (there >= 4u) {
-            const floatx4 w = __builtin_bit_cast(floatx4, *reinterpret_cast<const words4_any*>(p));
-            for (uint32_t i = 0; i < 4u; ++i) v[i] = w[i];
+        if (there >= N) {
+#pragma unroll
+            for (uint32_t i = 0; i < N / 4u; ++i) {
+                const floatx4 w = __builtin_bit_cast(floatx4, reinterpret_cast<const words4_any*>(p)[i]);
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; ++j) v[4u * i + j] = w[j];
+            }
         } else {
-            for (uint32_t i = 0; i < 4u; ++i) v[i] = i < there ? p[i] : 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) v[i] = i < there ? p[i] : 0.0f;
         }
     }
 }
 
-// Four consecutive channels of a row, sums in 32 bits, to the output.
-__device__ __forceinline__ void finish_four(const LinearParams& p, uint64_t row, uint64_t col, const float (&sum)[4]) {
+// N consecutive channels of a row, sums in 32 bits, to the output.
+template <uint32_t N>
+__device__ __forceinline__ void finish(const LinearParams& p, uint64_t row, uint64_t col, const float (&sum)[N]) {
     if (row >= p.rows || col >= p.cols) return;
-    const uint32_t there = p.cols - col >= 4u ? 4u : uint32_t(p.cols - col);
+    const uint32_t there = p.cols - col >= N ? N : uint32_t(p.cols - col);
     const float by = p.x_scales ? p.scale * p.x_scales[row] : p.scale;
-    float v[4], t[4];
-    for (uint32_t i = 0; i < 4u; ++i) {
-        v[i] = sum[i] * by;
-        if (p.channel_scales && i < there) v[i] *= p.channel_scales[col + i];
-        if (p.bias && i < there) v[i] += p.bias[col + i];
-        v[i] = activated(v[i], p.activation);
+    float v[N], t[N];
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) v[i] = sum[i] * by;
+    if (p.channel_scales) {
+        load_some<N>(p.channel_scales, ANSZP_OUT_F32, col, there, t);
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] *= t[i];
     }
+    if (p.bias) {
+        load_some<N>(p.bias, ANSZP_OUT_F32, col, there, t);
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] += t[i];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) v[i] = activated(v[i], p.activation);
     if (p.mul) {
-        load_four(p.mul, p.out_dtype, row * p.mul_stride + col, there, t);
-        for (uint32_t i = 0; i < 4u; ++i) v[i] *= t[i];
+        load_some<N>(p.mul, p.out_dtype, row * p.mul_stride + col, there, t);
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] *= t[i];
     }
     if (p.residual) {
-        load_four(p.residual, p.out_dtype, row * p.residual_stride + col, there, t);
-        for (uint32_t i = 0; i < 4u; ++i) v[i] += t[i];
+        load_some<N>(p.residual, p.out_dtype, row * p.residual_stride + col, there, t);
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] += t[i];
     }
     const uint64_t to = row * p.out_stride + col;
     if (p.out_dtype == ANSZP_OUT_BF16) {
         uint16_t* out = static_cast<uint16_t*>(p.out) + to;
-        if (there >= 4u) {
-            *reinterpret_cast<words2_any*>(out) = words2{to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3])};
+        if (there >= N) {
+            if constexpr (N == 8u)
+                *reinterpret_cast<words4_any*>(out) = words4{to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3]), to_bf16_pair(v[4], v[5]), to_bf16_pair(v[6], v[7])};
+            else
+                *reinterpret_cast<words2_any*>(out) = words2{to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3])};
         } else {
-            for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i)
                 if (i < there) out[i] = to_bf16(v[i]);
         }
     } else {
         float* out = static_cast<float*>(p.out) + to;
-        if (there >= 4u) {
-            *reinterpret_cast<words4_any*>(out) = __builtin_bit_cast(words4, floatx4{v[0], v[1], v[2], v[3]});
+        if (there >= N) {
+#pragma unroll
+            for (uint32_t i = 0; i < N / 4u; ++i)
+                reinterpret_cast<words4_any*>(out)[i] = __builtin_bit_cast(words4, floatx4{v[4u * i], v[4u * i + 1u], v[4u * i + 2u], v[4u * i + 3u]});
         } else {
-            for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i)
                 if (i < there) out[i] = v[i];
         }
     }
@@ -106,6 +138,17 @@ __device__ __forceinline__ words4 piece_of(const uint8_t* row, uint32_t at, uint
     for (uint32_t i = 0; i < 16u; ++i)
         if (at + i < row_bytes) w[i >> 2] |= uint32_t(row[at + i]) << (8u * (i & 3u));
     return w;
+}
+
+// The same of a row of at least 16 bytes, without a loop: the row's last 16 bytes, moved down by what they start before `at`.
+__device__ __forceinline__ words4 piece_of_long(const uint8_t* row, uint32_t at, uint32_t row_bytes) {
+    const uint32_t first = at < row_bytes - 16u ? at : row_bytes - 16u, over = at - first;
+    words4 w = *reinterpret_cast<const words4_any*>(row + first);
+    if (over & 8u) w = words4{w[2], w[3], 0u, 0u};
+    if (over & 4u) w = words4{w[1], w[2], w[3], 0u};
+    const uint32_t bits = 8u * (over & 3u);
+    w = words4{__builtin_amdgcn_alignbit(w[1], w[0], bits), __builtin_amdgcn_alignbit(w[2], w[1], bits), __builtin_amdgcn_alignbit(w[3], w[2], bits), w[3] >> bits};
+    return over < 16u ? w : words4{0u, 0u, 0u, 0u};
 }
 
 // BYTES: 8-bit operands.  One step over 64 bytes of k.
@@ -168,7 +211,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p) {
                 if constexpr (BYTES) sum[i] = float(acc[a][b][i] + p.offset * ones[b][i]);
                 else sum[i] = acc[a][b][i];
             }
-            finish_four(p, r0 + (wave >> 1) * 32u + b * 16u + (lane & 15u), c0 + (wave & 1u) * 32u + a * 16u + (lane >> 4) * 4u, sum);
+            finish<4u>(p, r0 + (wave >> 1) * 32u + b * 16u + (lane & 15u), c0 + (wave & 1u) * 32u + a * 16u + (lane >> 4) * 4u, sum);
         }
 }
 
@@ -184,32 +227,44 @@ __global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p)
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint64_t c0 = uint64_t(blockIdx.x) * (16u * CH), r0 = uint64_t(blockIdx.y) * (16u * TOK);
     const uint8_t *w_row[CH], *x_row[TOK];
+#pragma unroll
     for (uint32_t a = 0; a < CH; ++a) w_row[a] = p.w + least(c0 + 16u * a + c, p.cols - 1u) * p.w_stride;
+#pragma unroll
     for (uint32_t b = 0; b < TOK; ++b) x_row[b] = p.x + least(r0 + 16u * b + c, p.rows - 1u) * p.x_stride;
     const words4 all_one = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
     sums acc[CH][TOK] = {}, ones[TOK] = {};
     words4 w[2][CH][kPieces], x[2][TOK][kPieces];
-    const auto load = [&](uint32_t slot, uint32_t k0) {
+    const auto load = [&](uint32_t slot, uint32_t k0) __attribute__((always_inline)) {
         if (k0 + kChunk <= p.k_bytes) {
+#pragma unroll
             for (uint32_t u = 0; u < kPieces; ++u) {
+#pragma unroll
                 for (uint32_t a = 0; a < CH; ++a) w[slot][a][u] = *reinterpret_cast<const words4_any*>(w_row[a] + k0 + 64u * u + 16u * g);
+#pragma unroll
                 for (uint32_t b = 0; b < TOK; ++b) x[slot][b][u] = *reinterpret_cast<const words4_any*>(x_row[b] + k0 + 64u * u + 16u * g);
             }
         } else {
+#pragma unroll
             for (uint32_t u = 0; u < kPieces; ++u) {
                 const uint32_t at = k0 + 64u * u + 16u * g;
-                const bool there = at < p.k_bytes;
-                for (uint32_t a = 0; a < CH; ++a) w[slot][a][u] = there ? piece_of(w_row[a], at, p.k_bytes) : words4{0u, 0u, 0u, 0u};
-                for (uint32_t b = 0; b < TOK; ++b) x[slot][b][u] = there ? piece_of(x_row[b], at, p.k_bytes) : words4{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (uint32_t a = 0; a < CH; ++a) w[slot][a][u] = piece_of_long(w_row[a], at, p.k_bytes);
+#pragma unroll
+                for (uint32_t b = 0; b < TOK; ++b) x[slot][b][u] = piece_of_long(x_row[b], at, p.k_bytes);
             }
         }
     };
-    const auto multiply = [&](uint32_t slot) {
+    const auto multiply = [&](uint32_t slot) __attribute__((always_inline)) {
+#pragma unroll
         for (uint32_t u = 0; u < kPieces; ++u) {
             if constexpr (BYTES)
+#pragma unroll
                 for (uint32_t a = 0; a < CH; ++a)
+#pragma unroll
                     for (uint32_t e = 0; e < 4u; ++e) w[slot][a][u][e] ^= 0x80808080u;
+#pragma unroll
             for (uint32_t b = 0; b < TOK; ++b) {
+#pragma unroll
                 for (uint32_t a = 0; a < CH; ++a) acc[a][b] = Sums<BYTES>::step(w[slot][a][u], x[slot][b][u], acc[a][b]);
                 if constexpr (BYTES) ones[b] = Sums<BYTES>::step(all_one, x[slot][b][u], ones[b]);
             }
@@ -226,7 +281,9 @@ __global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p)
         if (k0 < p.k_bytes) load(0u, k0);
         multiply(1u);
     }
+#pragma unroll
     for (uint32_t b = 0; b < TOK; ++b) {
+#pragma unroll
         for (uint32_t a = 0; a < CH; ++a) joined[wave][a * TOK + b][lane] = acc[a][b];
         if constexpr (BYTES) joined[wave][CH * TOK + b][lane] = ones[b];
     }
@@ -239,11 +296,13 @@ __global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p)
         if constexpr (BYTES) {
             sums one = joined[0][CH * TOK + b][lane];
             for (uint32_t v = 1; v < WAVES; ++v) one += joined[v][CH * TOK + b][lane];
+#pragma unroll
             for (uint32_t i = 0; i < 4u; ++i) sum[i] = float(all[i] + p.offset * one[i]);
         } else {
+#pragma unroll
             for (uint32_t i = 0; i < 4u; ++i) sum[i] = all[i];
         }
-        finish_four(p, r0 + b * 16u + c, c0 + a * 16u + g * 4u, sum);
+        finish<4u>(p, r0 + b * 16u + c, c0 + a * 16u + g * 4u, sum);
     }
 }
 
@@ -255,11 +314,213 @@ void launch_few(const LinearParams& p, hipStream_t s) {
 
 template <bool BYTES>
 bool take_few(const LinearParams& p, hipStream_t s) {
+    if (p.k_bytes < 16u) return false;
     if (p.rows <= 16u) launch_few<BYTES, 1u, 1u, 8u>(p, s);
     else if (p.rows <= 32u) launch_few<BYTES, 2u, 1u, 8u>(p, s);
     else if (p.rows <= 64u) launch_few<BYTES, 4u, 1u, 8u>(p, s);
     else return false;
     return true;
+}
+
+// Many rows: TOK activations' rows x CH channels a workgroup of WT x WC wavefronts, v_mfma_*_32x32, k in steps of 128 bytes through two
+// buffers in LDS.  A row of a buffer is 8 pieces of 16 bytes; piece j of row r lies in place j ^ (r / 2 % 8), so that 16 lanes that read one
+// piece of neighbouring rows meet all 64 banks.
+// DIRECT: rows begin at multiples of 16 bytes, and steps go from memory to LDS without passing through registers; a wavefront's load fills 8
+// rows end to end, each lane asking for the piece that belongs where its 16 bytes land.  Otherwise, and for what is left of k behind the last
+// whole step, pieces are loaded to registers, with zeros behind the end of a row.
+typedef __attribute__((ext_vector_type(16))) float floatx16;
+typedef __attribute__((ext_vector_type(16))) int32_t intx16;
+template <bool BYTES>
+struct Sums32 {
+    typedef floatx16 type;
+    static __device__ __forceinline__ floatx16 step(words4 w, words4 x, floatx16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+    }
+};
+template <>
+struct Sums32<true> {
+    typedef intx16 type;
+    static __device__ __forceinline__ intx16 step(words4 w, words4 x, intx16 c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, w), __builtin_bit_cast(intx4, x), c, 0, 0, 0);
+    }
+};
+
+typedef __attribute__((address_space(1))) const void global_void;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Workgroups go to the chip's eight dies in turn, and each die has an L2 of its own: those of one die get neighbouring tiles, columns of
+// kPanel tiles one behind the other, so that the 32 tiles a die works on at a time share 8 + 4 blocks of rows.
+constexpr uint32_t kDies = 8u, kPanel = 8u;
+__device__ __forceinline__ void place_tile(uint32_t block, uint32_t tiles_t, uint32_t tiles_c, uint32_t& tile_t, uint32_t& tile_c) {
+    const uint32_t n = tiles_t * tiles_c, die = block % kDies;
+    const uint32_t at = die * (n / kDies) + (die < n % kDies ? die : n % kDies) + block / kDies;
+    const uint32_t panel = at / (kPanel * tiles_c), in = at - panel * kPanel * tiles_c;
+    const uint32_t left = tiles_t - panel * kPanel, high = left < kPanel ? left : kPanel;
+    tile_c = in / high;
+    tile_t = panel * kPanel + in % high;
+}
+
+template <bool BYTES, bool DIRECT, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC>
+__global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams p, uint32_t tiles_c, uint32_t tiles_t) {
+    constexpr uint32_t kThreads = WT * WC * 64u, kRows = TOK + CH, kFT = TOK / WT / 32u, kFC = CH / WC / 32u;
+    constexpr uint32_t kStepBytes = 128u, kLoads = kRows * 8u / kThreads, kHalf = kLoads / 2u;      // pieces a thread brings per step
+    static_assert(kRows * 8u % kThreads == 0u && TOK * 8u % kThreads == 0u, "a load is of one operand");
+    __shared__ words4 buffer[2][kRows][8];                            // activations, then weights
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wt = wave / WC, wc = wave % WC;
+    uint32_t tile_t, tile_c;
+    place_tile(blockIdx.x, tiles_t, tiles_c, tile_t, tile_c);
+    const uint64_t t0 = uint64_t(tile_t) * TOK, c0 = uint64_t(tile_c) * CH;
+
+    // Where this thread's pieces come from: bytes behind the tile's first row of activations or weights (rows that do not exist are the last one
+    // again), for a step with what of k lies before it.
+    const uint8_t *const x_tile = p.x + t0 * p.x_stride, *const w_tile = p.w + c0 * p.w_stride;
+    const uint32_t x_last = uint32_t(least(p.rows - t0, TOK) - 1u), w_last = uint32_t(least(p.cols - c0, CH) - 1u);
+    const uint32_t piece = 16u * ((threadIdx.x & 7u) ^ ((threadIdx.x >> 4) & 7u));
+    uint32_t from[kLoads];
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t row = (i * kThreads + threadIdx.x) >> 3;
+        from[i] = i * kThreads < TOK * 8u ? min(row, x_last) * uint32_t(p.x_stride) : min(row - TOK, w_last) * uint32_t(p.w_stride);
+    }
+    const auto operand = [&](uint32_t i) __attribute__((always_inline)) { return i * kThreads < TOK * 8u ? x_tile : w_tile; };
+    // Step 0 is what is left of k behind the whole steps, if anything.
+    const uint32_t whole = p.k_bytes / kStepBytes, rest = p.k_bytes % kStepBytes ? 1u : 0u, steps = whole + rest;
+    words4 held[kLoads];
+    const auto load = [&](uint32_t s) __attribute__((always_inline)) {
+        if (s >= steps) return;
+        if (s < rest) {
+#pragma unroll
+            for (uint32_t i = 0; i < kLoads; ++i) held[i] = piece_of_long(operand(i) + from[i], whole * kStepBytes + piece, p.k_bytes);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kLoads; ++i) held[i] = *reinterpret_cast<const words4_any*>(operand(i) + (s - rest) * kStepBytes + (from[i] + piece));
+        }
+    };
+    const auto put = [&](uint32_t s) __attribute__((always_inline)) {
+        if (s >= steps) return;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) buffer[s & 1u][(i * kThreads + threadIdx.x) >> 3][threadIdx.x & 7u] = held[i];
+    };
+    const auto bring = [&](uint32_t s, uint32_t begin, uint32_t end) __attribute__((always_inline)) {      // loads of a whole step
+#pragma unroll
+        for (uint32_t i = begin; i < end; ++i)
+            __builtin_amdgcn_global_load_lds((global_void*)(operand(i) + (s - rest) * kStepBytes + (from[i] + piece)),
+                                             (lds_void*)(&buffer[s & 1u][(i * kThreads + wave * 64u) >> 3][0]), 16, 0, 0);
+    };
+    // The step behind is there for all wavefronts, and what they read before has been read.  No barrier waits by itself for loads that go to LDS.
+    const auto arrived = [&]() __attribute__((always_inline)) {
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    typename Sums32<BYTES>::type acc[kFC][kFT] = {};
+    int32_t x_sums[kFT] = {};
+    words4 x[2][kFT], w[2][kFC];
+    const uint32_t r = lane & 31u;
+    const auto fetch = [&](uint32_t slot, uint32_t s, uint32_t kk) __attribute__((always_inline)) {
+        const uint32_t j = (kk * 2u + (lane >> 5)) ^ ((r >> 1) & 7u);
+#pragma unroll
+        for (uint32_t f = 0; f < kFC; ++f) w[slot][f] = buffer[s & 1u][TOK + wc * (CH / WC) + f * 32u + r][j];
+#pragma unroll
+        for (uint32_t f = 0; f < kFT; ++f) x[slot][f] = buffer[s & 1u][wt * (TOK / WT) + f * 32u + r][j];
+    };
+    // A quarter of a step; between(a) comes behind the instructions of the a-th rows of channels.
+    const auto multiply = [&](uint32_t slot, auto between) __attribute__((always_inline)) {
+#pragma unroll
+        for (uint32_t a = 0; a < kFC; ++a) {
+            if constexpr (BYTES) {
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; ++e) w[slot][a][e] ^= 0x80808080u;
+            }
+#pragma unroll
+            for (uint32_t b = 0; b < kFT; ++b) {
+                acc[a][b] = Sums32<BYTES>::step(w[slot][a], x[slot][b], acc[a][b]);
+                if constexpr (BYTES) {                                       // a word of each piece behind each row of channels
+#pragma unroll
+                    for (uint32_t e = 0; e < 4u; ++e)
+                        if (e * kFC / 4u == a) x_sums[b] = __builtin_amdgcn_sdot4(int32_t(x[slot][b][e]), 0x01010101, x_sums[b], false);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            between(a);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // The operands of the next quarter of a step are on their way to registers while this one's are multiplied.  Before a step's last quarter is
+    // multiplied every wavefront has all it needs of the step's buffer: from there on it takes the step after the next.  Its loads are spread
+    // over that quarter and the next one (asked for in one go they keep the wavefront from multiplying), which leaves them half a step to arrive.
+    load(0u);
+    put(0u);
+    if constexpr (DIRECT) {
+        if (1u < steps) bring(1u, 0u, kHalf);
+    } else {
+        load(1u);
+    }
+    __syncthreads();
+    fetch(0u, 0u, 0u);
+    const auto step = [&](uint32_t s, auto more) __attribute__((always_inline)) {
+        constexpr bool kMore = decltype(more)::value;                        // two steps are still to come
+        multiply(0u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(1u, s, 1u);
+            if (DIRECT && (kMore || s + 1u < steps)) bring(s + 1u, kHalf + a * (kLoads - kHalf) / kFC, kHalf + (a + 1u) * (kLoads - kHalf) / kFC);
+            if (!DIRECT && a + 1u == kFC) put(s + 1u);
+        });
+        multiply(1u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(0u, s, 2u);
+            if (!DIRECT && a + 1u == kFC) load(s + 2u);
+        });
+        multiply(0u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(1u, s, 3u);
+        });
+        arrived();
+        if (kMore || s + 1u < steps) fetch(0u, s + 1u, 0u);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (DIRECT && kMore) bring(s + 2u, a * kHalf / kFC, (a + 1u) * kHalf / kFC);
+        });
+    };
+    uint32_t s = 0u;
+    for (; s + 2u < steps; ++s) step(s, std::true_type{});
+    for (; s < steps; ++s) step(s, std::false_type{});
+
+    // To the output through LDS, 32 rows of a wavefront's channels at a time, so that a row's channels are stored end to end (and mul and
+    // residual read so); four channels of row r lie in place (channel / 4) ^ (r & 7).
+    constexpr uint32_t kWidth = CH / WC, kLanes = kWidth / 8u;               // channels of a wavefront; lanes that have a row of them
+    static_assert(WT * WC * 32u * kWidth * 4u <= sizeof(buffer) && 64u % kLanes == 0u, "the epilogue's part of LDS");
+    floatx4(*part)[kWidth / 4u] = reinterpret_cast<floatx4(*)[kWidth / 4u]>(reinterpret_cast<uint8_t*>(buffer) + wave * (32u * kWidth * 4u));
+    __syncthreads();
+#pragma unroll
+    for (uint32_t b = 0; b < kFT; ++b) {
+        int32_t more = 0;
+        if constexpr (BYTES) more = p.offset * (x_sums[b] + __shfl_xor(x_sums[b], 32));
+#pragma unroll
+        for (uint32_t a = 0; a < kFC; ++a)
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) {
+                floatx4 four;
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; ++e) {
+                    if constexpr (BYTES) four[e] = float(acc[a][b][4u * i + e] + more);
+                    else four[e] = acc[a][b][4u * i + e];
+                }
+                part[r][(a * 8u + 2u * i + (lane >> 5)) ^ (r & 7u)] = four;
+            }
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t own = lane % kLanes;
+        for (uint32_t n = lane / kLanes; n < 32u; n += 64u / kLanes) {
+            const floatx4 lo = part[n][(2u * own) ^ (n & 7u)], hi = part[n][(2u * own + 1u) ^ (n & 7u)];
+            const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            finish<8u>(p, t0 + wt * (TOK / WT) + b * 32u + n, c0 + wc * kWidth + own * 8u, sum);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC>
+void launch_tile(const LinearParams& p, bool direct, hipStream_t s) {
+    const uint32_t tiles_c = static_cast<uint32_t>((p.cols + CH - 1u) / CH), tiles_t = static_cast<uint32_t>((p.rows + TOK - 1u) / TOK);
+    if (direct) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC>), dim3(tiles_c * tiles_t), dim3(WT * WC * 64u), 0, s, p, tiles_c, tiles_t);
+    else hipLaunchKernelGGL((linear_tile_kernel<BYTES, false, TOK, CH, WT, WC>), dim3(tiles_c * tiles_t), dim3(WT * WC * 64u), 0, s, p, tiles_c, tiles_t);
 }
 
 }  // namespace
@@ -281,6 +542,12 @@ extern "C" int anszp_linear(const anszp_linear_args_t* a, void* hip_stream) {
     if (grid.y > 65535u) return ANSZP_E_RANGE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (bytes ? take_few<true>(p, s) : take_few<false>(p, s)) return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
+    const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | p.x_stride | p.w_stride) & 15u) == 0u;
+    if (p.rows > 128u && p.k_bytes >= 16u && std::max(p.x_stride, p.w_stride) <= 1u << 23) {
+        if (bytes) launch_tile<true, 256u, 256u, 4u, 2u>(p, direct, s);
+        else launch_tile<false, 256u, 256u, 4u, 2u>(p, direct, s);
+        return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
+    }
     if (bytes) hipLaunchKernelGGL(linear_any_kernel<true>, grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(linear_any_kernel<false>, grid, dim3(256), 0, s, p);
     return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
