@@ -82,9 +82,9 @@ __device__ Tile find_tile(const AttendParams& p, uint32_t tile, uint32_t rows) {
         if (here) {
             const int src = __builtin_ctzll(here);
             t.seq = s0 + uint32_t(src);
-            t.first_token = __shfl(a, src);
-            t.n_new = __shfl(n, src);
-            t.first_row = __shfl(mine, src) * rows;
+            t.first_token = __builtin_amdgcn_readlane(a, src);
+            t.n_new = __builtin_amdgcn_readlane(n, src);
+            t.first_row = __builtin_amdgcn_readlane(mine, src) * rows;
             t.n_rows = min(rows, t.n_new * p.group - t.first_row);
             const int64_t most = int64_t(p.table_width) << p.page_log;
             const int32_t given = p.lengths[t.seq];
@@ -92,7 +92,7 @@ __device__ Tile find_tile(const AttendParams& p, uint32_t tile, uint32_t rows) {
             if (p.n_pages == 0u) t.length = 0;
             return t;
         }
-        before += __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return t;
 }
@@ -133,13 +133,33 @@ struct Bytes {
     }
 };
 
+// over the four lanes of a query: lane ^ 16, lane ^ 32
+__device__ __forceinline__ float most_of_query(float v) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+    const auto a = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];
+    const uint32_t h = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    const auto b = __builtin_amdgcn_permlane16_swap(h, h, false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+// the power of two at or above a value, for values of 2^-126 .. 2^126; 0 for 0
+__device__ __forceinline__ float power_above(float v) {
+    return v > 0.0f ? __builtin_bit_cast(float, min((__builtin_bit_cast(uint32_t, v) + 0x7FFFFFu) & 0xFF800000u, 0x7E800000u)) : 0.0f;
+}
+
+// Few rows: 16 a workgroup, whose four wavefronts take 32 tokens each in turn.  Memory is what bounds it where it can: what a step reads
+// is asked for a step ahead (two steps' worth of registers; heads of 256 leave no room for that).
+// The running maximum and the values' power of two are looked up together in one vote; queries that meet a larger one rescale, the rest of the steps
+// exchange nothing between lanes.
 template <uint32_t D, uint32_t BITS>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendParams p) {
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     constexpr uint32_t kKeyBytes = D * BITS / 32u, kValueBytes = D * BITS / 128u;      // of a key, of a value, that a lane feeds
     constexpr uint32_t kMfmas = D / 32u, kTiles = D / 16u, kVector = D * BITS / 8u;
+    constexpr bool kAhead = D <= 128u;
     __shared__ float joined[kAttendWaves][kTileRows][D + 4u];
     __shared__ float stats[kAttendWaves][kTileRows][2];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
     const uint32_t head = blockIdx.y, split = blockIdx.z;
     const Tile t = find_tile(p, blockIdx.x, kTileRows);
     if (t.n_rows == 0u) return;
@@ -151,122 +171,154 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendParams p) {
         return;
     }
 
+    // What a step reads.  The lane feeds token c of each half as a key, tokens 4 g .. 4 g + 3 of each half as values, whose pairs (scale,
+    // zero-point) it needs, like the scales of the keys of those tokens.
+    struct Step {
+        Bytes<kKeyBytes> keys[2];
+        Bytes<kValueBytes> values[2][4];
+        float key_zero[2];
+        words4 key_params[2][2], value_params[2][2];
+        bool there[2];
+    };
+    const int32_t* const table = p.pages + uint64_t(t.seq) * p.table_width;
+    // Pages of 32 turns of the wavefront, a lane for each half of each: read together, so that no step waits for where it is to read.
+    constexpr int32_t kTurn = int32_t(kAttendWaves * kStep);
+    const int32_t own = begin + int32_t(wave * kStep);
+    int32_t pages = 0;
+    bool missing = false;
+    const auto ask = [&](Step& s, int32_t turn) __attribute__((always_inline)) {
+        const int32_t t0 = own + turn * kTurn;
+        if (turn % 32 == 0) {
+            const int32_t first = t0 + int32_t(lane >> 1) * kTurn + int32_t(16u * (lane & 1u));
+            const int32_t read = first < end ? table[uint32_t(first) >> p.page_log] : 0;
+            asm volatile("v_mov_b32 %0, %1" : "=v"(pages) : "v"(read));                 // (waited for here, not by every step that uses it)
+        }
+        const int32_t named[2] = {__builtin_amdgcn_readlane(pages, 2 * (turn % 32)), __builtin_amdgcn_readlane(pages, 2 * (turn % 32) + 1)};
+#pragma unroll
+        for (uint32_t u = 0; u < 2u; ++u) {
+            const int32_t first = t0 + int32_t(16u * u);
+            const bool known = named[u] >= 0 && uint64_t(named[u]) < p.n_pages;
+            s.there[u] = first < end && known;
+            missing |= first < end && !known;
+            const uint64_t base = ((uint64_t(s.there[u] ? named[u] : 0) * p.heads + head) << p.page_log) + (uint32_t(first) & ((1u << p.page_log) - 1u) & ~15u);
+            s.keys[u].load(p.k + base * kVector + (c * kVector + g * kKeyBytes));
+            s.key_zero[u] = p.k_params[2u * base + (2u * c + 1u)];
+            const words4* const kp = reinterpret_cast<const words4*>(p.k_params + 2u * base) + 2u * g;
+            const words4* const vp = reinterpret_cast<const words4*>(p.v_params + 2u * base) + 2u * g;
+            s.key_params[u][0] = kp[0]; s.key_params[u][1] = kp[1];
+            s.value_params[u][0] = vp[0]; s.value_params[u][1] = vp[1];
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) s.values[u][i].load(p.v + base * kVector + ((g * 4u + i) * kVector + c * kValueBytes));
+        }
+    };
+
     // the lane's part of query c, scaled into fp16
     const uint32_t row = t.first_row + min(c, t.n_rows - 1u), token = row / p.group, member = row - token * p.group;
     const int32_t position = t.length - int32_t(t.n_new) + int32_t(token);
+    const int32_t least_position = t.length - int32_t(t.n_new) + int32_t(t.first_row / p.group);
     words4 q[kMfmas];
     float to_scores;
     {
         const uint16_t* from = p.q + uint64_t(t.first_token + token) * p.q_token_stride + uint64_t(head * p.group + member) * p.q_head_stride + g * (D / 4u);
-        float v[kMfmas][8], most = 0.0f;
-        for (uint32_t m = 0; m < kMfmas; ++m) {
-            Eight<ANSZP_OUT_BF16> e;
-            e.load(from, m * 8u, 8u);
-            for (uint32_t j = 0; j < 8u; ++j) {
-                v[m][j] = e[j];
-                most = fmaxf(most, fabsf(e[j]));
-            }
-        }
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
+        Eight<ANSZP_OUT_BF16> v[kMfmas];
+        float most = 0.0f;
+#pragma unroll
+        for (uint32_t m = 0; m < kMfmas; ++m) v[m].load(from, m * 8u, 8u);
+#pragma unroll
+        for (uint32_t m = 0; m < kMfmas; ++m)
+#pragma unroll
+            for (uint32_t j = 0; j < 8u; ++j) most = fmaxf(most, fabsf(v[m][j]));
+        most = most_of_query(most);
         const int32_t exponent = int32_t(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
         const int32_t up = exponent == 128 ? 0 : min(13 - exponent, 126);
         const float factor = __builtin_bit_cast(float, uint32_t(up + 127) << 23);
         to_scores = p.scale * __builtin_bit_cast(float, uint32_t(127 - up) << 23);
+#pragma unroll
         for (uint32_t m = 0; m < kMfmas; ++m) {
-            // 4 bits: bytes of low halves, then of high ones
-            constexpr uint32_t kOrder4[8] = {0, 2, 4, 6, 1, 3, 5, 7};
+            constexpr uint32_t kOrder4[8] = {0, 2, 4, 6, 1, 3, 5, 7};                   // 4 bits: bytes of low halves, then of high ones
             f16x8 h;
+#pragma unroll
             for (uint32_t j = 0; j < 8u; ++j) h[j] = static_cast<_Float16>(v[m][BITS == 4u ? kOrder4[j] : j] * factor);
             q[m] = __builtin_bit_cast(words4, h);
         }
     }
 
     floatx4 acc[kTiles] = {};
-    float top = -__builtin_inff(), sum = 0.0f, reach = 0.0f;                            // m, the lane's part of l, the values' power of two
-    for (int32_t t0 = begin + int32_t(wave * kStep); t0 < end; t0 += int32_t(kAttendWaves * kStep)) {
-        floatx4 x[2];
-        uint32_t hidden = 0u;                                                           // bit 4 u + i
-        Bytes<kValueBytes> vb[2][4];
-        float vs[2][4], vz[2][4];
+    float top = -__builtin_inff(), sum = 0.0f, reach = 0.0f, less = 0.0f;               // m, the lane's part of l, the values' power of two and 1 over it
+    const auto take = [&](const Step& step, int32_t t0) __attribute__((always_inline)) {
+        float x[8], vs[8], vz[8];
+#pragma unroll
         for (uint32_t u = 0; u < 2u; ++u) {
-            const int32_t first = t0 + int32_t(16u * u);
-            const bool inside = first < end;
-            const uint32_t at = inside ? uint32_t(first) >> p.page_log : 0u;
-            const int32_t named = p.pages[uint64_t(t.seq) * p.table_width + at];
-            const bool there = inside && named >= 0 && uint64_t(named) < p.n_pages;
-            if (inside && !there && lane == 0u) flag(p);
-            const uint64_t base = ((uint64_t(there ? named : 0) * p.heads + head) << p.page_log) + (uint32_t(first) & ((1u << p.page_log) - 1u) & ~15u);
-            // keys
-            Bytes<kKeyBytes> kb;
-            kb.load(p.k + (base + c) * kVector + g * kKeyBytes);
-            float kz = p.k_params[2u * (base + c) + 1u];
-            if (!there || first + int32_t(c) >= end) kz = 0.0f;
-            const f16x2 offset = both(1024.0f + kz);
+            const f16x2 offset = both(1024.0f + step.key_zero[u]);
             floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
             for (uint32_t m = 0; m < kMfmas; ++m) {
                 words2 a, b;
                 if constexpr (BITS == 8u) {
-                    a = less_zero(kb.w[2u * m], offset);
-                    b = less_zero(kb.w[2u * m + 1u], offset);
+                    a = less_zero(step.keys[u].w[2u * m], offset);
+                    b = less_zero(step.keys[u].w[2u * m + 1u], offset);
                 } else {
-                    a = less_zero(kb.w[m] & 0x0F0F0F0Fu, offset);
-                    b = less_zero((kb.w[m] >> 4) & 0x0F0F0F0Fu, offset);
+                    a = less_zero(step.keys[u].w[m] & 0x0F0F0F0Fu, offset);
+                    b = less_zero((step.keys[u].w[m] >> 4) & 0x0F0F0F0Fu, offset);
                 }
                 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, words4{a[0], a[1], b[0], b[1]}), __builtin_bit_cast(f16x8, q[m]), s, 0, 0, 0);
             }
+#pragma unroll
             for (uint32_t i = 0; i < 4u; ++i) {
-                const uint64_t n = base + g * 4u + i;
-                const int32_t place = first + int32_t(g * 4u + i);
-                vb[u][i].load(p.v + n * kVector + c * kValueBytes);
-                const float2 w = reinterpret_cast<const float2*>(p.v_params)[n];
-                const bool held = there && place < end;
-                vs[u][i] = held ? w.x : 0.0f;
-                vz[u][i] = held ? w.y : 0.0f;
-                x[u][i] = s[i] * to_scores * p.k_params[2u * n];
-                if (!held || place > position) {
-                    x[u][i] = -__builtin_inff();
-                    hidden |= 1u << (4u * u + i);
-                }
+                const uint32_t ks = step.key_params[u][i / 2u][2u * (i & 1u)], vsi = step.value_params[u][i / 2u][2u * (i & 1u)], vzi = step.value_params[u][i / 2u][2u * (i & 1u) + 1u];
+                x[4u * u + i] = s[i] * (to_scores * __builtin_bit_cast(float, ks));
+                vs[4u * u + i] = __builtin_bit_cast(float, vsi);
+                vz[4u * u + i] = __builtin_bit_cast(float, vzi);
+            }
+            // (The keys' zero-points came with their scales, for other lanes' tokens.  Without a use their registers are given away while the loads are
+            // still under way, and whoever gets them waits for all loads.)
+            asm volatile("" ::"v"(step.key_params[u][0][1]), "v"(step.key_params[u][0][3]), "v"(step.key_params[u][1][1]), "v"(step.key_params[u][1][3]));
+        }
+        if (!(step.there[0] && step.there[1] && t0 + 31 <= least_position && t0 + 32 <= end)) {
+            // Tokens that no row sees give nothing, whatever their numbers are; nor do, in their row, those that it does not see.
+#pragma unroll
+            for (uint32_t n = 0; n < 8u; ++n) {
+                const int32_t place = t0 + int32_t(16u * (n / 4u) + g * 4u + n % 4u);
+                const bool held = step.there[n / 4u] && place < end, sees = held && place <= position;
+                x[n] = sees ? x[n] : -__builtin_inff();
+                vs[n] = sees ? vs[n] : 0.0f;
+                vz[n] = held ? vz[n] : 0.0f;
             }
         }
-        // running maximum, over the lane's tokens and the other lanes of the same query
-        float high = top, far = reach;
-        for (uint32_t u = 0; u < 2u; ++u)
-            for (uint32_t i = 0; i < 4u; ++i) {
-                high = fmaxf(high, x[u][i]);
-                far = fmaxf(far, fabsf(vs[u][i]));
-            }
-        high = fmaxf(high, __shfl_xor(high, 16));
-        high = fmaxf(high, __shfl_xor(high, 32));
-        far = fmaxf(far, __shfl_xor(far, 16));
-        far = fmaxf(far, __shfl_xor(far, 32));
-        if (far > reach) far = __builtin_bit_cast(float, min((__builtin_bit_cast(uint32_t, far) + 0x7FFFFFu) & 0xFF800000u, 0x7E800000u));
-        const float less = far > 0.0f ? 1.0f / far : 0.0f;
-        const float safe = high == -__builtin_inff() ? 0.0f : high;
-        const float kept = __builtin_amdgcn_exp2f(top - safe), kept_values = kept * (reach * less);
-        top = high;
-        reach = far;
-        float l = 0.0f;
+        float high = x[0], far = fabsf(vs[0]);
+#pragma unroll
+        for (uint32_t n = 1; n < 8u; ++n) {
+            high = fmaxf(high, x[n]);
+            far = fmaxf(far, fabsf(vs[n]));
+        }
+        if (__any(high > top || far > reach)) {
+            high = fmaxf(top, most_of_query(high));
+            far = fmaxf(reach, power_above(most_of_query(far)));
+            less = far > 0.0f ? 1.0f / far : 0.0f;
+            const float kept = __builtin_amdgcn_exp2f(top - (high == -__builtin_inff() ? 0.0f : high)), kept_values = kept * (reach * less);
+            top = high;
+            reach = far;
+            sum *= kept;
+#pragma unroll
+            for (uint32_t e = 0; e < kTiles; ++e) acc[e] *= kept_values;
+        }
+        const float safe = (top == -__builtin_inff() ? 0.0f : top) - 15.0f;
         words4 weights;
-        for (uint32_t u = 0; u < 2u; ++u)
-            for (uint32_t i = 0; i < 4u; i += 2u) {
-                float w[2];
-                for (uint32_t j = 0; j < 2u; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(x[u][i + j] - safe + 15.0f);
-                    l += e;
-                    w[j] = hidden >> (4u * u + i + j) & 1u ? 0.0f : e * (vs[u][i + j] * less);
-                }
-                weights[2u * u + i / 2u] = bits_of(f16x2{static_cast<_Float16>(w[0]), static_cast<_Float16>(w[1])});
-            }
-        sum = sum * kept + l;
+#pragma unroll
+        for (uint32_t n = 0; n < 8u; n += 2u) {
+            const float e0 = __builtin_amdgcn_exp2f(x[n] - safe), e1 = __builtin_amdgcn_exp2f(x[n + 1u] - safe);
+            sum += e0 + e1;
+            weights[n / 2u] = bits_of(f16x2{static_cast<_Float16>(e0 * (vs[n] * less)), static_cast<_Float16>(e1 * (vs[n + 1u] * less))});
+        }
         f16x2 z[4];
-        for (uint32_t j = 0; j < 4u; ++j)
-            z[j] = f16x2{static_cast<_Float16>(1024.0f + vz[j >> 1][2u * (j & 1u)]), static_cast<_Float16>(1024.0f + vz[j >> 1][2u * (j & 1u) + 1u])};
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j) z[j] = f16x2{static_cast<_Float16>(1024.0f + vz[2u * j]), static_cast<_Float16>(1024.0f + vz[2u * j + 1u])};
+#pragma unroll
         for (uint32_t e = 0; e < kTiles; ++e) {
             words4 a;
+#pragma unroll
             for (uint32_t j = 0; j < 4u; ++j) {
-                const Bytes<kValueBytes>&one = vb[j >> 1][2u * (j & 1u)], &two = vb[j >> 1][2u * (j & 1u) + 1u];
+                const Bytes<kValueBytes>&one = step.values[j >> 1][2u * (j & 1u)], &two = step.values[j >> 1][2u * (j & 1u) + 1u];
                 uint32_t pair;
                 if constexpr (BITS == 8u) {
                     pair = __builtin_amdgcn_perm(two.w[e >> 2], one.w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
@@ -276,10 +328,30 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendParams p) {
                 }
                 a[j] = bits_of(halves(pair | 0x64006400u) - z[j]);
             }
-            acc[e] *= kept_values;
             acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, weights), acc[e], 0, 0, 0);
         }
+    };
+    if (own < end) {
+        Step one, two;
+        ask(one, 0);
+        // Two turns a round, the second behind the end where their number is odd: a way out between them would make the compiler wait, at the loop's
+        // head, for loads that are under way on that way only.  Behind the end the first page is read, and nothing is seen.
+        __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0), for the same reason
+        for (int32_t turn = 0; own + turn * kTurn < end; turn += kAhead ? 2 : 1) {
+            if constexpr (kAhead) {
+                ask(two, turn + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                take(one, own + turn * kTurn);
+                ask(one, turn + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                take(two, own + (turn + 1) * kTurn);
+            } else {
+                take(one, own + turn * kTurn);
+                ask(one, turn + 1);
+            }
+        }
     }
+    if (missing && lane == 0u) flag(p);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
 
@@ -319,48 +391,67 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendParams p) {
     }
 }
 
-// The splits' results together: a workgroup per tile and head, 16 threads a row.
+// The splits' results together: four workgroups per tile and head, a row of it at a time; D / 4 lanes have a split, their sums meet in LDS.
 template <uint32_t D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
-    constexpr uint32_t kMine = D / 16u;
+    constexpr uint32_t kLanes = D / 4u, kGroups = 256u / kLanes;
+    __shared__ floatx4 joined[kGroups][kLanes];
+    __shared__ float sums[kGroups], tops[4];
     const uint32_t head = blockIdx.y;
     const Tile t = find_tile(p, blockIdx.x, kTileRows);
-    const uint32_t r = threadIdx.x >> 4, d0 = (threadIdx.x & 15u) * kMine;
-    if (r >= t.n_rows) return;
+    const uint32_t d = threadIdx.x % kLanes, n = threadIdx.x / kLanes;
     const float2* stats = reinterpret_cast<const float2*>(p.part_stats);
-    float high = -__builtin_inff(), l = 0.0f, o[kMine] = {};
-    for (uint32_t s = 0; s < p.splits; ++s) high = fmaxf(high, stats[((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * kTileRows + r].x);
-    const float safe = high == -__builtin_inff() ? 0.0f : high;
-    for (uint32_t s = 0; s < p.splits; ++s) {
-        const uint64_t part = ((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * kTileRows + r;
-        const float2 w = stats[part];
-        if (w.y == 0.0f) continue;
-        const float by = __builtin_amdgcn_exp2f(w.x - safe);
-        l += w.y * by;
-        for (uint32_t d = 0; d < kMine; ++d) o[d] += p.parts[part * D + d0 + d] * by;
-    }
-    const float over = l == 0.0f ? 0.0f : 1.0f / l;
-    const uint32_t row = t.first_row + r, token = row / p.group, member = row - token * p.group;
-    const uint64_t to = uint64_t(t.first_token + token) * p.out_token_stride + uint64_t(head * p.group + member) * p.out_head_stride + d0;
-    for (uint32_t d = 0; d < kMine; d += 4u) {
-        const floatx4 v = {o[d] * over, o[d + 1u] * over, o[d + 2u] * over, o[d + 3u] * over};
-        if (p.out_dtype == ANSZP_OUT_BF16)
-            *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + to + d) = words2{to_bf16_pair(v[0], v[1]), to_bf16_pair(v[2], v[3])};
-        else
-            *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + to + d) = __builtin_bit_cast(words4, v);
+    for (uint32_t r = blockIdx.z; r < t.n_rows; r += gridDim.z) {
+        const auto part_of = [&](uint32_t s) { return ((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * kTileRows + r; };
+        float high = -__builtin_inff();
+        for (uint32_t s = threadIdx.x; s < p.splits; s += 256u) high = fmaxf(high, stats[part_of(s)].x);
+        for (int x = 32; x; x >>= 1) high = fmaxf(high, __shfl_xor(high, x));
+        if ((threadIdx.x & 63u) == 0u) tops[threadIdx.x >> 6] = high;
+        __syncthreads();
+        high = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        const float safe = high == -__builtin_inff() ? 0.0f : high;
+        floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        float l = 0.0f;
+        for (uint32_t s = n; s < p.splits; s += kGroups) {
+            const float2 w = stats[part_of(s)];
+            if (w.y == 0.0f) continue;                                                  // (nothing was written for it)
+            const float by = __builtin_amdgcn_exp2f(w.x - safe);
+            l += w.y * by;
+            o += *reinterpret_cast<const floatx4*>(p.parts + part_of(s) * D + 4u * d) * by;
+        }
+        joined[n][d] = o;
+        if (d == 0u) sums[n] = l;
+        __syncthreads();
+        if (n == 0u) {
+            for (uint32_t m = 1; m < kGroups; ++m) {
+                o += joined[m][d];
+                l += sums[m];
+            }
+            const float over = l == 0.0f ? 0.0f : 1.0f / l;
+            const uint32_t row = t.first_row + r, token = row / p.group, member = row - token * p.group;
+            const uint64_t to = uint64_t(t.first_token + token) * p.out_token_stride + uint64_t(head * p.group + member) * p.out_head_stride + 4u * d;
+            o *= over;
+            if (p.out_dtype == ANSZP_OUT_BF16)
+                *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + to) = words2{to_bf16_pair(o[0], o[1]), to_bf16_pair(o[2], o[3])};
+            else
+                *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + to) = __builtin_bit_cast(words4, o);
+        }
+        __syncthreads();
     }
 }
 
-// How the tokens are shared out: enough workgroups for the chip, at least 256 tokens in each.
+// How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of
+// about 1024 tokens, since sequences differ in length and the longest would end last (48 sequences of 17 to 4100 tokens, 32 heads
+// in 4 bits: 184 us with a workgroup for each, %SHARED% with shares).  The lengths are on the device: what the page tables can hold counts.
 struct Shares {
     uint32_t tiles, splits, span;
 };
 Shares shares_of(const anszp_attend_args_t& a) {
     Shares s;
     s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / kTileRows + a.n_seqs);
-    const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads);
-    uint64_t splits = std::min<uint64_t>(4u * device_cus() / groups, (most + 255u) / 256u);
-    splits = std::max<uint64_t>(1u, std::min<uint64_t>(splits, 1024u));
+    const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();
+    uint64_t splits = std::max(2u * cus / groups, std::min<uint64_t>(32u * cus / groups, (most + 1023u) / 1024u));
+    splits = std::max<uint64_t>(1u, std::min<uint64_t>(std::min<uint64_t>(splits, (most + 255u) / 256u), 1024u));
     const uint64_t whole = kStep * kAttendWaves;
     s.span = static_cast<uint32_t>((most + splits * whole - 1u) / (splits * whole) * whole);
     s.splits = static_cast<uint32_t>((most + s.span - 1u) / s.span);
@@ -382,7 +473,7 @@ void launch(const AttendParams& p, uint32_t bits, hipStream_t s) {
     const dim3 grid(p.n_tiles, p.heads, p.splits);
     if (bits == 8u) hipLaunchKernelGGL((attend_rows_kernel<D, 8u>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((attend_rows_kernel<D, 4u>), grid, dim3(256), 0, s, p);
-    if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads), dim3(256), 0, s, p);
+    if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, 4u), dim3(256), 0, s, p);
 }
 
 }  // namespace

@@ -83,10 +83,19 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheParams p) {
     const float by = sound && scale > 0.0f ? scale : 1.0f;          // (a range below what 32 bits can divide is all zero-point)
     const float zero = sound && scale > 0.0f ? rintf(-lo / by) : 0.0f;
     uint32_t q[8];
-    for (uint32_t i = 0; i < 8u; ++i) {
-        const float v = sound && scale > 0.0f ? rintf(x[i] / by) + zero : 0.0f;
-        q[i] = uint32_t(fminf(fmaxf(v, 0.0f), kMost));
+    if (by >= 0x1p-100f && by <= 0x1p100f) {
+        // x / by rounded once, in three instructions: y the reciprocal rounded, a = x y rounded, then a + (x - a by) y is x / by rounded (Markstein's
+        // theorem; away from the ends of the exponents' range, where no quotient that matters here lies).
+        const float y = 1.0f / by;
+        for (uint32_t i = 0; i < 8u; ++i) {
+            const float a = x[i] * y;
+            q[i] = uint32_t(fminf(fmaxf(rintf(fmaf(fmaf(-a, by, x[i]), y, a)) + zero, 0.0f), kMost));
+        }
+    } else {
+        for (uint32_t i = 0; i < 8u; ++i) q[i] = uint32_t(fminf(fmaxf(rintf(x[i] / by) + zero, 0.0f), kMost));
     }
+    if (!(sound && scale > 0.0f))
+        for (uint32_t i = 0; i < 8u; ++i) q[i] = 0u;
     uint8_t* to = p.symbols[which] + at.vector * (p.dim * BITS / 8u);
     if constexpr (BITS == 8u)
         reinterpret_cast<words2*>(to)[lane] = words2{q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
