@@ -22,7 +22,7 @@
 
 namespace {
 
-constexpr uint32_t kTileRows = 16u, kStep = 32u, kAttendWaves = 4u;
+constexpr uint32_t kTileRows = 16u, kStep = 32u, kAttendWaves = 4u;      // of attend_rows_kernel
 
 struct AttendParams {
     const uint8_t* k;
@@ -41,6 +41,7 @@ struct AttendParams {
     uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
     uint32_t n_tokens, n_seqs, n_tiles, heads, group, table_width, page_log, out_dtype;
     uint32_t splits, span;              // tokens a split covers
+    uint32_t tile_rows;
     float scale;                        // times log2 e
 };
 
@@ -391,6 +392,307 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     }
 }
 
+// 16 x n matrix of fp16 whose rows are PIECES pieces of 16 bytes: where piece j of row r lies, so that 16 lanes that read a piece of 16 consecutive
+// rows meet all 64 banks (and the 16 that write 8 rows apart few of them twice).
+template <uint32_t PIECES>
+__device__ __forceinline__ uint32_t place_of_piece(uint32_t r, uint32_t j) {
+    if constexpr (PIECES >= 16u) return j ^ (r & 15u);
+    else if constexpr (PIECES == 8u) return j ^ ((r >> 1) & 7u) ^ ((r >> 4) & 7u);
+    else return j ^ ((r >> 2) & 3u) ^ ((r >> 4) & 3u);
+}
+
+// Many rows: 64 * RT a workgroup, 16 * RT a wavefront, T tokens a step.  The matrix instructions and the weights' exponentials bound it, so symbols become
+// operands once for all four wavefronts: each thread turns some of the next step's bytes, which it asked for a step ahead, into fp16 in LDS while
+// others still multiply, keys [token][dimension], values [dimension][token] with the eight tokens that a lane feeds (4 g .. 4 g + 3 of both halves of
+// 32) side by side.  Otherwise as above.
+template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT>
+__global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
+    constexpr uint32_t kMfmas = D / 32u, kTiles = D / 16u, kVector = D * BITS / 8u, kRows = 64u * RT;
+    constexpr uint32_t kKeyDims = T * D / 256u, kValueDims = T * D / 1024u;             // a thread's: of one key; of each of four values
+    constexpr uint32_t kKeyBytes = kKeyDims * BITS / 8u, kValueBytes = kValueDims * BITS / 8u, kChunks = D / kValueDims;
+    constexpr uint32_t kKeyPieces = D / 8u, kValuePieces = T / 8u;
+    __shared__ words4 key_buffer[2][T][kKeyPieces];
+    __shared__ words2 value_buffer[2][D][kValuePieces * 2u];
+    __shared__ float key_scales[2][T], value_scales[2][T];
+    __shared__ uint32_t known[2][T / 16u];
+    __shared__ int32_t lost[2];                                                         // the last step whose buffer lacks pages
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
+    const uint32_t head = blockIdx.x % p.heads, tile = p.n_tiles - 1u - blockIdx.x / p.heads;       // (later tokens see more: first)
+    const uint32_t split = blockIdx.y;
+    const Tile t = find_tile(p, tile, kRows);
+    if (t.n_rows == 0u) return;
+    const int32_t begin = int32_t(split * p.span), end = min(seen_by(p, t), begin + int32_t(p.span));
+    const uint64_t part = (uint64_t(split) * p.n_tiles + tile) * p.heads + head;
+    if (p.splits > 1u && begin >= end) {
+        if (threadIdx.x < kRows) reinterpret_cast<float2*>(p.part_stats)[part * kRows + threadIdx.x] = make_float2(-__builtin_inff(), 0.0f);
+        return;
+    }
+
+    // staging
+    const uint32_t key_token = threadIdx.x / (256u / T), key_part = threadIdx.x % (256u / T);
+    const uint32_t quad = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+    const int32_t* const table = p.pages + uint64_t(t.seq) * p.table_width;
+    const auto page_at = [&](int32_t place) __attribute__((always_inline)) { return table[place < end ? uint32_t(place) >> p.page_log : 0u]; };
+    bool missing = false;
+    if (threadIdx.x < 2u) lost[threadIdx.x] = -1;
+    Bytes<kKeyBytes> key_bytes;
+    Bytes<kValueBytes> value_bytes[4];
+    float2 key_pair;
+    words4 value_pairs[2];
+    int32_t key_page, value_page;                                                       // of the step to be asked for next
+    bool key_there, value_there;                                                        // of what has been asked for
+    const auto ask_pages = [&](int32_t step) __attribute__((always_inline)) {
+        key_page = page_at(begin + step * int32_t(T) + int32_t(key_token));
+        value_page = page_at(begin + step * int32_t(T) + int32_t(quad * 4u));
+    };
+    const auto vector_at = [&](int32_t place, int32_t page, bool there) __attribute__((always_inline)) {
+        return ((uint64_t(there ? page : 0) * p.heads + head) << p.page_log) + (uint32_t(place) & ((1u << p.page_log) - 1u));
+    };
+    const auto ask = [&](int32_t step) __attribute__((always_inline)) {
+        const int32_t key_place = begin + step * int32_t(T) + int32_t(key_token), value_place = begin + step * int32_t(T) + int32_t(quad * 4u);
+        const bool key_known = uint64_t(int64_t(key_page)) < p.n_pages, value_known = uint64_t(int64_t(value_page)) < p.n_pages;
+        missing |= key_place < end && !key_known;
+        key_there = key_place < end && key_known;
+        value_there = value_place < end && value_known;
+        const uint64_t kv = vector_at(key_place, key_page, key_there), vv = vector_at(value_place, value_page, value_there);
+        key_bytes.load(p.k + kv * kVector + key_part * kKeyBytes);
+        key_pair = reinterpret_cast<const float2*>(p.k_params)[kv];
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) value_bytes[i].load(p.v + (vv + i) * kVector + chunk * kValueBytes);
+        value_pairs[0] = reinterpret_cast<const words4*>(p.v_params)[vv / 2u];
+        value_pairs[1] = reinterpret_cast<const words4*>(p.v_params)[vv / 2u + 1u];
+    };
+    const auto put = [&](int32_t step) __attribute__((always_inline)) {
+        const uint32_t to = uint32_t(step) & 1u;
+        const f16x2 offset = both(1024.0f + (key_there ? key_pair.y : 0.0f));
+#pragma unroll
+        for (uint32_t j = 0; j < kKeyDims / 8u; ++j) {
+            words2 a, b;
+            if constexpr (BITS == 8u) {
+                a = less_zero(key_bytes.w[2u * j], offset);
+                b = less_zero(key_bytes.w[2u * j + 1u], offset);
+            } else {
+                a = less_zero(key_bytes.w[j] & 0x0F0F0F0Fu, offset);
+                b = less_zero((key_bytes.w[j] >> 4) & 0x0F0F0F0Fu, offset);
+            }
+            key_buffer[to][key_token][place_of_piece<kKeyPieces>(key_token, key_part * (kKeyDims / 8u) + j)] = words4{a[0], a[1], b[0], b[1]};
+        }
+        if (key_part == 0u) key_scales[to][key_token] = key_pair.x;
+        float vs[4], vz[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            const uint32_t si = value_pairs[i / 2u][2u * (i & 1u)], zi = value_pairs[i / 2u][2u * (i & 1u) + 1u];
+            const bool held = value_there && begin + step * int32_t(T) + int32_t(quad * 4u + i) < end;
+            vs[i] = held ? __builtin_bit_cast(float, si) : 0.0f;
+            vz[i] = held ? __builtin_bit_cast(float, zi) : 0.0f;
+        }
+        const f16x2 z0 = {static_cast<_Float16>(1024.0f + vz[0]), static_cast<_Float16>(1024.0f + vz[1])};
+        const f16x2 z1 = {static_cast<_Float16>(1024.0f + vz[2]), static_cast<_Float16>(1024.0f + vz[3])};
+        // the quad's place among the 32 tokens of its group: half (quad / 4) % 2 of piece quad % 4
+        const uint32_t piece = quad / 8u * 4u + (quad & 3u), half = (quad >> 2) & 1u;
+#pragma unroll
+        for (uint32_t e = 0; e < kValueDims; ++e) {
+            uint32_t lo, hi;
+            if constexpr (BITS == 8u) {
+                lo = __builtin_amdgcn_perm(value_bytes[1].w[e >> 2], value_bytes[0].w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
+                hi = __builtin_amdgcn_perm(value_bytes[3].w[e >> 2], value_bytes[2].w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
+            } else {
+                lo = __builtin_amdgcn_perm(value_bytes[1].w[e >> 3], value_bytes[0].w[e >> 3], 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
+                hi = __builtin_amdgcn_perm(value_bytes[3].w[e >> 3], value_bytes[2].w[e >> 3], 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
+                lo = (e & 1u ? lo >> 4 : lo) & 0x000F000Fu;
+                hi = (e & 1u ? hi >> 4 : hi) & 0x000F000Fu;
+            }
+            const uint32_t dim = chunk * kValueDims + e;
+            value_buffer[to][dim][2u * place_of_piece<kValuePieces>(dim, piece) + half] = words2{bits_of(halves(lo | 0x64006400u) - z0), bits_of(halves(hi | 0x64006400u) - z1)};
+        }
+        if (chunk == 0u) *reinterpret_cast<floatx4*>(&value_scales[to][quad * 4u]) = floatx4{vs[0], vs[1], vs[2], vs[3]};
+        if (key_part == 0u && (key_token & 15u) == 0u) {
+            known[to][key_token / 16u] = key_there ? 1u : 0u;
+            if (!key_there && begin + step * int32_t(T) + int32_t(key_token) < end) lost[to] = step;
+        }
+    };
+
+    // the wavefront's queries, scaled into fp16
+    const uint32_t own_row = t.first_row + wave * (16u * RT), last_row = t.first_row + t.n_rows - 1u;
+    words4 q[RT][kMfmas];
+    float to_scores[RT];
+    int32_t position[RT];
+    uint64_t out_at[RT];
+#pragma unroll
+    for (uint32_t b = 0; b < RT; ++b) {
+        const uint32_t row = min(own_row + 16u * b + c, last_row), token = row / p.group, member = row - token * p.group;
+        position[b] = t.length - int32_t(t.n_new) + int32_t(token);
+        out_at[b] = uint64_t(t.first_token + token) * p.out_token_stride + uint64_t(head * p.group + member) * p.out_head_stride;
+        const uint16_t* from = p.q + uint64_t(t.first_token + token) * p.q_token_stride + uint64_t(head * p.group + member) * p.q_head_stride + g * 8u;
+        Eight<ANSZP_OUT_BF16> v[kMfmas];
+        float most = 0.0f;
+#pragma unroll
+        for (uint32_t m = 0; m < kMfmas; ++m) v[m].load(from, m * 32u, 8u);
+#pragma unroll
+        for (uint32_t m = 0; m < kMfmas; ++m)
+#pragma unroll
+            for (uint32_t j = 0; j < 8u; ++j) most = fmaxf(most, fabsf(v[m][j]));
+        most = most_of_query(most);
+        const int32_t exponent = int32_t(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
+        const int32_t up = exponent == 128 ? 0 : min(13 - exponent, 126);
+        const float factor = __builtin_bit_cast(float, uint32_t(up + 127) << 23);
+        to_scores[b] = p.scale * __builtin_bit_cast(float, uint32_t(127 - up) << 23);
+#pragma unroll
+        for (uint32_t m = 0; m < kMfmas; ++m) {
+            constexpr uint32_t kOrder4[8] = {0, 2, 4, 6, 1, 3, 5, 7};
+            f16x8 h;
+#pragma unroll
+            for (uint32_t j = 0; j < 8u; ++j) h[j] = static_cast<_Float16>(v[m][BITS == 4u ? kOrder4[j] : j] * factor);
+            q[b][m] = __builtin_bit_cast(words4, h);
+        }
+    }
+    const int32_t least_position = t.length - int32_t(t.n_new) + int32_t(min(own_row, last_row) / p.group);
+    const int32_t most_position = t.length - int32_t(t.n_new) + int32_t(min(own_row + 16u * RT - 1u, last_row) / p.group);
+
+    floatx4 acc[kTiles][RT] = {};
+    float top[RT], sum[RT] = {}, reach = 0.0f, less = 0.0f;                             // (the power of two is the wavefront's)
+#pragma unroll
+    for (uint32_t b = 0; b < RT; ++b) top[b] = -__builtin_inff();
+    const auto take = [&](int32_t step) __attribute__((always_inline)) {
+        const uint32_t in = uint32_t(step) & 1u;
+        {                                                                               // values larger than any before
+            const float far = fabsf(value_scales[in][lane % T]);
+            if (__any(far > reach)) {
+                float high = most_of_query(far);
+                for (int x = 8; x; x >>= 1) high = fmaxf(high, __shfl_xor(high, x));
+                const float now = fmaxf(reach, power_above(high));
+                less = 1.0f / now;
+                const float kept = reach * less;
+                reach = now;
+#pragma unroll
+                for (uint32_t e = 0; e < kTiles; ++e)
+#pragma unroll
+                    for (uint32_t b = 0; b < RT; ++b) acc[e][b] *= kept;
+            }
+        }
+        const bool lacking = lost[in] == step;
+#pragma unroll
+        for (uint32_t h = 0; h < T / 32u; ++h) {
+            const int32_t t0 = begin + step * int32_t(T) + int32_t(32u * h);
+            if (t0 > most_position || t0 >= end) break;                                 // nothing that these rows see
+            float y[RT][8];
+            f16x2 ratio[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 2u; ++u) {
+                const uint32_t row = 32u * h + 16u * u + c;
+                floatx4 s[RT] = {};
+#pragma unroll
+                for (uint32_t m = 0; m < kMfmas; ++m) {
+                    const words4 a = key_buffer[in][row][place_of_piece<kKeyPieces>(row, m * 4u + g)];
+#pragma unroll
+                    for (uint32_t b = 0; b < RT; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, q[b][m]), s[b], 0, 0, 0);
+                }
+                const floatx4 ks = *reinterpret_cast<const floatx4*>(&key_scales[in][32u * h + 16u * u + 4u * g]);
+                const floatx4 vs = *reinterpret_cast<const floatx4*>(&value_scales[in][32u * h + 16u * u + 4u * g]) * less;
+                ratio[2u * u] = f16x2{static_cast<_Float16>(vs[0]), static_cast<_Float16>(vs[1])};
+                ratio[2u * u + 1u] = f16x2{static_cast<_Float16>(vs[2]), static_cast<_Float16>(vs[3])};
+#pragma unroll
+                for (uint32_t b = 0; b < RT; ++b)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) y[b][4u * u + i] = s[b][i] * (ks[i] * to_scores[b]);
+            }
+            uint32_t unseen[RT] = {};
+            const bool whole = !lacking && t0 + 31 <= least_position && t0 + 32 <= end;
+            if (!whole) {
+#pragma unroll
+                for (uint32_t n = 0; n < 8u; ++n) {
+                    const int32_t place = t0 + int32_t(16u * (n / 4u) + g * 4u + n % 4u);
+                    const bool held = place < end && known[in][2u * h + n / 4u];
+#pragma unroll
+                    for (uint32_t b = 0; b < RT; ++b)
+                        if (!held || place > position[b]) {
+                            y[b][n] = -__builtin_inff();
+                            unseen[b] |= 1u << n;
+                        }
+                }
+            }
+            bool grows = false;
+            float high[RT];
+#pragma unroll
+            for (uint32_t b = 0; b < RT; ++b) {
+                high[b] = y[b][0];
+#pragma unroll
+                for (uint32_t n = 1; n < 8u; ++n) high[b] = fmaxf(high[b], y[b][n]);
+                grows |= high[b] > top[b];
+            }
+            if (__any(grows)) {
+#pragma unroll
+                for (uint32_t b = 0; b < RT; ++b) {
+                    const float now = fmaxf(top[b], most_of_query(high[b]));
+                    const float kept = __builtin_amdgcn_exp2f(top[b] - (now == -__builtin_inff() ? 0.0f : now));
+                    top[b] = now;
+                    sum[b] *= kept;
+#pragma unroll
+                    for (uint32_t e = 0; e < kTiles; ++e) acc[e][b] *= kept;
+                }
+            }
+            words4 weights[RT];
+#pragma unroll
+            for (uint32_t b = 0; b < RT; ++b) {
+                const float safe = (top[b] == -__builtin_inff() ? 0.0f : top[b]) - 15.0f;
+#pragma unroll
+                for (uint32_t n = 0; n < 8u; n += 2u) {
+                    const float e0 = __builtin_amdgcn_exp2f(y[b][n] - safe), e1 = __builtin_amdgcn_exp2f(y[b][n + 1u] - safe);
+                    sum[b] += e0 + e1;
+                    weights[b][n / 2u] = bits_of(f16x2{static_cast<_Float16>(e0), static_cast<_Float16>(e1)} * ratio[n / 2u]);
+                    if (!whole) weights[b][n / 2u] &= (unseen[b] >> n & 1u ? 0u : 0x0000FFFFu) | (unseen[b] >> n & 2u ? 0u : 0xFFFF0000u);
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < kTiles; ++e) {
+                const uint32_t dim = 16u * e + c;
+                const words4 a = *reinterpret_cast<const words4*>(&value_buffer[in][dim][2u * place_of_piece<kValuePieces>(dim, 4u * h + g)]);
+#pragma unroll
+                for (uint32_t b = 0; b < RT; ++b) acc[e][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, weights[b]), acc[e][b], 0, 0, 0);
+            }
+        }
+    };
+    const int32_t steps = (max(0, end - begin) + int32_t(T) - 1) / int32_t(T);
+    if (steps > 0) {
+        ask_pages(0);
+        ask(0);
+        ask_pages(1);
+        __syncthreads();                                                                // (`lost` is cleared)
+        put(0);
+        ask(1);
+        ask_pages(2);
+        __syncthreads();
+        for (int32_t step = 0; step < steps; ++step) {
+            take(step);
+            put(step + 1);                                                              // (behind the end: nothing that is looked at)
+            ask(step + 2);
+            ask_pages(step + 3);
+            __syncthreads();
+        }
+    }
+    if (missing) flag(p);
+#pragma unroll
+    for (uint32_t b = 0; b < RT; ++b) {
+        sum[b] += __shfl_xor(sum[b], 16);
+        sum[b] += __shfl_xor(sum[b], 32);
+        const uint32_t r = wave * (16u * RT) + 16u * b + c;
+        if (r >= t.n_rows) continue;
+        const float over = p.splits > 1u ? reach : sum[b] == 0.0f ? 0.0f : reach / sum[b];
+        if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b], sum[b]);
+#pragma unroll
+        for (uint32_t e = 0; e < kTiles; ++e) {
+            const floatx4 o = acc[e][b] * over;
+            const uint32_t d = 16u * e + 4u * g;
+            if (p.splits > 1u)
+                *reinterpret_cast<floatx4*>(p.parts + (part * kRows + r) * D + d) = o;
+            else if (p.out_dtype == ANSZP_OUT_BF16)
+                *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + out_at[b] + d) = words2{to_bf16_pair(o[0], o[1]), to_bf16_pair(o[2], o[3])};
+            else
+                *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + out_at[b] + d) = __builtin_bit_cast(words4, o);
+        }
+    }
+}
+
 // The splits' results together: four workgroups per tile and head, a row of it at a time; D / 4 lanes have a split, their sums meet in LDS.
 template <uint32_t D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
@@ -398,11 +700,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     __shared__ floatx4 joined[kGroups][kLanes];
     __shared__ float sums[kGroups], tops[4];
     const uint32_t head = blockIdx.y;
-    const Tile t = find_tile(p, blockIdx.x, kTileRows);
+    const Tile t = find_tile(p, blockIdx.x, p.tile_rows);
     const uint32_t d = threadIdx.x % kLanes, n = threadIdx.x / kLanes;
     const float2* stats = reinterpret_cast<const float2*>(p.part_stats);
     for (uint32_t r = blockIdx.z; r < t.n_rows; r += gridDim.z) {
-        const auto part_of = [&](uint32_t s) { return ((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * kTileRows + r; };
+        const auto part_of = [&](uint32_t s) { return ((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * p.tile_rows + r; };
         float high = -__builtin_inff();
         for (uint32_t s = threadIdx.x; s < p.splits; s += 256u) high = fmaxf(high, stats[part_of(s)].x);
         for (int x = 32; x; x >>= 1) high = fmaxf(high, __shfl_xor(high, x));
@@ -440,19 +742,25 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     }
 }
 
+// Above so many rows per sequence and head of the cache, on average, attend_tile_kernel is the faster one.
+constexpr uint64_t kManyRows = 32u;
+
 // How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of
 // about 1024 tokens, since sequences differ in length and the longest would end last (48 sequences of 17 to 4100 tokens, 32 heads
 // in 4 bits: 184 us with a workgroup for each, %SHARED% with shares).  The lengths are on the device: what the page tables can hold counts.
 struct Shares {
-    uint32_t tiles, splits, span;
+    uint32_t rows, tiles, splits, span;     // rows of a tile: attend_rows_kernel's, or attend_tile_kernel's
 };
 Shares shares_of(const anszp_attend_args_t& a) {
     Shares s;
-    s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / kTileRows + a.n_seqs);
+    const bool many = a.n_tokens * a.group > kManyRows * a.n_seqs;
+    s.rows = !many ? kTileRows : a.cache.head_dim == 256u ? 64u : 128u;
+    s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / s.rows + a.n_seqs);
     const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();
-    uint64_t splits = std::max(2u * cus / groups, std::min<uint64_t>(32u * cus / groups, (most + 1023u) / 1024u));
+    uint64_t splits = 2u * cus / groups;
+    if (!many) splits = std::max(splits, std::min<uint64_t>(32u * cus / groups, (most + 1023u) / 1024u));
     splits = std::max<uint64_t>(1u, std::min<uint64_t>(std::min<uint64_t>(splits, (most + 255u) / 256u), 1024u));
-    const uint64_t whole = kStep * kAttendWaves;
+    const uint64_t whole = 2u * kStep * kAttendWaves;                                   // (the few rows' wavefronts take two turns a round)
     s.span = static_cast<uint32_t>((most + splits * whole - 1u) / (splits * whole) * whole);
     s.splits = static_cast<uint32_t>((most + s.span - 1u) / s.span);
     return s;
@@ -461,19 +769,26 @@ Shares shares_of(const anszp_attend_args_t& a) {
 bool in_range(const anszp_attend_args_t& a) {
     const anszp_cache_t& c = a.cache;
     return !(a.n_tokens >= 1u << 24 || a.n_seqs >= 1u << 24 || a.table_width == 0u || uint64_t(a.table_width) * c.page_size > 1ull << 30 || a.group == 0u ||
-             a.group > 256u || (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || a.n_tokens * a.group / kTileRows + a.n_seqs >= 1ull << 31);
+             a.group > 256u || (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || (a.n_tokens * a.group / kTileRows + a.n_seqs) * c.heads >= 1ull << 31);
 }
 
 uint64_t workspace_of(const anszp_attend_args_t& a, const Shares& s) {
-    return s.splits > 1u ? uint64_t(s.splits) * s.tiles * a.cache.heads * kTileRows * (a.cache.head_dim + 2u) * sizeof(float) : 0u;
+    return s.splits > 1u ? uint64_t(s.splits) * s.tiles * a.cache.heads * s.rows * (a.cache.head_dim + 2u) * sizeof(float) : 0u;
 }
 
 template <uint32_t D>
 void launch(const AttendParams& p, uint32_t bits, hipStream_t s) {
-    const dim3 grid(p.n_tiles, p.heads, p.splits);
-    if (bits == 8u) hipLaunchKernelGGL((attend_rows_kernel<D, 8u>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((attend_rows_kernel<D, 4u>), grid, dim3(256), 0, s, p);
-    if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, 4u), dim3(256), 0, s, p);
+    if (p.tile_rows == kTileRows) {
+        const dim3 grid(p.n_tiles, p.heads, p.splits);
+        if (bits == 8u) hipLaunchKernelGGL((attend_rows_kernel<D, 8u>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((attend_rows_kernel<D, 4u>), grid, dim3(256), 0, s, p);
+    } else {
+        constexpr uint32_t T = D == 256u ? 32u : 64u, RT = D == 256u ? 1u : 2u;
+        const dim3 grid(p.n_tiles * p.heads, p.splits);
+        if (bits == 8u) hipLaunchKernelGGL((attend_tile_kernel<D, 8u, T, RT>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((attend_tile_kernel<D, 4u, T, RT>), grid, dim3(256), 0, s, p);
+    }
+    if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, p.tile_rows / 4u), dim3(256), 0, s, p);
 }
 
 }  // namespace
@@ -500,7 +815,8 @@ int anszp_attend(const anszp_attend_args_t* a, void* hip_stream) {
     p.k = a->cache.k; p.k_params = a->cache.k_params; p.v = a->cache.v; p.v_params = a->cache.v_params;
     p.q = static_cast<const uint16_t*>(a->q); p.out = a->out; p.pages = a->pages; p.lengths = a->lengths; p.starts = a->starts; p.status = a->status;
     p.parts = static_cast<float*>(a->workspace);
-    p.part_stats = p.parts + uint64_t(s.splits) * s.tiles * a->cache.heads * kTileRows * a->cache.head_dim;
+    p.part_stats = p.parts + uint64_t(s.splits) * s.tiles * a->cache.heads * s.rows * a->cache.head_dim;
+    p.tile_rows = s.rows;
     p.n_pages = a->cache.n_pages;
     p.q_token_stride = a->q_token_stride; p.q_head_stride = a->q_head_stride; p.out_token_stride = a->out_token_stride; p.out_head_stride = a->out_head_stride;
     p.n_tokens = static_cast<uint32_t>(a->n_tokens); p.n_seqs = static_cast<uint32_t>(a->n_seqs); p.n_tiles = s.tiles;
