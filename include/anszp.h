@@ -474,7 +474,7 @@ typedef struct {
     float*   k_params;            /* [device] n_pages x heads x page_size x 2, 16-byte aligned; zero-points are whole, 0 .. 2^bits - 1 */
     uint8_t* v;
     float*   v_params;
-    uint64_t n_pages;             /* < 2^31                                                          */
+    uint64_t n_pages;             /* < 2^31, and n_pages * heads * page_size < 2^32                  */
     uint32_t page_size;           /* a power of two from 16 to 65536                                 */
     uint32_t heads;               /* of keys and values, 1 .. 65535                                  */
     uint32_t head_dim;            /* 64, 128 or 256                                                  */

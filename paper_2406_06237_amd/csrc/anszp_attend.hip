@@ -438,6 +438,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
     Bytes<kKeyBytes> key_bytes;
     Bytes<kValueBytes> value_bytes[4];
     float2 key_pair;
+    float value_scale;                                                                  // of the key's token
     words4 value_pairs[2];
     int32_t key_page, value_page;                                                       // of the step to be asked for next
     bool key_there, value_there;                                                        // of what has been asked for
@@ -445,20 +446,21 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
         key_page = page_at(begin + step * int32_t(T) + int32_t(key_token));
         value_page = page_at(begin + step * int32_t(T) + int32_t(quad * 4u));
     };
-    const auto vector_at = [&](int32_t place, int32_t page, bool there) __attribute__((always_inline)) {
-        return ((uint64_t(there ? page : 0) * p.heads + head) << p.page_log) + (uint32_t(place) & ((1u << p.page_log) - 1u));
+    const auto vector_at = [&](int32_t place, int32_t page, bool there) __attribute__((always_inline)) {     // (a cache has fewer than 2^32)
+        return ((uint32_t(there ? page : 0) * p.heads + head) << p.page_log) + (uint32_t(place) & ((1u << p.page_log) - 1u));
     };
     const auto ask = [&](int32_t step) __attribute__((always_inline)) {
         const int32_t key_place = begin + step * int32_t(T) + int32_t(key_token), value_place = begin + step * int32_t(T) + int32_t(quad * 4u);
-        const bool key_known = uint64_t(int64_t(key_page)) < p.n_pages, value_known = uint64_t(int64_t(value_page)) < p.n_pages;
+        const bool key_known = uint32_t(key_page) < uint32_t(p.n_pages), value_known = uint32_t(value_page) < uint32_t(p.n_pages);
         missing |= key_place < end && !key_known;
         key_there = key_place < end && key_known;
         value_there = value_place < end && value_known;
-        const uint64_t kv = vector_at(key_place, key_page, key_there), vv = vector_at(value_place, value_page, value_there);
-        key_bytes.load(p.k + kv * kVector + key_part * kKeyBytes);
+        const uint32_t kv = vector_at(key_place, key_page, key_there), vv = vector_at(value_place, value_page, value_there);
+        key_bytes.load(p.k + uint64_t(kv) * kVector + key_part * kKeyBytes);
         key_pair = reinterpret_cast<const float2*>(p.k_params)[kv];
+        value_scale = p.v_params[2u * uint64_t(kv)];
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i) value_bytes[i].load(p.v + (vv + i) * kVector + chunk * kValueBytes);
+        for (uint32_t i = 0; i < 4u; ++i) value_bytes[i].load(p.v + uint64_t(vv) * kVector + (i * kVector + chunk * kValueBytes));
         value_pairs[0] = reinterpret_cast<const words4*>(p.v_params)[vv / 2u];
         value_pairs[1] = reinterpret_cast<const words4*>(p.v_params)[vv / 2u + 1u];
     };
@@ -477,14 +479,24 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
             }
             key_buffer[to][key_token][place_of_piece<kKeyPieces>(key_token, key_part * (kKeyDims / 8u) + j)] = words4{a[0], a[1], b[0], b[1]};
         }
-        if (key_part == 0u) key_scales[to][key_token] = key_pair.x;
-        float vs[4], vz[4];
+        if (key_part == 0u) {
+            // A value without a scale makes its key's NaN: rows that see the token get NaN, and the weights of others stay 0.
+            const bool held = key_there && begin + step * int32_t(T) + int32_t(key_token) < end, sound = fabsf(value_scale) < __builtin_inff();
+            key_scales[to][key_token] = sound ? key_pair.x : __builtin_nanf("");
+            value_scales[to][key_token] = held && sound ? value_scale : 0.0f;
+        }
+        float vz[4];
 #pragma unroll
         for (uint32_t i = 0; i < 4u; ++i) {
-            const uint32_t si = value_pairs[i / 2u][2u * (i & 1u)], zi = value_pairs[i / 2u][2u * (i & 1u) + 1u];
-            const bool held = value_there && begin + step * int32_t(T) + int32_t(quad * 4u + i) < end;
-            vs[i] = held ? __builtin_bit_cast(float, si) : 0.0f;
-            vz[i] = held ? __builtin_bit_cast(float, zi) : 0.0f;
+            const uint32_t zi = value_pairs[i / 2u][2u * (i & 1u) + 1u];
+            asm volatile("" ::"v"(value_pairs[i / 2u][2u * (i & 1u)]));                 // (the scale came with it: see attend_rows_kernel)
+            vz[i] = __builtin_bit_cast(float, zi);
+        }
+        if (!value_there || begin + (step + 1) * int32_t(T) > end) {                    // what lies behind the end, and pages that are not there
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) {
+                vz[i] = value_there && begin + step * int32_t(T) + int32_t(quad * 4u + i) < end ? vz[i] : 0.0f;
+            }
         }
         const f16x2 z0 = {static_cast<_Float16>(1024.0f + vz[0]), static_cast<_Float16>(1024.0f + vz[1])};
         const f16x2 z1 = {static_cast<_Float16>(1024.0f + vz[2]), static_cast<_Float16>(1024.0f + vz[3])};
@@ -505,7 +517,6 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
             const uint32_t dim = chunk * kValueDims + e;
             value_buffer[to][dim][2u * place_of_piece<kValuePieces>(dim, piece) + half] = words2{bits_of(halves(lo | 0x64006400u) - z0), bits_of(halves(hi | 0x64006400u) - z1)};
         }
-        if (chunk == 0u) *reinterpret_cast<floatx4*>(&value_scales[to][quad * 4u]) = floatx4{vs[0], vs[1], vs[2], vs[3]};
         if (key_part == 0u && (key_token & 15u) == 0u) {
             known[to][key_token / 16u] = key_there ? 1u : 0u;
             if (!key_there && begin + step * int32_t(T) + int32_t(key_token) < end) lost[to] = step;
@@ -515,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
     // the wavefront's queries, scaled into fp16
     const uint32_t own_row = t.first_row + wave * (16u * RT), last_row = t.first_row + t.n_rows - 1u;
     words4 q[RT][kMfmas];
-    float to_scores[RT];
+    float to_exponent[RT];
     int32_t position[RT];
     uint64_t out_at[RT];
 #pragma unroll
@@ -535,8 +546,9 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
         most = most_of_query(most);
         const int32_t exponent = int32_t(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
         const int32_t up = exponent == 128 ? 0 : min(13 - exponent, 126);
-        const float factor = __builtin_bit_cast(float, uint32_t(up + 127) << 23);
-        to_scores[b] = p.scale * __builtin_bit_cast(float, uint32_t(127 - up) << 23);
+        // Scores are kept without the factor that makes them exponents, which is positive: the scale's sign (and a scale of 0) go with the queries.
+        const float factor = __builtin_bit_cast(float, uint32_t(up + 127) << 23) * (p.scale > 0.0f ? 1.0f : p.scale < 0.0f ? -1.0f : 0.0f * p.scale);
+        to_exponent[b] = fmaxf(fabsf(p.scale) * __builtin_bit_cast(float, uint32_t(127 - up) << 23), 0x1p-126f);
 #pragma unroll
         for (uint32_t m = 0; m < kMfmas; ++m) {
             constexpr uint32_t kOrder4[8] = {0, 2, 4, 6, 1, 3, 5, 7};
@@ -594,9 +606,8 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b)
 #pragma unroll
-                    for (uint32_t i = 0; i < 4u; ++i) y[b][4u * u + i] = s[b][i] * (ks[i] * to_scores[b]);
+                    for (uint32_t i = 0; i < 4u; ++i) y[b][4u * u + i] = s[b][i] * ks[i];
             }
-            uint32_t unseen[RT] = {};
             const bool whole = !lacking && t0 + 31 <= least_position && t0 + 32 <= end;
             if (!whole) {
 #pragma unroll
@@ -605,26 +616,21 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
                     const bool held = place < end && known[in][2u * h + n / 4u];
 #pragma unroll
                     for (uint32_t b = 0; b < RT; ++b)
-                        if (!held || place > position[b]) {
-                            y[b][n] = -__builtin_inff();
-                            unseen[b] |= 1u << n;
-                        }
+                        y[b][n] = held && place <= position[b] ? y[b][n] : -__builtin_inff();
                 }
             }
             bool grows = false;
             float high[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
-                high[b] = y[b][0];
-#pragma unroll
-                for (uint32_t n = 1; n < 8u; ++n) high[b] = fmaxf(high[b], y[b][n]);
+                high[b] = fmaxf(fmaxf(fmaxf(y[b][0], y[b][1]), fmaxf(fmaxf(y[b][2], y[b][3]), y[b][4])), fmaxf(fmaxf(y[b][5], y[b][6]), y[b][7]));
                 grows |= high[b] > top[b];
             }
             if (__any(grows)) {
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b) {
                     const float now = fmaxf(top[b], most_of_query(high[b]));
-                    const float kept = __builtin_amdgcn_exp2f(top[b] - (now == -__builtin_inff() ? 0.0f : now));
+                    const float kept = __builtin_amdgcn_exp2f((top[b] - (now == -__builtin_inff() ? 0.0f : now)) * to_exponent[b]);
                     top[b] = now;
                     sum[b] *= kept;
 #pragma unroll
@@ -634,13 +640,13 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
             words4 weights[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
-                const float safe = (top[b] == -__builtin_inff() ? 0.0f : top[b]) - 15.0f;
+                const float less_top = 15.0f - (top[b] == -__builtin_inff() ? 0.0f : top[b]) * to_exponent[b];
 #pragma unroll
                 for (uint32_t n = 0; n < 8u; n += 2u) {
-                    const float e0 = __builtin_amdgcn_exp2f(y[b][n] - safe), e1 = __builtin_amdgcn_exp2f(y[b][n + 1u] - safe);
-                    sum[b] += e0 + e1;
-                    weights[b][n / 2u] = bits_of(f16x2{static_cast<_Float16>(e0), static_cast<_Float16>(e1)} * ratio[n / 2u]);
-                    if (!whole) weights[b][n / 2u] &= (unseen[b] >> n & 1u ? 0u : 0x0000FFFFu) | (unseen[b] >> n & 2u ? 0u : 0xFFFF0000u);
+                    const f16x2 e = {static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n], to_exponent[b], less_top))),
+                                     static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n + 1u], to_exponent[b], less_top)))};
+                    sum[b] = __builtin_amdgcn_fdot2(e, f16x2{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)}, sum[b], false);
+                    weights[b][n / 2u] = bits_of(e * ratio[n / 2u]);
                 }
             }
 #pragma unroll
@@ -678,7 +684,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
         const uint32_t r = wave * (16u * RT) + 16u * b + c;
         if (r >= t.n_rows) continue;
         const float over = p.splits > 1u ? reach : sum[b] == 0.0f ? 0.0f : reach / sum[b];
-        if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b], sum[b]);
+        if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b] * to_exponent[b], sum[b]);
 #pragma unroll
         for (uint32_t e = 0; e < kTiles; ++e) {
             const floatx4 o = acc[e][b] * over;

@@ -157,7 +157,8 @@ extern "C" {
 int anszp_cache_check(const anszp_cache_t* c) {
     if (!c) return ANSZP_E_NULL;
     if (c->page_size < 16u || c->page_size > 65536u || (c->page_size & (c->page_size - 1u)) || c->heads == 0u || c->heads > 65535u ||
-        (c->head_dim != 64u && c->head_dim != 128u && c->head_dim != 256u) || (c->bits != 8u && c->bits != 4u) || c->n_pages >= 1ull << 31)
+        (c->head_dim != 64u && c->head_dim != 128u && c->head_dim != 256u) || (c->bits != 8u && c->bits != 4u) || c->n_pages >= 1ull << 31 ||
+        c->n_pages * c->heads >= (1ull << 32) / c->page_size)            // (no GPU has memory for 2^32 vectors)
         return ANSZP_E_RANGE;
     if (c->n_pages && (!c->k || !c->v || !c->k_params || !c->v_params)) return ANSZP_E_NULL;
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) return ANSZP_E_RANGE;
