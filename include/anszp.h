@@ -460,10 +460,14 @@ typedef struct {
     uint32_t     x_dtype;         /* ANSZP_OUT_BF16 or ANSZP_I8                                      */
     uint32_t     out_dtype;       /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
     uint32_t     zero_point;      /* 0 .. 255; with x in ANSZP_I8 only                               */
-    uint32_t     activation;      /* ANSZP_FN_*                                                    */
+    uint32_t     activation;      /* ANSZP_FN_*                                                      */
     float        scale;
+    void*        workspace;       /* [device] anszp_linear_workspace_bytes, 16-byte aligned, in use until the call is done; or NULL: */
+    uint64_t     workspace_bytes; /* products that would share k out over more of the chip take longer then                */
 } anszp_linear_args_t;
-/* Errors: E_NULL, E_RANGE, E_HIP. */
+/* [host only] Bytes of workspace with which a call is fastest (0: none); reads sizes only, no pointers. */
+uint64_t anszp_linear_workspace_bytes(const anszp_linear_args_t* args);
+/* Errors: E_NULL, E_RANGE (also for a workspace that is too small), E_HIP. */
 int anszp_linear(const anszp_linear_args_t* args, void* hip_stream);
 
 /* A paged cache of keys and values in 8 or 4 bits.  A slot is a token's place: page * page_size + token in page.  A vector (one

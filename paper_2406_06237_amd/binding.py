@@ -82,7 +82,7 @@ class LinearArgs(C.Structure):
                 ("mul", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
                 ("x_stride", C.c_uint64), ("weight_stride", C.c_uint64), ("mul_stride", C.c_uint64), ("residual_stride", C.c_uint64),
                 ("out_stride", C.c_uint64), ("k", C.c_uint32), ("x_dtype", C.c_uint32), ("out_dtype", C.c_uint32), ("zero_point", C.c_uint32),
-                ("activation", C.c_uint32), ("scale", C.c_float)]
+                ("activation", C.c_uint32), ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
 class CacheArg(C.Structure):
@@ -110,7 +110,7 @@ EXPORTS = ["anszp_version", "anszp_strerror", "anszp_normalize_freqs", "anszp_bu
            "anszp_dequant_zp", "anszp_conv_fused", "anszp_pack_layer_device",
            "anszp_plan_bytes", "anszp_plan_decode", "anszp_decode_planned", "anszp_decode_static_plan",
            "anszp_pack_layers_device", "anszp_pack_scratch_bytes", "anszp_pack_set_device", "anszp_test_set_spin_limit",
-           "anszp_rms_norm", "anszp_linear", "anszp_cache_check", "anszp_cache_write", "anszp_cache_read", "anszp_attend_workspace_bytes", "anszp_attend"]
+           "anszp_rms_norm", "anszp_linear_workspace_bytes", "anszp_linear", "anszp_cache_check", "anszp_cache_write", "anszp_cache_read", "anszp_attend_workspace_bytes", "anszp_attend"]
 
 
 def lib():
@@ -158,6 +158,8 @@ def lib():
         L.anszp_test_set_spin_limit.restype = None
         L.anszp_rms_norm.argtypes = [C.c_void_p, C.c_void_p]
         L.anszp_linear.argtypes = [C.c_void_p, C.c_void_p]
+        L.anszp_linear_workspace_bytes.argtypes = [C.c_void_p]
+        L.anszp_linear_workspace_bytes.restype = C.c_uint64
         L.anszp_cache_check.argtypes = [C.c_void_p]
         L.anszp_cache_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint64,
                                         C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]
@@ -940,7 +942,12 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
         a.residual, a.residual_stride = _want(residual, "residual", dev, (rows, cols), out.dtype), residual.stride(0)
     a.rows, a.cols, a.k, a.x_stride, a.weight_stride, a.out_stride = rows, cols, k, x.stride(0), weight.stride(0), out.stride(0)
     a.x_dtype, a.out_dtype, a.zero_point, a.activation, a.scale = _CODE_OF[str(x.dtype)], _CODE_OF[str(out.dtype)], zero_point, FN_CODES[activation], scale
-    _enqueue("anszp_linear", lib().anszp_linear, dev, C.addressof(a))
+    L = lib()
+    need = L.anszp_linear_workspace_bytes(C.addressof(a))
+    if need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+    _enqueue("anszp_linear", L.anszp_linear, dev, C.addressof(a))
     return out
 
 

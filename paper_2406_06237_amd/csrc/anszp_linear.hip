@@ -12,6 +12,8 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "anszp_cus.h"
+#include "anszp_linear_plan.h"
 #include "anszp_numbers.h"
 
 namespace {
@@ -31,6 +33,10 @@ struct LinearParams {
     uint32_t k_bytes, activation, out_dtype;
     int32_t offset;                     // 128 - zero_point
     float scale;
+    // k in shares: sums of 32 bits, [share][rows][cols up to a multiple of 8], that linear_join_kernel adds up; NULL: none
+    uint32_t* parts;
+    uint32_t shares, share_steps;       // whole steps of 128 bytes a share has; the last one has what is left of k, too
+    uint64_t parts_stride;              // columns of a row
 };
 
 __device__ __forceinline__ float activated(float v, uint32_t activation) {
@@ -171,10 +177,10 @@ struct Sums<true> {
 // time through LDS.  A row of a tile is 8 pieces of 16 bytes; piece j of row r lies in place j ^ (r & 7), so that the 16 lanes that
 // read one piece of 16 rows each meet no bank more than twice.
 template <bool BYTES>
-__global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p) {
+__global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, uint32_t tiles_c) {
     __shared__ words4 tile[2][64][8];                               // weights, activations
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint64_t c0 = uint64_t(blockIdx.x) * 64u, r0 = uint64_t(blockIdx.y) * 64u;
+    const uint64_t c0 = uint64_t(blockIdx.x % tiles_c) * 64u, r0 = uint64_t(blockIdx.x / tiles_c) * 64u;
     typename Sums<BYTES>::type acc[2][2] = {}, ones[2] = {};
     const words4 all_one = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
     for (uint32_t k0 = 0; k0 < p.k_bytes; k0 += 128u) {
@@ -219,9 +225,9 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p) {
 // 16 * CH channels and all rows (16 * TOK at most); its wavefronts share k, 256 bytes of a row at a time each, and their sums meet in LDS.
 // Lane (c, g), c = lane % 16, g = lane / 16, feeds bytes [64 u + 16 g, 64 u + 16 g + 16) of weight row c and of activation row c.
 // Rows of either that do not exist are the last one again; their sums are not stored.
-template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WAVES>
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WAVES, uint32_t PIECES>
 __global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p) {
-    constexpr uint32_t kPieces = 4u, kChunk = 64u * kPieces;
+    constexpr uint32_t kPieces = PIECES, kChunk = 64u * kPieces;
     typedef typename Sums<BYTES>::type sums;
     __shared__ sums joined[WAVES][(CH + (BYTES ? 1u : 0u)) * TOK][64];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
@@ -306,19 +312,12 @@ __global__ __launch_bounds__(WAVES * 64u) void linear_few_kernel(LinearParams p)
     }
 }
 
-template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WAVES>
-void launch_few(const LinearParams& p, hipStream_t s) {
-    const dim3 grid(static_cast<uint32_t>((p.cols + 16u * CH - 1u) / (16u * CH)), static_cast<uint32_t>((p.rows + 16u * TOK - 1u) / (16u * TOK)));
-    hipLaunchKernelGGL((linear_few_kernel<BYTES, TOK, CH, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
-}
-
-template <bool BYTES>
-bool take_few(const LinearParams& p, hipStream_t s) {
-    if (p.k_bytes < 16u) return false;
-    if (p.rows <= 16u) launch_few<BYTES, 1u, 1u, 8u>(p, s);
-    else if (p.rows <= 32u) launch_few<BYTES, 2u, 1u, 8u>(p, s);
-    else if (p.rows <= 64u) launch_few<BYTES, 4u, 1u, 8u>(p, s);
-    else return false;
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t PIECES>
+bool launch_few(const LinearParams& p, hipStream_t s) {
+    constexpr uint32_t kWaves = 8u;
+    const uint64_t groups_c = (p.cols + 16u * CH - 1u) / (16u * CH), groups_t = (p.rows + 16u * TOK - 1u) / (16u * TOK);
+    if (groups_c >= 1ull << 31 || groups_t > 65535u) return false;
+    hipLaunchKernelGGL((linear_few_kernel<BYTES, TOK, CH, kWaves, PIECES>), dim3(static_cast<uint32_t>(groups_c), static_cast<uint32_t>(groups_t)), dim3(kWaves * 64u), 0, s, p);
     return true;
 }
 
@@ -374,7 +373,8 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
 
     // Where this thread's pieces come from: bytes behind the tile's first row of activations or weights (rows that do not exist are the last one
     // again), for a step with what of k lies before it.
-    const uint8_t *const x_tile = p.x + t0 * p.x_stride, *const w_tile = p.w + c0 * p.w_stride;
+    const uint32_t all_whole = p.k_bytes / kStepBytes, before = blockIdx.y * p.share_steps;      // steps of the shares before this one
+    const uint8_t *const x_tile = p.x + t0 * p.x_stride + before * kStepBytes, *const w_tile = p.w + c0 * p.w_stride + before * kStepBytes;
     const uint32_t x_last = uint32_t(least(p.rows - t0, TOK) - 1u), w_last = uint32_t(least(p.cols - c0, CH) - 1u);
     const uint32_t piece = 16u * ((threadIdx.x & 7u) ^ ((threadIdx.x >> 4) & 7u));
     uint32_t from[kLoads];
@@ -385,13 +385,14 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
     }
     const auto operand = [&](uint32_t i) __attribute__((always_inline)) { return i * kThreads < TOK * 8u ? x_tile : w_tile; };
     // Step 0 is what is left of k behind the whole steps, if anything.
-    const uint32_t whole = p.k_bytes / kStepBytes, rest = p.k_bytes % kStepBytes ? 1u : 0u, steps = whole + rest;
+    const uint32_t whole = min(p.share_steps, all_whole - before), rest = blockIdx.y + 1u == p.shares && p.k_bytes % kStepBytes ? 1u : 0u, steps = whole + rest;
+    const uint32_t row_end = p.k_bytes - before * kStepBytes;
     words4 held[kLoads];
     const auto load = [&](uint32_t s) __attribute__((always_inline)) {
         if (s >= steps) return;
         if (s < rest) {
 #pragma unroll
-            for (uint32_t i = 0; i < kLoads; ++i) held[i] = piece_of_long(operand(i) + from[i], whole * kStepBytes + piece, p.k_bytes);
+            for (uint32_t i = 0; i < kLoads; ++i) held[i] = piece_of_long(operand(i) + from[i], whole * kStepBytes + piece, row_end);
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) held[i] = *reinterpret_cast<const words4_any*>(operand(i) + (s - rest) * kStepBytes + (from[i] + piece));
@@ -500,8 +501,12 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
                 floatx4 four;
 #pragma unroll
                 for (uint32_t e = 0; e < 4u; ++e) {
-                    if constexpr (BYTES) four[e] = float(acc[a][b][4u * i + e] + more);
-                    else four[e] = acc[a][b][4u * i + e];
+                    if constexpr (BYTES) {
+                        const int32_t sum = acc[a][b][4u * i + e] + more;
+                        four[e] = p.parts ? __builtin_bit_cast(float, sum) : float(sum);
+                    } else {
+                        four[e] = acc[a][b][4u * i + e];
+                    }
                 }
                 part[r][(a * 8u + 2u * i + (lane >> 5)) ^ (r & 7u)] = four;
             }
@@ -509,46 +514,115 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
         const uint32_t own = lane % kLanes;
         for (uint32_t n = lane / kLanes; n < 32u; n += 64u / kLanes) {
             const floatx4 lo = part[n][(2u * own) ^ (n & 7u)], hi = part[n][(2u * own + 1u) ^ (n & 7u)];
-            const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<8u>(p, t0 + wt * (TOK / WT) + b * 32u + n, c0 + wc * kWidth + own * 8u, sum);
+            const uint64_t row = t0 + wt * (TOK / WT) + b * 32u + n, col = c0 + wc * kWidth + own * 8u;
+            if (p.parts) {
+                if (row < p.rows && col < p.cols) {
+                    floatx4* const to = reinterpret_cast<floatx4*>(p.parts + (blockIdx.y * p.rows + row) * p.parts_stride + col);
+                    to[0] = lo;
+                    to[1] = hi;
+                }
+            } else {
+                const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                finish<8u>(p, row, col, sum);
+            }
         }
         __builtin_amdgcn_wave_barrier();
     }
 }
 
+// The shares' sums together, eight channels a thread, and the epilogue.
+template <bool BYTES>
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
+    const uint64_t n = (uint64_t(blockIdx.x) * 256u + threadIdx.x) * 8u, row = n / p.parts_stride, col = n - row * p.parts_stride;
+    if (row >= p.rows) return;
+    typedef typename Sums<BYTES>::type sums;
+    const sums* from = reinterpret_cast<const sums*>(p.parts + n);
+    sums lo = from[0], hi = from[1];
+    for (uint32_t s = 1; s < p.shares; ++s) {
+        from = reinterpret_cast<const sums*>(p.parts + s * p.rows * p.parts_stride + n);
+        lo += from[0];
+        hi += from[1];
+    }
+    const float sum[8] = {float(lo[0]), float(lo[1]), float(lo[2]), float(lo[3]), float(hi[0]), float(hi[1]), float(hi[2]), float(hi[3])};
+    finish<8u>(p, row, col, sum);
+}
+
 template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC>
-void launch_tile(const LinearParams& p, bool direct, hipStream_t s) {
-    const uint32_t tiles_c = static_cast<uint32_t>((p.cols + CH - 1u) / CH), tiles_t = static_cast<uint32_t>((p.rows + TOK - 1u) / TOK);
-    if (direct) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC>), dim3(tiles_c * tiles_t), dim3(WT * WC * 64u), 0, s, p, tiles_c, tiles_t);
-    else hipLaunchKernelGGL((linear_tile_kernel<BYTES, false, TOK, CH, WT, WC>), dim3(tiles_c * tiles_t), dim3(WT * WC * 64u), 0, s, p, tiles_c, tiles_t);
+bool launch_tile(const LinearParams& p, bool direct, hipStream_t s) {
+    const uint64_t tiles_c = (p.cols + CH - 1u) / CH, tiles_t = (p.rows + TOK - 1u) / TOK, joins = (p.rows * p.parts_stride / 8u + 255u) / 256u;
+    if (tiles_c * tiles_t >= 1ull << 31 || (p.parts && joins >= 1ull << 31)) return false;
+    const dim3 grid(static_cast<uint32_t>(tiles_c * tiles_t), p.shares), threads(WT * WC * 64u);
+    const uint32_t c = static_cast<uint32_t>(tiles_c), t = static_cast<uint32_t>(tiles_t);
+    if (direct) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC>), grid, threads, 0, s, p, c, t);
+    else hipLaunchKernelGGL((linear_tile_kernel<BYTES, false, TOK, CH, WT, WC>), grid, threads, 0, s, p, c, t);
+    if (p.parts) hipLaunchKernelGGL(linear_join_kernel<BYTES>, dim3(static_cast<uint32_t>(joins)), dim3(256), 0, s, p);
+    return true;
+}
+
+template <bool BYTES>
+bool launch(const LinearParams& p, LinearKernel kernel, hipStream_t s) {
+    const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | p.x_stride | p.w_stride) & 15u) == 0u;
+    switch (kernel) {
+        case kFew11: return launch_few<BYTES, 1u, 1u, 4u>(p, s);
+        case kFew21: return launch_few<BYTES, 2u, 1u, 2u>(p, s);
+        case kFew22: return launch_few<BYTES, 2u, 2u, 2u>(p, s);
+        case kFew24: return launch_few<BYTES, 2u, 4u, 2u>(p, s);
+        case kTile64: return launch_tile<BYTES, 64u, 64u, 2u, 2u>(p, direct, s);
+        case kTile128: return launch_tile<BYTES, 128u, 128u, 2u, 2u>(p, direct, s);
+        case kTile192: return launch_tile<BYTES, 192u, 256u, 2u, 4u>(p, direct, s);
+        case kTile256: return launch_tile<BYTES, 256u, 256u, 4u, 2u>(p, direct, s);
+        default: break;
+    }
+    const uint64_t tiles_c = (p.cols + 63u) / 64u, tiles_t = (p.rows + 63u) / 64u;
+    if (tiles_c * tiles_t >= 1ull << 31) return false;
+    hipLaunchKernelGGL(linear_any_kernel<BYTES>, dim3(static_cast<uint32_t>(tiles_c * tiles_t)), dim3(256), 0, s, p, static_cast<uint32_t>(tiles_c));
+    return true;
+}
+
+// The call's parameters but for its shares of k; an error code.
+int linear_params(const anszp_linear_args_t& a, LinearParams& p) {
+    const bool bytes = a.x_dtype == ANSZP_I8;
+    if ((!bytes && a.x_dtype != ANSZP_OUT_BF16) || (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || a.activation > ANSZP_FN_SILU ||
+        a.k == 0 || a.k > (bytes ? 65536u : 1u << 30) || a.rows >= 1ull << 31 || a.cols >= 1ull << 31 || a.zero_point > 255u)
+        return ANSZP_E_RANGE;
+    if (a.rows > 1 && a.out_stride < a.cols) return ANSZP_E_RANGE;
+    const uint32_t size = bytes ? 1u : 2u;
+    p = {};
+    p.x = static_cast<const uint8_t*>(a.x); p.w = static_cast<const uint8_t*>(a.weight); p.x_scales = a.x_scales; p.channel_scales = a.channel_scales;
+    p.bias = a.bias; p.mul = a.mul; p.residual = a.residual; p.out = a.out;
+    p.x_stride = a.rows > 1 ? a.x_stride * size : 0u; p.w_stride = a.cols > 1 ? a.weight_stride * size : 0u;      // (the stride of a single row says nothing)
+    p.mul_stride = a.mul_stride; p.residual_stride = a.residual_stride; p.out_stride = a.out_stride;
+    p.rows = a.rows; p.cols = a.cols; p.k_bytes = a.k * size; p.activation = a.activation; p.out_dtype = a.out_dtype;
+    p.offset = 128 - static_cast<int32_t>(a.zero_point); p.scale = a.scale;
+    return ANSZP_OK;
+}
+
+LinearPlan plan_of(const anszp_linear_args_t& a, const LinearParams& p, bool may_share) {
+    return linear_plan(a.x_dtype == ANSZP_I8, p.rows, p.cols, p.k_bytes, p.x_stride, p.w_stride, device_cus(), may_share);
 }
 
 }  // namespace
 
+extern "C" uint64_t anszp_linear_workspace_bytes(const anszp_linear_args_t* a) {
+    LinearParams p;
+    if (!a || linear_params(*a, p) || a->rows == 0 || a->cols == 0) return 0u;
+    return plan_of(*a, p, true).workspace;
+}
+
 extern "C" int anszp_linear(const anszp_linear_args_t* a, void* hip_stream) {
     if (!a) return ANSZP_E_NULL;
-    const bool bytes = a->x_dtype == ANSZP_I8;
-    if ((!bytes && a->x_dtype != ANSZP_OUT_BF16) || (a->out_dtype != ANSZP_OUT_F32 && a->out_dtype != ANSZP_OUT_BF16) || a->activation > ANSZP_FN_SILU ||
-        a->k == 0 || a->k > (bytes ? 65536u : 1u << 30) || a->rows >= 1ull << 31 || a->cols >= 1ull << 31 || a->zero_point > 255u)
-        return ANSZP_E_RANGE;
-    if (a->rows > 1 && a->out_stride < a->cols) return ANSZP_E_RANGE;
+    LinearParams p;
+    const int rc = linear_params(*a, p);
+    if (rc) return rc;
     if (a->rows == 0 || a->cols == 0) return ANSZP_OK;
     if (!a->x || !a->weight || !a->out) return ANSZP_E_NULL;
-    const uint32_t size = bytes ? 1u : 2u;
-    LinearParams p = {static_cast<const uint8_t*>(a->x), static_cast<const uint8_t*>(a->weight), a->x_scales, a->channel_scales, a->bias, a->mul, a->residual, a->out,
-                      a->x_stride * size, a->weight_stride * size, a->mul_stride, a->residual_stride, a->out_stride, a->rows, a->cols,
-                      a->k * size, a->activation, a->out_dtype, 128 - static_cast<int32_t>(a->zero_point), a->scale};
-    const dim3 grid(static_cast<uint32_t>((p.cols + 63u) / 64u), static_cast<uint32_t>((p.rows + 63u) / 64u));
-    if (grid.y > 65535u) return ANSZP_E_RANGE;
+    const LinearPlan plan = plan_of(*a, p, a->workspace != nullptr);
+    if (plan.workspace && (a->workspace_bytes < plan.workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u))) return ANSZP_E_RANGE;
+    p.shares = plan.shares;
+    p.share_steps = plan.share_steps;
+    p.parts_stride = plan.parts_stride;
+    p.parts = plan.shares > 1u ? static_cast<uint32_t*>(a->workspace) : nullptr;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (bytes ? take_few<true>(p, s) : take_few<false>(p, s)) return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
-    const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | p.x_stride | p.w_stride) & 15u) == 0u;
-    if (p.rows > 128u && p.k_bytes >= 16u && std::max(p.x_stride, p.w_stride) <= 1u << 23) {
-        if (bytes) launch_tile<true, 256u, 256u, 4u, 2u>(p, direct, s);
-        else launch_tile<false, 256u, 256u, 4u, 2u>(p, direct, s);
-        return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
-    }
-    if (bytes) hipLaunchKernelGGL(linear_any_kernel<true>, grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(linear_any_kernel<false>, grid, dim3(256), 0, s, p);
+    if (!(a->x_dtype == ANSZP_I8 ? launch<true>(p, plan.kernel, s) : launch<false>(p, plan.kernel, s))) return ANSZP_E_RANGE;
     return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
 }

@@ -96,6 +96,12 @@ py::object linear(const at::Tensor& x, const at::Tensor& weight, const Maybe& x_
         a.x_stride = rows_apart(x); a.weight_stride = rows_apart(weight); a.mul_stride = mul ? rows_apart(*mul) : 0u;
         a.residual_stride = residual ? rows_apart(*residual) : 0u; a.out_stride = rows_apart(*out);
         a.x_dtype = code_of(x); a.out_dtype = code_of(*out); a.zero_point = uint32_t(zero_point); a.activation = activation; a.scale = float(scale);
+        at::Tensor workspace;
+        a.workspace_bytes = anszp_linear_workspace_bytes(&a);
+        if (a.workspace_bytes) {
+            workspace = at::empty({int64_t(a.workspace_bytes)}, x.options().dtype(at::kByte));
+            a.workspace = workspace.data_ptr();
+        }
         return anszp_linear(&a, stream_of(stream));
     });
     return rc ? failed(rc) : py::cast(*out);

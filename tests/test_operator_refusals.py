@@ -118,7 +118,7 @@ def calls(monkeypatch):
 
     class Stub:
         def __getattr__(self, name):
-            if name == "anszp_attend_workspace_bytes":
+            if name in ("anszp_attend_workspace_bytes", "anszp_linear_workspace_bytes"):
                 return getattr(real, name)
             return lambda *args: seen.append(name) or 0
 
