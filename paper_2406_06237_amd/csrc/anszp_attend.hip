@@ -23,6 +23,7 @@
 namespace {
 
 constexpr uint32_t kTileRows = 16u, kStep = 32u, kAttendWaves = 4u;      // of attend_rows_kernel
+constexpr uint32_t kMostSplits = 1024u;
 
 struct AttendParams {
     const uint8_t* k;
@@ -705,6 +706,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     constexpr uint32_t kLanes = D / 4u, kGroups = 256u / kLanes;
     __shared__ floatx4 joined[kGroups][kLanes];
     __shared__ float sums[kGroups], tops[4];
+    __shared__ float2 stats_of[kMostSplits];
     const uint32_t head = blockIdx.y;
     const Tile t = find_tile(p, blockIdx.x, p.tile_rows);
     const uint32_t d = threadIdx.x % kLanes, n = threadIdx.x / kLanes;
@@ -712,7 +714,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     for (uint32_t r = blockIdx.z; r < t.n_rows; r += gridDim.z) {
         const auto part_of = [&](uint32_t s) { return ((uint64_t(s) * p.n_tiles + blockIdx.x) * p.heads + head) * p.tile_rows + r; };
         float high = -__builtin_inff();
-        for (uint32_t s = threadIdx.x; s < p.splits; s += 256u) high = fmaxf(high, stats[part_of(s)].x);
+        for (uint32_t s = threadIdx.x; s < p.splits; s += 256u) {
+            stats_of[s] = stats[part_of(s)];
+            high = fmaxf(high, stats_of[s].x);
+        }
         for (int x = 32; x; x >>= 1) high = fmaxf(high, __shfl_xor(high, x));
         if ((threadIdx.x & 63u) == 0u) tops[threadIdx.x >> 6] = high;
         __syncthreads();
@@ -720,12 +725,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
         const float safe = high == -__builtin_inff() ? 0.0f : high;
         floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
         float l = 0.0f;
-        for (uint32_t s = n; s < p.splits; s += kGroups) {
-            const float2 w = stats[part_of(s)];
-            if (w.y == 0.0f) continue;                                                  // (nothing was written for it)
-            const float by = __builtin_amdgcn_exp2f(w.x - safe);
-            l += w.y * by;
-            o += *reinterpret_cast<const floatx4*>(p.parts + part_of(s) * D + 4u * d) * by;
+        for (uint32_t first = n; first < p.splits; first += 4u * kGroups) {               // four of them under way
+            floatx4 part[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4u; ++u)
+                part[u] = *reinterpret_cast<const floatx4*>(p.parts + part_of(min(first + u * kGroups, p.splits - 1u)) * D + 4u * d);
+#pragma unroll
+            for (uint32_t u = 0; u < 4u; ++u) {
+                const uint32_t s = first + u * kGroups;
+                const float2 w = stats_of[min(s, p.splits - 1u)];
+                if (s >= p.splits || w.y == 0.0f) continue;                                 // (where the sum is nothing no part was written)
+                const float by = __builtin_amdgcn_exp2f(w.x - safe);
+                l += w.y * by;
+                o += part[u] * by;
+            }
         }
         joined[n][d] = o;
         if (d == 0u) sums[n] = l;
@@ -753,7 +766,7 @@ constexpr uint64_t kManyRows = 32u;
 
 // How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of
 // about 1024 tokens, since sequences differ in length and the longest would end last (48 sequences of 17 to 4100 tokens, 32 heads
-// in 4 bits: 184 us with a workgroup for each, %SHARED% with shares).  The lengths are on the device: what the page tables can hold counts.
+// in 4 bits: 184 us with a workgroup for each, 135 with shares).  The lengths are on the device: what the page tables can hold counts.
 struct Shares {
     uint32_t rows, tiles, splits, span;     // rows of a tile: attend_rows_kernel's, or attend_tile_kernel's
 };
@@ -765,7 +778,7 @@ Shares shares_of(const anszp_attend_args_t& a) {
     const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();
     uint64_t splits = 2u * cus / groups;
     if (!many) splits = std::max(splits, std::min<uint64_t>(32u * cus / groups, (most + 1023u) / 1024u));
-    splits = std::max<uint64_t>(1u, std::min<uint64_t>(std::min<uint64_t>(splits, (most + 255u) / 256u), 1024u));
+    splits = std::max<uint64_t>(1u, std::min<uint64_t>(std::min<uint64_t>(splits, (most + 255u) / 256u), kMostSplits));
     const uint64_t whole = 2u * kStep * kAttendWaves;                                   // (the few rows' wavefronts take two turns a round)
     s.span = static_cast<uint32_t>((most + splits * whole - 1u) / (splits * whole) * whole);
     s.splits = static_cast<uint32_t>((most + s.span - 1u) / s.span);

@@ -7,9 +7,9 @@
 //
 // Memory is what bounds both kernels, and instructions nearly: a lane has 8 elements, head_dim / 8 lanes a vector, so that 16 bytes in and 8 (or 4)
 // bytes out per lane lie one behind the other; the vector's extremes are found in log2(head_dim / 8) exchanges between those lanes.  8191 tokens
-// of 32 heads of 128 in bfloat16, keys and values, 4 bits: written in 40 us and read back in 40, 4.25 TB/s of what both read and write (a large copy
+// of 32 heads of 128 in bfloat16, keys and values, 4 bits: written in 46 us and read back in 35, 4.25 TB/s of what both read and write (a large copy
 // reaches 4.83).  (The writing took 57 us while the elements were asked for behind their slot's check, the exchanges went through LDS and symbols were
-// packed one shift at a time.)  16 tokens of the same, 8 bits, take 3.7 and 3.3 us, which is an empty launch's time.
+// packed one shift at a time.)  16 tokens of the same, 8 bits, take 3.1 and 3.0 us, which is an empty launch's time.
 #include <hip/hip_runtime.h>
 
 #include "anszp_numbers.h"
