@@ -11,8 +11,10 @@
 //     the dimensions [c D / 16, (c + 1) D / 16) of their values, 16 lanes reading a value end to end, and the bytes of one dimension
 //     are brought together by v_perm_b32.  Nothing passes through LDS but the join of the wavefronts' results.
 // Queries are scaled per row by a power of two that puts the largest element in [2^13, 2^14) (exact for all that is within 2^27 of it);
-// weights are 2^15 exp2(score - m) times the value's scale over the power of two above the largest seen: 11 bits for all weights down
-// to 2^-29 of the largest.
+// weights are 2^9 exp2(score - m) times the value's scale over the power of two above the largest seen: 11 bits for all weights down
+// to 2^-23 of the largest, and less than 2^-34 of it lost of any other.  The 2^6 left below fp16's largest number are for scores that pass m: m
+// and all that was summed under it are changed only where one does so by more than 6 (as log2), or, of 32 queries, some row's maximum would
+// grow in most steps of a few thousand tokens.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,7 +25,9 @@
 namespace {
 
 constexpr uint32_t kTileRows = 16u, kStep = 32u, kAttendWaves = 4u;      // of attend_rows_kernel
+constexpr uint32_t kManyTile = 128u;                                     // rows of attend_tile_kernel's workgroup
 constexpr uint32_t kMostSplits = 1024u;
+constexpr float kSlack = 6.0f;                                           // (see the weights above)
 
 struct AttendParams {
     const uint8_t* k;
@@ -246,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     }
 
     floatx4 acc[kTiles] = {};
-    float top = -__builtin_inff(), sum = 0.0f, reach = 0.0f, less = 0.0f;               // m, the lane's part of l, the values' power of two and 1 over it
+    float top = -__builtin_inff(), limit = top, sum = 0.0f, reach = 0.0f, less = 0.0f;  // m, what a score may reach before m is, the lane's part of l, the values' power of two and 1 over it
     const auto take = [&](const Step& step, int32_t t0) __attribute__((always_inline)) {
         float x[8], vs[8], vz[8];
 #pragma unroll
@@ -293,18 +297,19 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
             high = fmaxf(high, x[n]);
             far = fmaxf(far, fabsf(vs[n]));
         }
-        if (__any(high > top || far > reach)) {
+        if (__any(high > limit || far > reach)) {
             high = fmaxf(top, most_of_query(high));
             far = fmaxf(reach, power_above(most_of_query(far)));
             less = far > 0.0f ? 1.0f / far : 0.0f;
             const float kept = __builtin_amdgcn_exp2f(top - (high == -__builtin_inff() ? 0.0f : high)), kept_values = kept * (reach * less);
             top = high;
+            limit = high + kSlack;
             reach = far;
             sum *= kept;
 #pragma unroll
             for (uint32_t e = 0; e < kTiles; ++e) acc[e] *= kept_values;
         }
-        const float safe = (top == -__builtin_inff() ? 0.0f : top) - 15.0f;
+        const float safe = (top == -__builtin_inff() ? 0.0f : top) - (15.0f - kSlack);
         words4 weights;
 #pragma unroll
         for (uint32_t n = 0; n < 8u; n += 2u) {
@@ -402,14 +407,15 @@ __device__ __forceinline__ uint32_t place_of_piece(uint32_t r, uint32_t j) {
     else return j ^ ((r >> 2) & 3u) ^ ((r >> 4) & 3u);
 }
 
-// Many rows: 64 * RT a workgroup, 16 * RT a wavefront, T tokens a step.  The matrix instructions and the weights' exponentials bound it, so symbols become
+// Many rows: 128 a workgroup, 16 * RT a wavefront, T tokens a step.  The matrix instructions and the weights' exponentials bound it, so symbols become
 // operands once for all four wavefronts: each thread turns some of the next step's bytes, which it asked for a step ahead, into fp16 in LDS while
 // others still multiply, keys [token][dimension], values [dimension][token] with the eight tokens that a lane feeds (4 g .. 4 g + 3 of both halves of
 // 32) side by side.  Otherwise as above.
-template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT>
-__global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
-    constexpr uint32_t kMfmas = D / 32u, kTiles = D / 16u, kVector = D * BITS / 8u, kRows = 64u * RT;
-    constexpr uint32_t kKeyDims = T * D / 256u, kValueDims = T * D / 1024u;             // a thread's: of one key; of each of four values
+template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParams p) {
+    constexpr uint32_t kThreads = WAVES * 64u;
+    constexpr uint32_t kMfmas = D / 32u, kTiles = D / 16u, kVector = D * BITS / 8u, kRows = 16u * WAVES * RT;
+    constexpr uint32_t kKeyDims = T * D / kThreads, kValueDims = T * D / (4u * kThreads);             // a thread's: of one key; of each of four values
     constexpr uint32_t kKeyBytes = kKeyDims * BITS / 8u, kValueBytes = kValueDims * BITS / 8u, kChunks = D / kValueDims;
     constexpr uint32_t kKeyPieces = D / 8u, kValuePieces = T / 8u;
     __shared__ words4 key_buffer[2][T][kKeyPieces];
@@ -430,7 +436,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
     }
 
     // staging
-    const uint32_t key_token = threadIdx.x / (256u / T), key_part = threadIdx.x % (256u / T);
+    const uint32_t key_token = threadIdx.x / (kThreads / T), key_part = threadIdx.x % (kThreads / T);
     const uint32_t quad = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
     const int32_t* const table = p.pages + uint64_t(t.seq) * p.table_width;
     const auto page_at = [&](int32_t place) __attribute__((always_inline)) { return table[place < end ? uint32_t(place) >> p.page_log : 0u]; };
@@ -560,12 +566,12 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
         }
     }
     const int32_t least_position = t.length - int32_t(t.n_new) + int32_t(min(own_row, last_row) / p.group);
-    const int32_t most_position = t.length - int32_t(t.n_new) + int32_t(min(own_row + 16u * RT - 1u, last_row) / p.group);
+    const int32_t most_position = own_row > last_row ? -1 : t.length - int32_t(t.n_new) + int32_t(min(own_row + 16u * RT - 1u, last_row) / p.group);
 
     floatx4 acc[kTiles][RT] = {};
-    float top[RT], sum[RT] = {}, reach = 0.0f, less = 0.0f;                             // (the power of two is the wavefront's)
+    float top[RT], limit[RT], sum[RT] = {}, reach = 0.0f, less = 0.0f;                  // (the power of two is the wavefront's)
 #pragma unroll
-    for (uint32_t b = 0; b < RT; ++b) top[b] = -__builtin_inff();
+    for (uint32_t b = 0; b < RT; ++b) top[b] = limit[b] = -__builtin_inff();
     const auto take = [&](int32_t step) __attribute__((always_inline)) {
         const uint32_t in = uint32_t(step) & 1u;
         {                                                                               // values larger than any before
@@ -625,7 +631,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
                 high[b] = fmaxf(fmaxf(fmaxf(y[b][0], y[b][1]), fmaxf(fmaxf(y[b][2], y[b][3]), y[b][4])), fmaxf(fmaxf(y[b][5], y[b][6]), y[b][7]));
-                grows |= high[b] > top[b];
+                grows |= high[b] > limit[b];
             }
             if (__any(grows)) {
 #pragma unroll
@@ -633,6 +639,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
                     const float now = fmaxf(top[b], most_of_query(high[b]));
                     const float kept = __builtin_amdgcn_exp2f((top[b] - (now == -__builtin_inff() ? 0.0f : now)) * to_exponent[b]);
                     top[b] = now;
+                    limit[b] = now + fminf(kSlack / to_exponent[b], 0x1p126f);
                     sum[b] *= kept;
 #pragma unroll
                     for (uint32_t e = 0; e < kTiles; ++e) acc[e][b] *= kept;
@@ -641,7 +648,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendParams p) {
             words4 weights[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
-                const float less_top = 15.0f - (top[b] == -__builtin_inff() ? 0.0f : top[b]) * to_exponent[b];
+                const float less_top = 15.0f - kSlack - (top[b] == -__builtin_inff() ? 0.0f : top[b]) * to_exponent[b];
 #pragma unroll
                 for (uint32_t n = 0; n < 8u; n += 2u) {
                     const f16x2 e = {static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n], to_exponent[b], less_top))),
@@ -773,7 +780,7 @@ struct Shares {
 Shares shares_of(const anszp_attend_args_t& a) {
     Shares s;
     const bool many = a.n_tokens * a.group > kManyRows * a.n_seqs;
-    s.rows = !many ? kTileRows : a.cache.head_dim == 256u ? 64u : 128u;
+    s.rows = many ? kManyTile : kTileRows;
     s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / s.rows + a.n_seqs);
     const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();
     uint64_t splits = 2u * cus / groups;
@@ -802,10 +809,10 @@ void launch(const AttendParams& p, uint32_t bits, hipStream_t s) {
         if (bits == 8u) hipLaunchKernelGGL((attend_rows_kernel<D, 8u>), grid, dim3(256), 0, s, p);
         else hipLaunchKernelGGL((attend_rows_kernel<D, 4u>), grid, dim3(256), 0, s, p);
     } else {
-        constexpr uint32_t T = D == 256u ? 32u : 64u, RT = D == 256u ? 1u : 2u;
+        constexpr uint32_t RT = D == 256u ? 1u : 2u, WAVES = kManyTile / (16u * RT);
         const dim3 grid(p.n_tiles * p.heads, p.splits);
-        if (bits == 8u) hipLaunchKernelGGL((attend_tile_kernel<D, 8u, T, RT>), grid, dim3(256), 0, s, p);
-        else hipLaunchKernelGGL((attend_tile_kernel<D, 4u, T, RT>), grid, dim3(256), 0, s, p);
+        if (bits == 8u) hipLaunchKernelGGL((attend_tile_kernel<D, 8u, 64u, RT, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
+        else hipLaunchKernelGGL((attend_tile_kernel<D, 4u, 64u, RT, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
     }
     if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, p.tile_rows / 4u), dim3(256), 0, s, p);
 }
