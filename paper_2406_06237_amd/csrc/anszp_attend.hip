@@ -3,8 +3,9 @@
 // One pass over the tokens with the running maximum m and sum l of each query's weights, 32 tokens a step, products in
 // v_mfma_f32_16x16x32_f16.  The rows of a tile are the queries of one head of the cache: (new token, query head of the group).
 //
-// Symbols become matrix operands in registers.  fp16 holds 1024 + q for every byte q as the bits 0x6400 | q, so symbol - z is
-// one bitwise step and one packed subtraction of 1024 + z, exact.  A key's scale multiplies its scores; a value's scale goes into the weight.
+// Symbols become matrix operands in registers, without conversions and exactly: fp16 holds 1024 + q for every byte q as the bits 0x6400 | q, so that
+// symbol - z is a byte permutation and a packed subtraction of 1024 + z; values get by with a permutation and a packed multiplication and addition
+// (value_pair).  A key's scale multiplies its scores; a value's scale goes into the weight.
 //   scores^T = K Q^T: lane (c, g), c = lane % 16, g = lane / 16, feeds a key's dimensions [g D / 4, (g + 1) D / 4), which lie one behind
 //     the other in memory, and ends up with the scores of query c for tokens 4 g .. 4 g + 3 of each half of the step;
 //   out^T = V^T P^T: those are the weights the lane has to feed for query c, so they never leave their lane.  It feeds, for the same tokens,
@@ -118,6 +119,24 @@ __device__ __forceinline__ words2 less_zero(uint32_t w, f16x2 offset) {
     const uint32_t lo = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u), hi = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
     return words2{bits_of(halves(lo) - offset), bits_of(halves(hi) - offset)};
 }
+// ... and of bytes that are 16 times the symbols: (1024 + 16 q) / 16 - (64 + z), exact
+__device__ __forceinline__ words2 less_zero_of_16(uint32_t w, f16x2 minus_64_z) {
+    const uint32_t lo = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u), hi = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
+    return words2{bits_of(__builtin_elementwise_fma(halves(lo), both(0.0625f), minus_64_z)), bits_of(__builtin_elementwise_fma(halves(hi), both(0.0625f), minus_64_z))};
+}
+// Two tokens' values of dimension e, 2^-9 of them, as fp16: the bits of a whole number q are 2^-24 q there, so that one multiplication and addition,
+// q 2^-24 2^15 - z 2^-9, is exact (its inputs may be subnormal, its result is a multiple of 2^-9 below 1).  Four bits: the high halves of bytes are 16 q.
+constexpr float kValueStep = 0x1p-9f;
+template <uint32_t BITS>
+__device__ __forceinline__ uint32_t value_pair(uint32_t first, uint32_t second, uint32_t e, f16x2 minus_zeros) {
+    if constexpr (BITS == 8u) {
+        return bits_of(__builtin_elementwise_fma(halves(__builtin_amdgcn_perm(second, first, 0x0C040C00u + (e & 3u) * 0x00010001u)), both(0x1p15f), minus_zeros));
+    } else {
+        const uint32_t bytes = __builtin_amdgcn_perm(second, first, 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
+        return bits_of(__builtin_elementwise_fma(halves(bytes & (e & 1u ? 0x00F000F0u : 0x000F000Fu)), both(e & 1u ? 0x1p11f : 0x1p15f), minus_zeros));
+    }
+}
+__device__ __forceinline__ f16x2 minus_zeros_of(float z0, float z1) { return f16x2{static_cast<_Float16>(z0 * -kValueStep), static_cast<_Float16>(z1 * -kValueStep)}; }
 
 template <uint32_t BYTES>
 struct Bytes {
@@ -255,7 +274,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
         float x[8], vs[8], vz[8];
 #pragma unroll
         for (uint32_t u = 0; u < 2u; ++u) {
-            const f16x2 offset = both(1024.0f + step.key_zero[u]);
+            const f16x2 offset = both(1024.0f + step.key_zero[u]), minus_64_z = both(-64.0f - step.key_zero[u]);
             floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (uint32_t m = 0; m < kMfmas; ++m) {
@@ -265,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
                     b = less_zero(step.keys[u].w[2u * m + 1u], offset);
                 } else {
                     a = less_zero(step.keys[u].w[m] & 0x0F0F0F0Fu, offset);
-                    b = less_zero((step.keys[u].w[m] >> 4) & 0x0F0F0F0Fu, offset);
+                    b = less_zero_of_16(step.keys[u].w[m] & 0xF0F0F0F0u, minus_64_z);
                 }
                 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, words4{a[0], a[1], b[0], b[1]}), __builtin_bit_cast(f16x8, q[m]), s, 0, 0, 0);
             }
@@ -319,21 +338,14 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
         }
         f16x2 z[4];
 #pragma unroll
-        for (uint32_t j = 0; j < 4u; ++j) z[j] = f16x2{static_cast<_Float16>(1024.0f + vz[2u * j]), static_cast<_Float16>(1024.0f + vz[2u * j + 1u])};
+        for (uint32_t j = 0; j < 4u; ++j) z[j] = minus_zeros_of(vz[2u * j], vz[2u * j + 1u]);
 #pragma unroll
         for (uint32_t e = 0; e < kTiles; ++e) {
             words4 a;
 #pragma unroll
             for (uint32_t j = 0; j < 4u; ++j) {
                 const Bytes<kValueBytes>&one = step.values[j >> 1][2u * (j & 1u)], &two = step.values[j >> 1][2u * (j & 1u) + 1u];
-                uint32_t pair;
-                if constexpr (BITS == 8u) {
-                    pair = __builtin_amdgcn_perm(two.w[e >> 2], one.w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
-                } else {
-                    pair = __builtin_amdgcn_perm(two.w[e >> 3], one.w[e >> 3], 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
-                    pair = (e & 1u ? pair >> 4 : pair) & 0x000F000Fu;
-                }
-                a[j] = bits_of(halves(pair | 0x64006400u) - z[j]);
+                a[j] = value_pair<BITS>(one.w[BITS == 8u ? e >> 2 : e >> 3], two.w[BITS == 8u ? e >> 2 : e >> 3], e, z[j]);
             }
             acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, weights), acc[e], 0, 0, 0);
         }
@@ -364,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
 
     // the wavefronts' results together
     for (uint32_t e = 0; e < kTiles; ++e)
-        for (uint32_t i = 0; i < 4u; ++i) joined[wave][c][(g * 4u + i) * kTiles + e] = acc[e][i] * reach;
+        for (uint32_t i = 0; i < 4u; ++i) joined[wave][c][(g * 4u + i) * kTiles + e] = acc[e][i] * (1.0f / kValueStep) * reach;
     if (g == 0u) {
         stats[wave][c][0] = top;
         stats[wave][c][1] = sum;
@@ -473,7 +485,8 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     };
     const auto put = [&](int32_t step) __attribute__((always_inline)) {
         const uint32_t to = uint32_t(step) & 1u;
-        const f16x2 offset = both(1024.0f + (key_there ? key_pair.y : 0.0f));
+        const float key_zero = key_there ? key_pair.y : 0.0f;
+        const f16x2 offset = both(1024.0f + key_zero), minus_64_z = both(-64.0f - key_zero);
 #pragma unroll
         for (uint32_t j = 0; j < kKeyDims / 8u; ++j) {
             words2 a, b;
@@ -482,7 +495,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                 b = less_zero(key_bytes.w[2u * j + 1u], offset);
             } else {
                 a = less_zero(key_bytes.w[j] & 0x0F0F0F0Fu, offset);
-                b = less_zero((key_bytes.w[j] >> 4) & 0x0F0F0F0Fu, offset);
+                b = less_zero_of_16(key_bytes.w[j] & 0xF0F0F0F0u, minus_64_z);
             }
             key_buffer[to][key_token][place_of_piece<kKeyPieces>(key_token, key_part * (kKeyDims / 8u) + j)] = words4{a[0], a[1], b[0], b[1]};
         }
@@ -505,24 +518,15 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                 vz[i] = value_there && begin + step * int32_t(T) + int32_t(quad * 4u + i) < end ? vz[i] : 0.0f;
             }
         }
-        const f16x2 z0 = {static_cast<_Float16>(1024.0f + vz[0]), static_cast<_Float16>(1024.0f + vz[1])};
-        const f16x2 z1 = {static_cast<_Float16>(1024.0f + vz[2]), static_cast<_Float16>(1024.0f + vz[3])};
+        const f16x2 z0 = minus_zeros_of(vz[0], vz[1]), z1 = minus_zeros_of(vz[2], vz[3]);
         // the quad's place among the 32 tokens of its group: half (quad / 4) % 2 of piece quad % 4
         const uint32_t piece = quad / 8u * 4u + (quad & 3u), half = (quad >> 2) & 1u;
 #pragma unroll
         for (uint32_t e = 0; e < kValueDims; ++e) {
-            uint32_t lo, hi;
-            if constexpr (BITS == 8u) {
-                lo = __builtin_amdgcn_perm(value_bytes[1].w[e >> 2], value_bytes[0].w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
-                hi = __builtin_amdgcn_perm(value_bytes[3].w[e >> 2], value_bytes[2].w[e >> 2], 0x0C040C00u + (e & 3u) * 0x00010001u);
-            } else {
-                lo = __builtin_amdgcn_perm(value_bytes[1].w[e >> 3], value_bytes[0].w[e >> 3], 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
-                hi = __builtin_amdgcn_perm(value_bytes[3].w[e >> 3], value_bytes[2].w[e >> 3], 0x0C040C00u + ((e & 7u) >> 1) * 0x00010001u);
-                lo = (e & 1u ? lo >> 4 : lo) & 0x000F000Fu;
-                hi = (e & 1u ? hi >> 4 : hi) & 0x000F000Fu;
-            }
+            const uint32_t w = BITS == 8u ? e >> 2 : e >> 3;
             const uint32_t dim = chunk * kValueDims + e;
-            value_buffer[to][dim][2u * place_of_piece<kValuePieces>(dim, piece) + half] = words2{bits_of(halves(lo | 0x64006400u) - z0), bits_of(halves(hi | 0x64006400u) - z1)};
+            value_buffer[to][dim][2u * place_of_piece<kValuePieces>(dim, piece) + half] =
+                words2{value_pair<BITS>(value_bytes[0].w[w], value_bytes[1].w[w], e, z0), value_pair<BITS>(value_bytes[2].w[w], value_bytes[3].w[w], e, z1)};
         }
         if (key_part == 0u && (key_token & 15u) == 0u) {
             known[to][key_token / 16u] = key_there ? 1u : 0u;
@@ -568,8 +572,9 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     const int32_t least_position = t.length - int32_t(t.n_new) + int32_t(min(own_row, last_row) / p.group);
     const int32_t most_position = own_row > last_row ? -1 : t.length - int32_t(t.n_new) + int32_t(min(own_row + 16u * RT - 1u, last_row) / p.group);
 
-    floatx4 acc[kTiles][RT] = {};
-    float top[RT], limit[RT], sum[RT] = {}, reach = 0.0f, less = 0.0f;                  // (the power of two is the wavefront's)
+    floatx4 acc[kTiles][RT] = {}, sum[RT] = {};                                        // (sums: products with ones, alike in all four)
+    const uint32_t one = 0x3C003C00u;
+    float top[RT], limit[RT], reach = 0.0f, less = 0.0f;                  // (the power of two is the wavefront's)
 #pragma unroll
     for (uint32_t b = 0; b < RT; ++b) top[b] = limit[b] = -__builtin_inff();
     const auto take = [&](int32_t step) __attribute__((always_inline)) {
@@ -630,7 +635,9 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
             float high[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
-                high[b] = fmaxf(fmaxf(fmaxf(y[b][0], y[b][1]), fmaxf(fmaxf(y[b][2], y[b][3]), y[b][4])), fmaxf(fmaxf(y[b][5], y[b][6]), y[b][7]));
+                high[b] = fmaxf(y[b][0], y[b][1]);
+#pragma unroll
+                for (uint32_t n = 2; n < 8u; n += 2u) high[b] = fmaxf(fmaxf(high[b], y[b][n]), y[b][n + 1u]);
                 grows |= high[b] > limit[b];
             }
             if (__any(grows)) {
@@ -648,14 +655,16 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
             words4 weights[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
+                words4 plain;
                 const float less_top = 15.0f - kSlack - (top[b] == -__builtin_inff() ? 0.0f : top[b]) * to_exponent[b];
 #pragma unroll
                 for (uint32_t n = 0; n < 8u; n += 2u) {
                     const f16x2 e = {static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n], to_exponent[b], less_top))),
                                      static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n + 1u], to_exponent[b], less_top)))};
-                    sum[b] = __builtin_amdgcn_fdot2(e, f16x2{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)}, sum[b], false);
+                    plain[n / 2u] = bits_of(e);
                     weights[b][n / 2u] = bits_of(e * ratio[n / 2u]);
                 }
+                sum[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, words4{one, one, one, one}), __builtin_bit_cast(f16x8, plain), sum[b], 0, 0, 0);
             }
 #pragma unroll
             for (uint32_t e = 0; e < kTiles; ++e) {
@@ -687,15 +696,14 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     if (missing) flag(p);
 #pragma unroll
     for (uint32_t b = 0; b < RT; ++b) {
-        sum[b] += __shfl_xor(sum[b], 16);
-        sum[b] += __shfl_xor(sum[b], 32);
+        const float l = sum[b][0];
         const uint32_t r = wave * (16u * RT) + 16u * b + c;
         if (r >= t.n_rows) continue;
-        const float over = p.splits > 1u ? reach : sum[b] == 0.0f ? 0.0f : reach / sum[b];
-        if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b] * to_exponent[b], sum[b]);
+        const float over = p.splits > 1u ? reach : l == 0.0f ? 0.0f : reach / l;
+        if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b] * to_exponent[b], l);
 #pragma unroll
         for (uint32_t e = 0; e < kTiles; ++e) {
-            const floatx4 o = acc[e][b] * over;
+            const floatx4 o = acc[e][b] * (1.0f / kValueStep) * over;
             const uint32_t d = 16u * e + 4u * g;
             if (p.splits > 1u)
                 *reinterpret_cast<floatx4*>(p.parts + (part * kRows + r) * D + d) = o;
