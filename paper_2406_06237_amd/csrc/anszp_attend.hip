@@ -413,10 +413,23 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
 // 16 x n matrix of fp16 whose rows are PIECES pieces of 16 bytes: where piece j of row r lies, so that 16 lanes that read a piece of 16 consecutive
 // rows meet all 64 banks (and the 16 that write 8 rows apart few of them twice).
 template <uint32_t PIECES>
-__device__ __forceinline__ uint32_t place_of_piece(uint32_t r, uint32_t j) {
+__host__ __device__ constexpr uint32_t place_of_piece(uint32_t r, uint32_t j) {
     if constexpr (PIECES >= 16u) return j ^ (r & 15u);
     else if constexpr (PIECES == 8u) return j ^ ((r >> 1) & 7u) ^ ((r >> 4) & 7u);
     else return j ^ ((r >> 2) & 3u) ^ ((r >> 4) & 3u);
+}
+
+// The order in which a run of COUNT loads from LDS, each for EACH matrix instructions, is issued: four loads ahead, where the compiler would have two and
+// wait for every one of them.
+template <uint32_t COUNT, uint32_t EACH, int RUN>
+__device__ __forceinline__ void loads_ahead() {
+    constexpr int kMatrix = 0x8, kFromLds = 0x100;
+    __builtin_amdgcn_sched_group_barrier(kFromLds, 4, RUN);
+#pragma unroll
+    for (uint32_t n = 0; n < COUNT; ++n) {
+        __builtin_amdgcn_sched_group_barrier(kMatrix, EACH, RUN);
+        if (n + 4u < COUNT) __builtin_amdgcn_sched_group_barrier(kFromLds, 1, RUN);
+    }
 }
 
 // Many rows: 128 a workgroup, 16 * RT a wavefront, T tokens a step.  The matrix instructions and the weights' exponentials bound it, so symbols become
@@ -577,8 +590,12 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     float top[RT], limit[RT], reach = 0.0f, less = 0.0f;                  // (the power of two is the wavefront's)
 #pragma unroll
     for (uint32_t b = 0; b < RT; ++b) top[b] = limit[b] = -__builtin_inff();
+    // Places are exclusive ors of what r and j give, so that the lane's own part, of row c and piece g, and the rest of a row and piece make up any of them: one
+    // register for all addresses, and registers are what loads from LDS can be under way in.
+    const uint32_t key_own = 16u * (c * kKeyPieces + place_of_piece<kKeyPieces>(c, g)), value_own = 16u * (c * kValuePieces + place_of_piece<kValuePieces>(c, g));
     const auto take = [&](int32_t step) __attribute__((always_inline)) {
         const uint32_t in = uint32_t(step) & 1u;
+        const uint32_t key_at = key_own + in * uint32_t(sizeof key_buffer[0]), value_at = value_own + in * uint32_t(sizeof value_buffer[0]);
         {                                                                               // values larger than any before
             const float far = fabsf(value_scales[in][lane % T]);
             if (__any(far > reach)) {
@@ -603,11 +620,12 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
             f16x2 ratio[4];
 #pragma unroll
             for (uint32_t u = 0; u < 2u; ++u) {
-                const uint32_t row = 32u * h + 16u * u + c;
+                const uint32_t row = 32u * h + 16u * u;
                 floatx4 s[RT] = {};
 #pragma unroll
                 for (uint32_t m = 0; m < kMfmas; ++m) {
-                    const words4 a = key_buffer[in][row][place_of_piece<kKeyPieces>(row, m * 4u + g)];
+                    const uint32_t at = (key_at ^ 16u * place_of_piece<kKeyPieces>(row, m * 4u)) + 16u * row * kKeyPieces;
+                    const words4 a = *reinterpret_cast<const words4*>(reinterpret_cast<const uint8_t*>(key_buffer) + at);
 #pragma unroll
                     for (uint32_t b = 0; b < RT; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, q[b][m]), s[b], 0, 0, 0);
                 }
@@ -620,6 +638,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
 #pragma unroll
                     for (uint32_t i = 0; i < 4u; ++i) y[b][4u * u + i] = s[b][i] * ks[i];
             }
+            loads_ahead<2u * kMfmas, RT, 1>();
             const bool whole = !lacking && t0 + 31 <= least_position && t0 + 32 <= end;
             if (!whole) {
 #pragma unroll
@@ -668,11 +687,12 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
             }
 #pragma unroll
             for (uint32_t e = 0; e < kTiles; ++e) {
-                const uint32_t dim = 16u * e + c;
-                const words4 a = *reinterpret_cast<const words4*>(&value_buffer[in][dim][2u * place_of_piece<kValuePieces>(dim, 4u * h + g)]);
+                const uint32_t at = (value_at ^ 16u * place_of_piece<kValuePieces>(16u * e, 4u * h)) + 256u * e * kValuePieces;
+                const words4 a = *reinterpret_cast<const words4*>(reinterpret_cast<const uint8_t*>(value_buffer) + at);
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b) acc[e][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, weights[b]), acc[e][b], 0, 0, 0);
             }
+            if constexpr (kTiles > 4u) loads_ahead<kTiles, RT, 0>();                    // (of four tiles all loads would be ahead: 84 us rather than 79)
         }
     };
     const int32_t steps = (max(0, end - begin) + int32_t(T) - 1) / int32_t(T);
