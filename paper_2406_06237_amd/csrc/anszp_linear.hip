@@ -99,8 +99,8 @@ struct Some {
 };
 
 // The epilogue of N consecutive channels: what belongs to the channels, what belongs to a row of them, and a row's sums to the output.  A row's
-// operands are asked for apart from their use, so that those of two rows are under way together (out may be one of them, which keeps
-// the compiler from moving a load before a store): with it 3001 x 4096 x 4096 took 111.5 us rather than 115.9, 8192 x 11008 x 4096 539 rather than 558.
+// operands are asked for apart from their use, so that those of several rows are under way together (out may be one of them, which
+// keeps the compiler from moving a load before a store).
 template <uint32_t N>
 struct Channels {
     Some<N> scale, bias;
@@ -113,9 +113,18 @@ struct Channels {
         if (p.bias) bias.load(p.bias, ANSZP_OUT_F32, col, there);
     }
 };
+// The operands of a row, in the output's type: one that is known here (eight elements of it), or else p.out_dtype.
+constexpr uint32_t kAnyType = ~0u;
+template <uint32_t N, uint32_t DTYPE>
+struct Operand : Eight<DTYPE> {
+    static_assert(N == 8u, "");
+    __device__ __forceinline__ float at(uint32_t, uint32_t i) const { return (*this)[i]; }
+};
 template <uint32_t N>
+struct Operand<N, kAnyType> : Some<N> {};
+template <uint32_t N, uint32_t DTYPE = kAnyType>
 struct RowOperands {
-    Some<N> mul, residual;
+    Operand<N, DTYPE> mul, residual;
     float by;
     __device__ __forceinline__ void load(const LinearParams& p, const Channels<N>& c, uint64_t row) {
         if (row >= p.rows || c.there == 0u) return;
@@ -124,8 +133,9 @@ struct RowOperands {
         if (p.residual) residual.load(p.residual, p.out_dtype, row * p.residual_stride + c.col, c.there);
     }
 };
-template <uint32_t N>
-__device__ __forceinline__ void finish(const LinearParams& p, const Channels<N>& c, const RowOperands<N>& o, uint64_t row, const float (&sum)[N]) {
+template <uint32_t N, uint32_t DTYPE>
+__device__ __forceinline__ void finish(const LinearParams& p, const Channels<N>& c, const RowOperands<N, DTYPE>& o, uint64_t row, const float (&sum)[N]) {
+    const uint32_t dtype = DTYPE == kAnyType ? p.out_dtype : DTYPE;
     if (row >= p.rows || c.there == 0u) return;
     float v[N];
 #pragma unroll
@@ -144,14 +154,14 @@ __device__ __forceinline__ void finish(const LinearParams& p, const Channels<N>&
     }
     if (p.mul) {
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) v[i] *= o.mul.at(p.out_dtype, i);
+        for (uint32_t i = 0; i < N; ++i) v[i] *= o.mul.at(dtype, i);
     }
     if (p.residual) {
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) v[i] += o.residual.at(p.out_dtype, i);
+        for (uint32_t i = 0; i < N; ++i) v[i] += o.residual.at(dtype, i);
     }
     const uint64_t to = row * p.out_stride + c.col;
-    if (p.out_dtype == ANSZP_OUT_BF16) {
+    if (dtype == ANSZP_OUT_BF16) {
         uint16_t* out = static_cast<uint16_t*>(p.out) + to;
         if (c.there >= N) {
             if constexpr (N == 8u)
@@ -182,7 +192,7 @@ __device__ __forceinline__ void finish(const LinearParams& p, uint64_t row, uint
     RowOperands<N> o;
     c.load(p, col);
     o.load(p, c, row);
-    finish<N>(p, c, o, row, sum);
+    finish<N, kAnyType>(p, c, o, row, sum);
 }
 
 // 16 bytes of a row from byte `at` on, zeros behind its end.
@@ -577,10 +587,37 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
                 }
             } else {
                 const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                finish<8u>(p, channels, operands, row, sum);
+                finish<8u, kAnyType>(p, channels, operands, row, sum);
             }
         };
         static_assert(kTurns % 2u == 0u, "two turns' operands at once");
+        if (!p.parts && p.out_dtype == ANSZP_OUT_BF16 && c0 + (wc + 1u) * kWidth <= p.cols) {
+            // What 32 rows need of memory is asked for together, under no condition of a lane's own (rows that do not exist are the last one again), before any
+            // is finished: 8192 x 11008 x 4096 of bytes with mul took 536 us with two rows under way, 466 with 32; 3001 x 4096 x 4096 with a residual 110 and 103.
+            RowOperands<8u, ANSZP_OUT_BF16> operands[kTurns];
+            Channels<8u> all = channels;
+            all.there = 8u;
+            const auto existing = [&](uint32_t turn) __attribute__((always_inline)) { return least(first + b * 32u + row_of(turn), p.rows - 1u); };
+            if (p.mul) {
+#pragma unroll
+                for (uint32_t turn = 0; turn < kTurns; ++turn) operands[turn].mul.load(p.mul, existing(turn) * p.mul_stride + all.col, 8u);
+            }
+            if (p.residual) {
+#pragma unroll
+                for (uint32_t turn = 0; turn < kTurns; ++turn) operands[turn].residual.load(p.residual, existing(turn) * p.residual_stride + all.col, 8u);
+            }
+#pragma unroll
+            for (uint32_t turn = 0; turn < kTurns; ++turn) operands[turn].by = p.x_scales ? p.scale * p.x_scales[existing(turn)] : p.scale;
+#pragma unroll
+            for (uint32_t turn = 0; turn < kTurns; ++turn) {
+                const uint32_t n = row_of(turn);
+                const floatx4 lo = part[n][(2u * own) ^ (n & 7u)], hi = part[n][(2u * own + 1u) ^ (n & 7u)];
+                const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                finish<8u, ANSZP_OUT_BF16>(p, all, operands[turn], first + b * 32u + n, sum);
+            }
+            __builtin_amdgcn_wave_barrier();
+            continue;
+        }
         for (uint32_t turn = 0; turn < kTurns; turn += 2u) {
             RowOperands<8u> one, two;
             if (!p.parts) {
