@@ -176,7 +176,9 @@ __device__ __forceinline__ float power_above(float v) {
 // Few rows: 16 a workgroup, whose four wavefronts take 32 tokens each in turn.  Memory is what bounds it where it can: what a step reads
 // is asked for a step ahead (two steps' worth of registers; heads of 256 leave no room for that).
 // The running maximum and the values' power of two are looked up together in one vote; queries that meet a larger one rescale, the rest of the steps
-// exchange nothing between lanes.
+// exchange nothing between lanes.  One sequence of 65000 tokens in 8 bits, 32 heads over 8, takes 27 us here, 5.2 TB/s; 48 sequences of 17 to 4100
+// tokens in 4 bits, 32 heads, 126, 3.6 TB/s: with half the bytes the instructions that make operands of them, 50 % of the vector unit's time, and what a
+// workgroup does before and after its 1024 tokens show.
 template <uint32_t D, uint32_t BITS>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     constexpr uint32_t kKeyBytes = D * BITS / 32u, kValueBytes = D * BITS / 128u;      // of a key, of a value, that a lane feeds
@@ -432,10 +434,14 @@ __device__ __forceinline__ void loads_ahead() {
     }
 }
 
-// Many rows: 128 a workgroup, 16 * RT a wavefront, T tokens a step.  The matrix instructions and the weights' exponentials bound it, so symbols become
-// operands once for all four wavefronts: each thread turns some of the next step's bytes, which it asked for a step ahead, into fp16 in LDS while
+// Many rows: 128 a workgroup, 16 * RT a wavefront, T tokens a step.  Scores and weights, more than the matrix instructions, bound it, so symbols become
+// operands once for all wavefronts: each thread turns some of the next step's bytes, which it asked for a step ahead, into fp16 in LDS while
 // others still multiply, keys [token][dimension], values [dimension][token] with the eight tokens that a lane feeds (4 g .. 4 g + 3 of both halves of
-// 32) side by side.  Otherwise as above.
+// 32) side by side.  Otherwise as above.  Heads of 64 and 128 have four wavefronts of 32 rows, two such workgroups a CU; eight wavefronts of 32 halve
+// what a row costs in staging, but all of a CU's wait for one barrier (16 sequences of 2048 tokens: 615 TFLOP/s rather than 693).  Heads of 256 leave room
+// for 16 rows a wavefront and need the eight: two chunks of 700 tokens 84 us rather than 97.
+// Sixteen sequences of 2048 new tokens behind up to 2048 more, 32 heads over 8 of 128, take 1690 us, 800 TFLOP/s (a large product 1330 to 1530): the
+// vector unit is at work for 52 % of the time, the matrix units for 26.
 template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParams p) {
     constexpr uint32_t kThreads = WAVES * 64u;
@@ -735,7 +741,8 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     }
 }
 
-// The splits' results together: four workgroups per tile and head, a row of it at a time; D / 4 lanes have a split, their sums meet in LDS.
+// The splits' results together: four workgroups per tile and head, a row of it at a time; D / 4 lanes have a split, their sums meet in LDS.  32 rows of 64
+// splits each take 5 us, most of it a launch.
 template <uint32_t D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     constexpr uint32_t kLanes = D / 4u, kGroups = 256u / kLanes;
@@ -796,8 +803,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
     }
 }
 
-// Above so many rows per sequence and head of the cache, on average, attend_tile_kernel is the faster one.
-constexpr uint64_t kManyRows = 32u;
+// Above so many rows per sequence and head of the cache, on average, attend_tile_kernel is the faster one: it reads tokens once for 128 rows, not 16, but
+// vectors of few bytes are no work for attend_rows_kernel.  16 sequences of 2000 to 4000 tokens, 8 heads, few rows' kernel and many rows', us:
+//   128 x 8 bits: 16 rows 42 and 57, 32 rows 59 and 61, 48 rows 70 and 64, 128 rows 138 and 96
+//   256 x 8 bits: 16 rows 62 and 84, 32 rows 88 and 88, 48 rows 110 and 92
+//   64 x 8 bits:  32 rows 38 and 50, 64 rows 52 and 66, 128 rows 83 and 79
+//   128 x 4 bits: 32 rows 44 and 60, 64 rows 64 and 80, 128 rows 104 and 94
+uint64_t few_rows_of(const anszp_cache_t& c) { return c.head_dim * c.bits / 8u <= 64u ? 96u : 32u; }
 
 // How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of
 // about 1024 tokens, since sequences differ in length and the longest would end last (48 sequences of 17 to 4100 tokens, 32 heads
@@ -807,7 +819,7 @@ struct Shares {
 };
 Shares shares_of(const anszp_attend_args_t& a) {
     Shares s;
-    const bool many = a.n_tokens * a.group > kManyRows * a.n_seqs;
+    const bool many = a.n_tokens * a.group > few_rows_of(a.cache) * a.n_seqs;
     s.rows = many ? kManyTile : kTileRows;
     s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / s.rows + a.n_seqs);
     const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();

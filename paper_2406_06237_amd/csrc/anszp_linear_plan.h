@@ -6,7 +6,7 @@
 //                  after the other: 16 x 4096 x 11008 in bf16 22 us;
 //   tiles          a step of 128 bytes of k takes at least `alone`, and `each` for every workgroup a CU has at a time (bf16, 8 bits): small tiles fill
 //                  the chip with few rows, large ones read less from LDS and L2 for a product (8192 x 4096 x 4096 in bf16: 64 x 64 438 us, 128 x 128 277,
-//                  256 x 256 231; 1024 x 4096 x 4096: 50, 53, 87);
+//                  256 x 256 219; 1024 x 4096 x 4096: 50, 53, 87);
 //   shares of k    cost the join's launch and the partial sums' way to memory and back, where tiles alone leave CUs without work (64 x 4096 x 11008 in bf16
 //                  42 us with the best kernel that has no shares, 29 with eight);
 //   memory         gives 4.6 bytes a ps.
