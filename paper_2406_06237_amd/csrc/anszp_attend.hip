@@ -177,8 +177,8 @@ __device__ __forceinline__ float power_above(float v) {
 // is asked for a step ahead (two steps' worth of registers; heads of 256 leave no room for that).
 // The running maximum and the values' power of two are looked up together in one vote; queries that meet a larger one rescale, the rest of the steps
 // exchange nothing between lanes.  One sequence of 65000 tokens in 8 bits, 32 heads over 8, takes 27 us here, 5.2 TB/s; 48 sequences of 17 to 4100
-// tokens in 4 bits, 32 heads, 126, 3.6 TB/s: with half the bytes the instructions that make operands of them, 50 % of the vector unit's time, and what a
-// workgroup does before and after its 1024 tokens show.
+// tokens in 4 bits, 32 heads, 113, 4.0 TB/s: with half the bytes the instructions that make operands of them, 50 % of the vector unit's time, and what a
+// workgroup does before and after its tokens show.
 template <uint32_t D, uint32_t BITS>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     constexpr uint32_t kKeyBytes = D * BITS / 32u, kValueBytes = D * BITS / 128u;      // of a key, of a value, that a lane feeds
@@ -741,7 +741,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     }
 }
 
-// The splits' results together: four workgroups per tile and head, a row of it at a time; D / 4 lanes have a split, their sums meet in LDS.  32 rows of 64
+// The splits' results together: a workgroup for every fourth row of a tile and head, if it has as many, a row at a time; D / 4 lanes have a split, their sums meet in LDS.  32 rows of 64
 // splits each take 5 us, most of it a launch.
 template <uint32_t D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
@@ -811,9 +811,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
 //   128 x 4 bits: 32 rows 44 and 60, 64 rows 64 and 80, 128 rows 104 and 94
 uint64_t few_rows_of(const anszp_cache_t& c) { return c.head_dim * c.bits / 8u <= 64u ? 96u : 32u; }
 
-// How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of
-// about 1024 tokens, since sequences differ in length and the longest would end last (48 sequences of 17 to 4100 tokens, 32 heads
-// in 4 bits: 184 us with a workgroup for each, 135 with shares).  The lengths are on the device: what the page tables can hold counts.
+// How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of a
+// length, since sequences differ in theirs and the longest would end last.  A share costs its workgroup's start and its part of the join, so many workgroups
+// have longer ones (us, with a share for 1408 and for 2816 tokens):
+//   48 sequences of 17 to 4100 tokens, 32 heads in 4 bits 131 and 127 (184 with one workgroup for all of a sequence's tokens), in 8 bits 184 and 181;
+//   200 of 10 to 2000, 8 heads in 4 bits 85 and 74;    64 of 100 to 4000, 8 heads of four queries in 8 bits 81 and 87;    16, 32 heads in 4 bits 51 and 54.
+// The lengths are on the device: what the page tables can hold counts.
 struct Shares {
     uint32_t rows, tiles, splits, span;     // rows of a tile: attend_rows_kernel's, or attend_tile_kernel's
 };
@@ -824,7 +827,8 @@ Shares shares_of(const anszp_attend_args_t& a) {
     s.tiles = static_cast<uint32_t>(a.n_tokens * a.group / s.rows + a.n_seqs);
     const uint64_t most = uint64_t(a.table_width) * a.cache.page_size, groups = std::max<uint64_t>(1u, uint64_t(s.tiles) * a.cache.heads), cus = device_cus();
     uint64_t splits = 2u * cus / groups;
-    if (!many) splits = std::max(splits, std::min<uint64_t>(32u * cus / groups, (most + 1023u) / 1024u));
+    const uint64_t share = groups < 4u * cus ? 1408u : 2816u;
+    if (!many) splits = std::max(splits, std::min<uint64_t>(32u * cus / groups, (most + share - 1u) / share));
     splits = std::max<uint64_t>(1u, std::min<uint64_t>(std::min<uint64_t>(splits, (most + 255u) / 256u), kMostSplits));
     const uint64_t whole = 2u * kStep * kAttendWaves;                                   // (the few rows' wavefronts take two turns a round)
     s.span = static_cast<uint32_t>((most + splits * whole - 1u) / (splits * whole) * whole);
@@ -854,7 +858,10 @@ void launch(const AttendParams& p, uint32_t bits, hipStream_t s) {
         if (bits == 8u) hipLaunchKernelGGL((attend_tile_kernel<D, 8u, 64u, RT, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
         else hipLaunchKernelGGL((attend_tile_kernel<D, 4u, 64u, RT, WAVES>), grid, dim3(WAVES * 64u), 0, s, p);
     }
-    if (p.splits > 1u) hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, p.tile_rows / 4u), dim3(256), 0, s, p);
+    if (p.splits > 1u) {
+        const uint64_t rows = (uint64_t(p.n_tokens) * p.group + p.n_seqs - 1u) / p.n_seqs;         // of a sequence and head
+        hipLaunchKernelGGL(attend_join_kernel<D>, dim3(p.n_tiles, p.heads, static_cast<uint32_t>(std::min<uint64_t>(p.tile_rows / 4u, rows))), dim3(256), 0, s, p);
+    }
 }
 
 }  // namespace
