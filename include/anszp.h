@@ -438,7 +438,7 @@ int anszp_rms_norm(const anszp_norm_args_t* args, void* hip_stream);
 /* activations of anszp_linear */
 #define ANSZP_FN_NONE        0
 #define ANSZP_FN_RELU        1
-#define ANSZP_FN_GELU        2     /* v / 2 * (1 + erf(v / sqrt 2))                                    */
+#define ANSZP_FN_GELU        2     /* v / 2 * (1 + erf(v / sqrt 2)), erf to 1.5e-7                     */
 #define ANSZP_FN_SILU        3     /* v / (1 + exp(-v))                                                */
 
 /* Matrix product with its epilogue: out = act(scale * x_scales[r] * channel_scales[c] * sum_k x[r, k] w[c, k] + bias[c]) * mul[r, c]
@@ -504,7 +504,7 @@ int anszp_cache_read(const anszp_cache_t* cache, void* k, void* v, uint32_t dtyp
  *   out = sum_t softmax_t(scale * q . k_t) v_t        a query that sees nothing (a position below 0): zeros
  * Query head h reads the cache's head h / group.  Position t of sequence s is in page pages[s * table_width + t / page_size].
  * Sums and statistics in fp32; queries go into the matrix instructions in fp16 scaled by a power of two per row, keys and values
- * exactly, weights in fp16 scaled to 2^15. */
+ * exactly, weights in fp16 with a scale that keeps 11 bits of each down to 2^-23 of the largest. */
 typedef struct {
     anszp_cache_t  cache;
     const void*    q;             /* [device] n_tokens x (heads * group) x head_dim, bf16            */
