@@ -210,3 +210,22 @@ def test_a_captured_step_and_other_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(static, B.attend(q, cache, table, lengths, starts)), i
+
+
+@pytest.mark.parametrize("rise", [-6.0, 0.5, 3.0, 5.9, 6.1, 40.0])
+@pytest.mark.parametrize("dim,bits", [(64, 8), (128, 8), (128, 4), (256, 8)])
+def test_a_maximum_that_rises(dim, bits, rise):
+    """Scores that rise (or fall) from step to step of 32 tokens, by less and by more than what moves the running maximum, in both kernels."""
+    for lengths, news in (([500, 70, 33], [1, 1, 1]), ([500, 333], [150, 160])):
+        case = _case(lengths, news, 1, 2, dim, 32, bits)
+        cache, q, table = case[:3]
+        q[:] = 1.0
+        g = torch.Generator(device=DEV).manual_seed(4)
+        high = 210 if bits == 8 else 0xFF
+        cache.k.copy_(torch.randint(200 if bits == 8 else 0xDD, high + 1, cache.k.shape, device=DEV, generator=g))
+        cache.k_params[..., 1] = 0
+        mean = 205.0 if bits == 8 else 14.0
+        for s, n in enumerate(lengths):
+            at = torch.arange(n, device=DEV)
+            cache.k_params[table[s, at // 32].long(), 0, at % 32, 0] = 0.6931 * rise * (at / 32.0 + 1.0) / (mean * dim)
+        _check(case, "f32", scale=1.0, what=(lengths, rise))
