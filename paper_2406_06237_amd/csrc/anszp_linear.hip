@@ -419,12 +419,12 @@ __device__ __forceinline__ void place_tile(uint32_t block, uint32_t tiles_t, uin
     tile_t = panel * kPanel + in % high;
 }
 
-template <bool BYTES, bool DIRECT, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC>
+template <bool BYTES, bool DIRECT, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC, uint32_t STAGES>
 __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams p, uint32_t tiles_c, uint32_t tiles_t) {
     constexpr uint32_t kThreads = WT * WC * 64u, kRows = TOK + CH, kFT = TOK / WT / 32u, kFC = CH / WC / 32u;
     constexpr uint32_t kStepBytes = 128u, kLoads = kRows * 8u / kThreads, kHalf = kLoads / 2u;      // pieces a thread brings per step
     static_assert(kRows * 8u % kThreads == 0u && TOK * 8u % kThreads == 0u, "a load is of one operand");
-    __shared__ words4 buffer[2][kRows][8];                            // activations, then weights
+    __shared__ words4 buffer[STAGES][kRows][8];                            // activations, then weights
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wt = wave / WC, wc = wave % WC;
     uint32_t tile_t, tile_c;
@@ -461,13 +461,13 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
     const auto put = [&](uint32_t s) __attribute__((always_inline)) {
         if (s >= steps) return;
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) buffer[s & 1u][(i * kThreads + threadIdx.x) >> 3][threadIdx.x & 7u] = held[i];
+        for (uint32_t i = 0; i < kLoads; ++i) buffer[s & (STAGES - 1u)][(i * kThreads + threadIdx.x) >> 3][threadIdx.x & 7u] = held[i];
     };
     const auto bring = [&](uint32_t s, uint32_t begin, uint32_t end) __attribute__((always_inline)) {      // loads of a whole step
 #pragma unroll
         for (uint32_t i = begin; i < end; ++i)
             __builtin_amdgcn_global_load_lds((global_void*)(operand(i) + (s - rest) * kStepBytes + (from[i] + piece)),
-                                             (lds_void*)(&buffer[s & 1u][(i * kThreads + wave * 64u) >> 3][0]), 16, 0, 0);
+                                             (lds_void*)(&buffer[s & (STAGES - 1u)][(i * kThreads + wave * 64u) >> 3][0]), 16, 0, 0);
     };
     // The step behind is there for all wavefronts, and what they read before has been read.  No barrier waits by itself for loads that go to LDS.
     const auto arrived = [&]() __attribute__((always_inline)) {
@@ -481,9 +481,9 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
     const auto fetch = [&](uint32_t slot, uint32_t s, uint32_t kk) __attribute__((always_inline)) {
         const uint32_t j = (kk * 2u + (lane >> 5)) ^ ((r >> 1) & 7u);
 #pragma unroll
-        for (uint32_t f = 0; f < kFC; ++f) w[slot][f] = buffer[s & 1u][TOK + wc * (CH / WC) + f * 32u + r][j];
+        for (uint32_t f = 0; f < kFC; ++f) w[slot][f] = buffer[s & (STAGES - 1u)][TOK + wc * (CH / WC) + f * 32u + r][j];
 #pragma unroll
-        for (uint32_t f = 0; f < kFT; ++f) x[slot][f] = buffer[s & 1u][wt * (TOK / WT) + f * 32u + r][j];
+        for (uint32_t f = 0; f < kFT; ++f) x[slot][f] = buffer[s & (STAGES - 1u)][wt * (TOK / WT) + f * 32u + r][j];
     };
     // A quarter of a step; between(a) comes behind the instructions of the a-th rows of channels.
     const auto multiply = [&](uint32_t slot, auto between) __attribute__((always_inline)) {
@@ -510,9 +510,15 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
     // The operands of the next quarter of a step are on their way to registers while this one's are multiplied.  Before a step's last quarter is
     // multiplied every wavefront has all it needs of the step's buffer: from there on it takes the step after the next.  Its loads are spread
     // over that quarter and the next one (asked for in one go they keep the wavefront from multiplying), which leaves them half a step to arrive.
+    constexpr bool kDeep = DIRECT && STAGES > 2u;
+    constexpr uint32_t kAhead = STAGES - 1u;
     load(0u);
     put(0u);
-    if constexpr (DIRECT) {
+    if constexpr (kDeep) {
+#pragma unroll
+        for (uint32_t i = 1; i < kAhead; ++i)
+            if (i < steps) bring(i, 0u, kLoads);
+    } else if constexpr (DIRECT) {
         if (1u < steps) bring(1u, 0u, kHalf);
     } else {
         load(1u);
@@ -540,9 +546,41 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
             if (DIRECT && kMore) bring(s + 2u, a * kHalf / kFC, (a + 1u) * kHalf / kFC);
         });
     };
+    // With more buffers than two a step's loads are under way for kAhead - 1 steps; the buffer they go to is that of the step before this one.
+    const auto step_deep = [&](uint32_t s, auto more) __attribute__((always_inline)) {
+        constexpr bool kMore = decltype(more)::value;                        // kAhead steps are still to come
+        const auto third = [&](uint32_t n, uint32_t a) __attribute__((always_inline)) {
+            if (kMore && a == 0u) bring(s + kAhead, n * kLoads / 3u, (n + 1u) * kLoads / 3u);
+        };
+        multiply(0u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(1u, s, 1u);
+            third(0u, a);
+        });
+        multiply(1u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(0u, s, 2u);
+            third(1u, a);
+        });
+        multiply(0u, [&](uint32_t a) __attribute__((always_inline)) {
+            if (a == 0u) fetch(1u, s, 3u);
+            third(2u, a);
+        });
+        // (A barrier of the language's own would wait for all loads that go to LDS.)
+        if constexpr (kMore) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kAhead - 1u) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (kMore || s + 1u < steps) fetch(0u, s + 1u, 0u);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1u, [](uint32_t) {});
+    };
     uint32_t s = 0u;
-    for (; s + 2u < steps; ++s) step(s, std::true_type{});
-    for (; s < steps; ++s) step(s, std::false_type{});
+    if constexpr (kDeep) {
+        for (; s + kAhead < steps; ++s) step_deep(s, std::true_type{});
+        for (; s < steps; ++s) step_deep(s, std::false_type{});
+    } else {
+        for (; s + 2u < steps; ++s) step(s, std::true_type{});
+        for (; s < steps; ++s) step(s, std::false_type{});
+    }
 
     // To the output through LDS, 32 rows of a wavefront's channels at a time, so that a row's channels are stored end to end (and mul and
     // residual read so); four channels of row r lie in place (channel / 4) ^ (r & 7).
@@ -633,7 +671,7 @@ __global__ __launch_bounds__(WT * WC * 64u) void linear_tile_kernel(LinearParams
     }
 }
 
-// The shares' sums together, eight channels a thread, and the epilogue.  Partial sums are read once, end to end: 64 x 4096 x 11008 in bf16 takes 29 us with
+// The shares' sums together, eight channels a thread, and the epilogue.  Partial sums are read once, end to end: 64 x 4096 x 11008 in bf16 takes 27 us with
 // eight shares and this, 42 with the best kernel that has none.
 template <bool BYTES>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
@@ -651,14 +689,19 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
     finish<8u>(p, row, col, sum);
 }
 
-template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC>
+template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC, uint32_t STAGES>
 bool launch_tile(const LinearParams& p, bool direct, hipStream_t s) {
     const uint64_t tiles_c = (p.cols + CH - 1u) / CH, tiles_t = (p.rows + TOK - 1u) / TOK, joins = (p.rows * p.parts_stride / 8u + 255u) / 256u;
     if (tiles_c * tiles_t >= 1ull << 31 || (p.parts && joins >= 1ull << 31)) return false;
     const dim3 grid(static_cast<uint32_t>(tiles_c * tiles_t), p.shares), threads(WT * WC * 64u);
     const uint32_t c = static_cast<uint32_t>(tiles_c), t = static_cast<uint32_t>(tiles_t);
-    if (direct) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC>), grid, threads, 0, s, p, c, t);
-    else hipLaunchKernelGGL((linear_tile_kernel<BYTES, false, TOK, CH, WT, WC>), grid, threads, 0, s, p, c, t);
+    // Four buffers, three steps' loads under way, where all workgroups that have them find place, two a CU: few others fill a workgroup's waits then.  In
+    // bf16, us with two buffers and with four: 64 x 4096 x 4096 15.0 and 12.7, 64 x 11008 x 4096 34 and 29.5; with more workgroups (256 x 4096 x 4096
+    // in four shares, 1024 of them) 24.1 and 26.9.
+    const bool deep = STAGES > 2u && tiles_c * tiles_t * p.shares <= 2u * device_cus();
+    if (direct && deep) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC, STAGES>), grid, threads, 0, s, p, c, t);
+    else if (direct) hipLaunchKernelGGL((linear_tile_kernel<BYTES, true, TOK, CH, WT, WC, 2u>), grid, threads, 0, s, p, c, t);
+    else hipLaunchKernelGGL((linear_tile_kernel<BYTES, false, TOK, CH, WT, WC, 2u>), grid, threads, 0, s, p, c, t);
     if (p.parts) hipLaunchKernelGGL(linear_join_kernel<BYTES>, dim3(static_cast<uint32_t>(joins)), dim3(256), 0, s, p);
     return true;
 }
@@ -671,10 +714,10 @@ bool launch(const LinearParams& p, LinearKernel kernel, hipStream_t s) {
         case kFew21: return launch_few<BYTES, 2u, 1u, 2u>(p, s);
         case kFew22: return launch_few<BYTES, 2u, 2u, 2u>(p, s);
         case kFew24: return launch_few<BYTES, 2u, 4u, 2u>(p, s);
-        case kTile64: return launch_tile<BYTES, 64u, 64u, 2u, 2u>(p, direct, s);
-        case kTile128: return launch_tile<BYTES, 128u, 128u, 2u, 2u>(p, direct, s);
-        case kTile192: return launch_tile<BYTES, 192u, 256u, 2u, 4u>(p, direct, s);
-        case kTile256: return launch_tile<BYTES, 256u, 256u, 4u, 2u>(p, direct, s);
+        case kTile64: return launch_tile<BYTES, 64u, 64u, 2u, 2u, 4u>(p, direct, s);
+        case kTile128: return launch_tile<BYTES, 128u, 128u, 2u, 2u, 2u>(p, direct, s);
+        case kTile192: return launch_tile<BYTES, 192u, 256u, 2u, 4u, 2u>(p, direct, s);
+        case kTile256: return launch_tile<BYTES, 256u, 256u, 4u, 2u, 2u>(p, direct, s);
         default: break;
     }
     const uint64_t tiles_c = (p.cols + 63u) / 64u, tiles_t = (p.rows + 63u) / 64u;

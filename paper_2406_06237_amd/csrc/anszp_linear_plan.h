@@ -8,7 +8,7 @@
 //                  the chip with few rows, large ones read less from LDS and L2 for a product (8192 x 4096 x 4096 in bf16: 64 x 64 438 us, 128 x 128 277,
 //                  256 x 256 219; 1024 x 4096 x 4096: 50, 53, 87);
 //   shares of k    cost the join's launch and the partial sums' way to memory and back, where tiles alone leave CUs without work (64 x 4096 x 11008 in bf16
-//                  42 us with the best kernel that has no shares, 29 with eight);
+//                  42 us with the best kernel that has no shares, 27 with eight);
 //   memory         gives 4.6 bytes a ps.
 #ifndef ANSZP_LINEAR_PLAN_H
 #define ANSZP_LINEAR_PLAN_H
