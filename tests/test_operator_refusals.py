@@ -206,3 +206,18 @@ def test_new_cache():
                 B.new_kv_cache(**{**dict(n_pages=2, page_size=16, heads=2, head_dim=64, bits=4, device="cpu"), **bad})
         cache = B.new_kv_cache(2, 16, 3, 128, 4, "cpu")
         assert cache.k.shape == (2, 3, 16, 64) and cache.head_dim == 128 and cache.page_size == 16
+
+
+def test_page_tables_are_read_row_after_row(calls):
+    """Sequence s's pages are entries s * width on: the view of a wider table's first columns is none such, at a width of 1 either; one row of it is."""
+    function, operands = _operands()["attend"]
+    wide = torch.zeros(2, 6, dtype=torch.int32)
+    for width in (1, 2, 5):
+        with pytest.raises(ValueError, match="contiguous"):
+            function(**{**operands, "pages": wide[:, :width]})
+    assert calls == []
+    one = dict(q=operands["q"], cache=operands["cache"], lengths=torch.zeros(1, dtype=torch.int32), starts=torch.zeros(2, dtype=torch.int32))
+    for pages in (wide[1:, :1], wide[:1, 2:4], torch.zeros(1, 1, dtype=torch.int32)):
+        function(pages=pages, **one)
+    function(**{**operands, "pages": torch.zeros(2, 1, dtype=torch.int32)})
+    assert calls == ["anszp_attend"] * 4
