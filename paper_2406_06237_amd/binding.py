@@ -1056,7 +1056,7 @@ def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = N
     a.q = _want(q, "q", cache.k.device, (None, None, c.head_dim), torch.bfloat16)
     a.pages = _want(pages, "pages", dev, (None, None), torch.int32)
     n_seqs, width = pages.shape
-    if pages.stride(0) != width and n_seqs > 1:
+    if not pages.is_contiguous():
         raise ValueError("pages must be contiguous")
     a.lengths = _want(lengths, "lengths", dev, (n_seqs,), torch.int32)
     a.starts = _want(starts, "starts", dev, (n_seqs + 1,), torch.int32)

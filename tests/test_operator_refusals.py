@@ -221,3 +221,11 @@ def test_page_tables_are_read_row_after_row(calls):
         function(pages=pages, **one)
     function(**{**operands, "pages": torch.zeros(2, 1, dtype=torch.int32)})
     assert calls == ["anszp_attend"] * 4
+
+
+def test_a_page_table_of_no_columns_is_the_librarys_to_refuse(calls):
+    """It is out of range, not out of order: its strides say nothing."""
+    function, operands = _operands()["attend"]
+    function(**{**operands, "pages": torch.zeros(2, 0, dtype=torch.int32)})
+    assert calls == ["anszp_attend"]
+    assert B.lib().anszp_attend(C.addressof(_attend(table_width=0)), None) == E_RANGE
