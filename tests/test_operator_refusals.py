@@ -228,4 +228,3 @@ def test_a_page_table_of_no_columns_is_the_librarys_to_refuse(calls):
     function, operands = _operands()["attend"]
     function(**{**operands, "pages": torch.zeros(2, 0, dtype=torch.int32)})
     assert calls == ["anszp_attend"]
-    assert B.lib().anszp_attend(C.addressof(_attend(table_width=0)), None) == E_RANGE
