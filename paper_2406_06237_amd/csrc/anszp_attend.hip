@@ -12,13 +12,14 @@
 //     the dimensions [c D / 16, (c + 1) D / 16) of their values, 16 lanes reading a value end to end, and the bytes of one dimension
 //     are brought together by v_perm_b32.  Nothing passes through LDS but the join of the wavefronts' results.
 // Queries are scaled per row by a power of two that puts the largest element in [2^13, 2^14) (exact for all that is within 2^27 of it);
-// weights are 2^9 exp2(score - m) times the value's scale over the power of two above the largest seen: 11 bits for all weights down
-// to 2^-23 of the largest, and less than 2^-34 of it lost of any other.  The 2^6 left below fp16's largest number are for scores that pass m: m
+// weights are 2^9 exp2(score - m) times the value's scale over the power of two above the largest that the query has seen, rounded once: 11 bits for all
+// weights down to 2^-23 of the largest, and less than 2^-34 of it lost of any other.  The 2^6 left below fp16's largest number are for scores that pass m: m
 // and all that was summed under it are changed only where one does so by more than 6 (as log2), or, of 32 queries, some row's maximum would
 // grow in most steps of a few thousand tokens.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "anszp_cus.h"
 #include "anszp_numbers.h"
@@ -444,6 +445,7 @@ __device__ __forceinline__ void loads_ahead() {
 // vector unit is at work for 52 % of the time, the matrix units for 26.
 template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParams p) {
+    static_assert(T == 64u, "a lane looks at one token of a step");
     constexpr uint32_t kThreads = WAVES * 64u;
     constexpr uint32_t kMfmas = D / 32u, kTiles = D / 16u, kVector = D * BITS / 8u, kRows = 16u * WAVES * RT;
     constexpr uint32_t kKeyDims = T * D / kThreads, kValueDims = T * D / (4u * kThreads);             // a thread's: of one key; of each of four values
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     constexpr uint32_t kKeyPieces = D / 8u, kValuePieces = T / 8u;
     __shared__ words4 key_buffer[2][T][kKeyPieces];
     __shared__ words2 value_buffer[2][D][kValuePieces * 2u];
-    __shared__ float key_scales[2][T], value_scales[2][T];
+    alignas(16) __shared__ float key_scales[2][T], value_scales[2][T], ratios[WAVES][T];            // (a wavefront's own: value scales over its power of two)
     __shared__ uint32_t known[2][T / 16u];
     __shared__ int32_t lost[2];                                                         // the last step whose buffer lacks pages
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
@@ -558,12 +560,10 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     words4 q[RT][kMfmas];
     float to_exponent[RT];
     int32_t position[RT];
-    uint64_t out_at[RT];
 #pragma unroll
     for (uint32_t b = 0; b < RT; ++b) {
         const uint32_t row = min(own_row + 16u * b + c, last_row), token = row / p.group, member = row - token * p.group;
         position[b] = t.length - int32_t(t.n_new) + int32_t(token);
-        out_at[b] = uint64_t(t.first_token + token) * p.out_token_stride + uint64_t(head * p.group + member) * p.out_head_stride;
         const uint16_t* from = p.q + uint64_t(t.first_token + token) * p.q_token_stride + uint64_t(head * p.group + member) * p.q_head_stride + g * 8u;
         Eight<ANSZP_OUT_BF16> v[kMfmas];
         float most = 0.0f;
@@ -593,37 +593,54 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
 
     floatx4 acc[kTiles][RT] = {}, sum[RT] = {};                                        // (sums: products with ones, alike in all four)
     const uint32_t one = 0x3C003C00u;
-    float top[RT], limit[RT], reach = 0.0f, less = 0.0f;                  // (the power of two is the wavefront's)
+    // m, 1 over the power of two above the value scales that the row has seen (0: none); the least of those powers among rows that still see any
+    float top[RT], less[RT], settled = 0.0f;
+    const auto reach_of = [](float one_over) __attribute__((always_inline)) { return one_over > 0.0f ? 1.0f / one_over : 0.0f; };
 #pragma unroll
-    for (uint32_t b = 0; b < RT; ++b) top[b] = limit[b] = -__builtin_inff();
+    for (uint32_t b = 0; b < RT; ++b) {
+        top[b] = -__builtin_inff();
+        less[b] = 0.0f;
+    }
     // Places are exclusive ors of what r and j give, so that the lane's own part, of row c and piece g, and the rest of a row and piece make up any of them: one
     // register for all addresses, and registers are what loads from LDS can be under way in.
     const uint32_t key_own = 16u * (c * kKeyPieces + place_of_piece<kKeyPieces>(c, g)), value_own = 16u * (c * kValuePieces + place_of_piece<kValuePieces>(c, g));
-    const auto take = [&](int32_t step) __attribute__((always_inline)) {
+    // APART: the tile's rows do not all see all of the step's tokens, and each has its own power of two from here on; before, all have the same.
+    const auto take = [&](int32_t step, auto apart) __attribute__((always_inline)) {
+        constexpr bool kApart = decltype(apart)::value;
+        if (most_position < 0) return;                                                  // (no rows, or none that see anything)
         const uint32_t in = uint32_t(step) & 1u;
         const uint32_t key_at = key_own + in * uint32_t(sizeof key_buffer[0]), value_at = value_own + in * uint32_t(sizeof value_buffer[0]);
-        {                                                                               // values larger than any before
-            const float far = fabsf(value_scales[in][lane % T]);
-            if (__any(far > reach)) {
-                float high = most_of_query(far);
-                for (int x = 8; x; x >>= 1) high = fmaxf(high, __shfl_xor(high, x));
-                const float now = fmaxf(reach, power_above(high));
-                less = 1.0f / now;
-                const float kept = reach * less;
-                reach = now;
+        const float scale = value_scales[in][lane];
+        const bool larger = __any(fabsf(scale) > settled);
+        float rescaled[RT];
 #pragma unroll
-                for (uint32_t e = 0; e < kTiles; ++e)
-#pragma unroll
-                    for (uint32_t b = 0; b < RT; ++b) acc[e][b] *= kept;
+        for (uint32_t b = 0; b < RT; ++b) rescaled[b] = 1.0f;
+        if (larger) {                                                                   // values larger than any that some row has seen
+            float upto = fabsf(scale);                                                  // the largest of the step's tokens up to the lane's own
+            for (uint32_t d = 1; d < 64u; d <<= 1) {
+                const float other = __shfl_up(upto, d);
+                if (lane >= d) upto = fmaxf(upto, other);
             }
+            float lowest = __builtin_inff();
+#pragma unroll
+            for (uint32_t b = 0; b < RT; ++b) {
+                const int32_t last = min(position[b] - (begin + step * int32_t(T)), 63);          // of the step's tokens, that the row sees
+                const float seen = __shfl(upto, max(last, 0)), before = reach_of(less[b]);
+                const float now = last < 0 ? before : fmaxf(before, power_above(seen));
+                if (last >= 0) lowest = fminf(lowest, now);                             // (the others see nothing any more)
+                less[b] = now > 0.0f ? 1.0f / now : 0.0f;
+                rescaled[b] = before * less[b];                                         // (done with the maximum's, below)
+            }
+            for (int x = 8; x; x >>= 1) lowest = fminf(lowest, __shfl_xor(lowest, x));
+            settled = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int32_t, lowest)));
         }
+        if constexpr (!kApart) ratios[wave][lane] = scale * less[0];
         const bool lacking = lost[in] == step;
 #pragma unroll
         for (uint32_t h = 0; h < T / 32u; ++h) {
             const int32_t t0 = begin + step * int32_t(T) + int32_t(32u * h);
-            if (t0 > most_position || t0 >= end) break;                                 // nothing that these rows see
+            if (kApart && (t0 > most_position || t0 >= end)) break;                     // nothing that these rows see
             float y[RT][8];
-            f16x2 ratio[4];
 #pragma unroll
             for (uint32_t u = 0; u < 2u; ++u) {
                 const uint32_t row = 32u * h + 16u * u;
@@ -636,16 +653,13 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                     for (uint32_t b = 0; b < RT; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, q[b][m]), s[b], 0, 0, 0);
                 }
                 const floatx4 ks = *reinterpret_cast<const floatx4*>(&key_scales[in][32u * h + 16u * u + 4u * g]);
-                const floatx4 vs = *reinterpret_cast<const floatx4*>(&value_scales[in][32u * h + 16u * u + 4u * g]) * less;
-                ratio[2u * u] = f16x2{static_cast<_Float16>(vs[0]), static_cast<_Float16>(vs[1])};
-                ratio[2u * u + 1u] = f16x2{static_cast<_Float16>(vs[2]), static_cast<_Float16>(vs[3])};
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b)
 #pragma unroll
                     for (uint32_t i = 0; i < 4u; ++i) y[b][4u * u + i] = s[b][i] * ks[i];
             }
             loads_ahead<2u * kMfmas, RT, 1>();
-            const bool whole = !lacking && t0 + 31 <= least_position && t0 + 32 <= end;
+            const bool whole = !lacking && (!kApart || t0 + 31 <= least_position) && t0 + 32 <= end;
             if (!whole) {
 #pragma unroll
                 for (uint32_t n = 0; n < 8u; ++n) {
@@ -653,7 +667,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                     const bool held = place < end && known[in][2u * h + n / 4u];
 #pragma unroll
                     for (uint32_t b = 0; b < RT; ++b)
-                        y[b][n] = held && place <= position[b] ? y[b][n] : -__builtin_inff();
+                        y[b][n] = held && (!kApart || place <= position[b]) ? y[b][n] : -__builtin_inff();
                 }
             }
             bool grows = false;
@@ -663,20 +677,23 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                 high[b] = fmaxf(y[b][0], y[b][1]);
 #pragma unroll
                 for (uint32_t n = 2; n < 8u; n += 2u) high[b] = fmaxf(fmaxf(high[b], y[b][n]), y[b][n + 1u]);
-                grows |= high[b] > limit[b];
+                grows |= (high[b] - top[b]) * to_exponent[b] > kSlack;
             }
-            if (__any(grows)) {
+            const bool moves = __any(grows);
+            if (moves || (h == 0u && larger)) {
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b) {
-                    const float now = fmaxf(top[b], most_of_query(high[b]));
-                    const float kept = __builtin_amdgcn_exp2f((top[b] - (now == -__builtin_inff() ? 0.0f : now)) * to_exponent[b]);
+                    const float now = moves ? fmaxf(top[b], most_of_query(high[b])) : top[b];
+                    const float kept = moves ? __builtin_amdgcn_exp2f((top[b] - (now == -__builtin_inff() ? 0.0f : now)) * to_exponent[b]) : 1.0f;
+                    const float kept_values = h == 0u ? kept * rescaled[b] : kept;
                     top[b] = now;
-                    limit[b] = now + fminf(kSlack / to_exponent[b], 0x1p126f);
                     sum[b] *= kept;
 #pragma unroll
-                    for (uint32_t e = 0; e < kTiles; ++e) acc[e][b] *= kept;
+                    for (uint32_t e = 0; e < kTiles; ++e) acc[e][b] *= kept_values;
                 }
             }
+            const float* const scales = kApart ? &value_scales[in][32u * h + 4u * g] : &ratios[wave][32u * h + 4u * g];
+            const floatx4 vs[2] = {reinterpret_cast<const floatx4*>(scales)[0], reinterpret_cast<const floatx4*>(scales)[4]};
             words4 weights[RT];
 #pragma unroll
             for (uint32_t b = 0; b < RT; ++b) {
@@ -684,10 +701,11 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
                 const float less_top = 15.0f - kSlack - (top[b] == -__builtin_inff() ? 0.0f : top[b]) * to_exponent[b];
 #pragma unroll
                 for (uint32_t n = 0; n < 8u; n += 2u) {
-                    const f16x2 e = {static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n], to_exponent[b], less_top))),
-                                     static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(y[b][n + 1u], to_exponent[b], less_top)))};
-                    plain[n / 2u] = bits_of(e);
-                    weights[b][n / 2u] = bits_of(e * ratio[n / 2u]);
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(y[b][n], to_exponent[b], less_top)), e1 = __builtin_amdgcn_exp2f(fmaf(y[b][n + 1u], to_exponent[b], less_top));
+                    plain[n / 2u] = bits_of(f16x2{static_cast<_Float16>(e0), static_cast<_Float16>(e1)});
+                    // Rounded once.  (In this order nothing is left of a token that the row does not see, however far it is above the row's power of two.)
+                    const float by = kApart ? less[b] : 1.0f;
+                    weights[b][n / 2u] = bits_of(f16x2{static_cast<_Float16>(e0 * vs[n / 4u][n & 3u] * by), static_cast<_Float16>(e1 * vs[n / 4u][(n + 1u) & 3u] * by)});
                 }
                 sum[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, words4{one, one, one, one}), __builtin_bit_cast(f16x8, plain), sum[b], 0, 0, 0);
             }
@@ -711,13 +729,18 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
         ask(1);
         ask_pages(2);
         __syncthreads();
-        for (int32_t step = 0; step < steps; ++step) {
-            take(step);
+        // Steps that all of the tile's rows see whole first: they have less to look at.
+        const int32_t shared = max(0, t.length - int32_t(t.n_new) + int32_t(t.first_row / p.group) + 1 - begin) / int32_t(T);
+        const auto round = [&](int32_t step, auto apart) __attribute__((always_inline)) {
+            take(step, apart);
             put(step + 1);                                                              // (behind the end: nothing that is looked at)
             ask(step + 2);
             ask_pages(step + 3);
             __syncthreads();
-        }
+        };
+        int32_t step = 0;
+        for (; step < min(shared, steps); ++step) round(step, std::false_type{});
+        for (; step < steps; ++step) round(step, std::true_type{});
     }
     if (missing) flag(p);
 #pragma unroll
@@ -725,7 +748,9 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
         const float l = sum[b][0];
         const uint32_t r = wave * (16u * RT) + 16u * b + c;
         if (r >= t.n_rows) continue;
-        const float over = p.splits > 1u ? reach : l == 0.0f ? 0.0f : reach / l;
+        const uint32_t row = t.first_row + r, token = row / p.group, member = row - token * p.group;
+        const uint64_t out_at = uint64_t(t.first_token + token) * p.out_token_stride + uint64_t(head * p.group + member) * p.out_head_stride;
+        const float over = p.splits > 1u ? reach_of(less[b]) : l == 0.0f ? 0.0f : reach_of(less[b]) / l;
         if (p.splits > 1u && g == 0u) reinterpret_cast<float2*>(p.part_stats)[part * kRows + r] = make_float2(top[b] * to_exponent[b], l);
 #pragma unroll
         for (uint32_t e = 0; e < kTiles; ++e) {
@@ -734,9 +759,9 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
             if (p.splits > 1u)
                 *reinterpret_cast<floatx4*>(p.parts + (part * kRows + r) * D + d) = o;
             else if (p.out_dtype == ANSZP_OUT_BF16)
-                *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + out_at[b] + d) = words2{to_bf16_pair(o[0], o[1]), to_bf16_pair(o[2], o[3])};
+                *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + out_at + d) = words2{to_bf16_pair(o[0], o[1]), to_bf16_pair(o[2], o[3])};
             else
-                *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + out_at[b] + d) = __builtin_bit_cast(words4, o);
+                *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + out_at + d) = __builtin_bit_cast(words4, o);
         }
     }
 }

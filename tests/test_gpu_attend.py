@@ -229,3 +229,44 @@ def test_a_maximum_that_rises(dim, bits, rise):
             at = torch.arange(n, device=DEV)
             cache.k_params[table[s, at // 32].long(), 0, at % 32, 0] = 0.6931 * rise * (at / 32.0 + 1.0) / (mean * dim)
         _check(case, "f32", scale=1.0, what=(lengths, rise))
+
+
+WIDTHS = [(64, 8), (128, 8), (128, 4), (256, 8)]
+
+
+@pytest.mark.parametrize("by", [1e-30, 1e-6, 1e6, 1e30])
+@pytest.mark.parametrize("dim,bits", WIDTHS)
+def test_value_scales_of_all_sizes_in_chunks(dim, bits, by):
+    """Of many rows, too: some values a million times smaller than others, and all of them small or large; zeros."""
+    case = _case([150, 90], [120, 70], 1, 2, dim, 16, bits)
+    v = case[0].v_params
+    v[..., 0] *= by
+    v[::2, :, 3:9, 0] *= 1e-6
+    v[1::2, :, 9:12, 0] = 0
+    _check(case, "f32")
+    v[..., 0] = 0
+    assert (B.attend(case[1], *((case[0],) + case[2:])) == 0).all()
+
+
+@pytest.mark.parametrize("by", [2.0 ** 16, 2.0 ** 20, 2.0 ** 26, 2.0 ** 60, 1e30])
+@pytest.mark.parametrize("dim,bits", WIDTHS)
+def test_later_tokens_of_any_size(dim, bits, by):
+    """A query's output does not depend on values of tokens behind it, however large they are; those that see them have them, and lose of the
+    others what is below 2^-34 of the largest's scale for each symbol: half a unit of the least weight in fp16, 2^-24, beside 2^9 for the maximum's."""
+    for group, new in ((2, 150), (4, 90), (1, 130), (2, 1)):
+        case = _case([210, 95], [new, min(new, 90)], 1, group, dim, 32, bits)
+        cache, q, table, lengths, starts = case
+        want = B.attend(q, cache, table, lengths, starts, out_dtype="f32")
+        loud = (130, 163, 209)
+        for t in loud:
+            cache.v_params[table[0, t // 32], :, t % 32, 0] *= by
+        got = B.attend(q, cache, table, lengths, starts, out_dtype="f32")
+        before = max(0, loud[0] - (210 - new))
+        assert torch.equal(got[:before], want[:before]) and torch.equal(got[new:], want[new:])
+        plain, error = P.attend(q, P.values(cache.k, cache.k_params, bits), P.values(cache.v, cache.v_params, bits), table, lengths, starts, 32, dim ** -0.5)
+        at = torch.arange(210)
+        scales = P.wide(cache.v_params)[table[0].cpu().long()[at // 32], 0, at % 32, 0]
+        for i in range(new):
+            seen = 210 - new + i + 1
+            error[i] += seen * 2.0 ** -34 * 2 * scales[:seen].max() * (2 ** bits - 1)
+        P.assert_within(got, plain, error + plain.abs() * 2.0 ** -24, (group, new))
