@@ -102,7 +102,7 @@ __device__ __forceinline__ float row_factor(const NormParams& p, const Gathered&
 template <uint32_t DTYPE, uint32_t THREADS, uint32_t NV>
 __global__ __launch_bounds__(THREADS == 64u ? 256u : THREADS) void rms_norm_kernel(NormParams p) {
     const uint32_t t = THREADS == 64u ? threadIdx.x & 63u : threadIdx.x;
-    const uint64_t row = THREADS == 64u ? uint64_t(blockIdx.x) * 4u + (threadIdx.x >> 6) : blockIdx.x;
+    const uint64_t group = uint64_t(blockIdx.y) * kAcross + blockIdx.x, row = THREADS == 64u ? group * 4u + (threadIdx.x >> 6) : group;
     if (row >= p.rows) return;
     Eight<DTYPE> x[NV], r[NV];
     float g[NV][8];
@@ -138,7 +138,8 @@ __global__ __launch_bounds__(THREADS == 64u ? 256u : THREADS) void rms_norm_kern
 // Longer rows are read twice.  What is written over an input is written when the thread has read it for the last time.
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormParams p) {
-    const uint64_t row = blockIdx.x;
+    const uint64_t row = uint64_t(blockIdx.y) * kAcross + blockIdx.x;
+    if (row >= p.rows) return;
     Gathered mine = {0.0f, 0.0f, 0.0f};
     float factor = 0.0f;
     for (uint32_t pass = 0; pass < 2u; ++pass) {
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormParams p) {
 template <uint32_t DTYPE>
 void launch(const NormParams& p, hipStream_t s) {
     const uint32_t eights = (p.cols + 7u) / 8u;
-    const dim3 rows(static_cast<uint32_t>(p.rows)), fours(static_cast<uint32_t>((p.rows + 3u) / 4u));
+    const dim3 rows(groups_across(p.rows), groups_down(p.rows)), fours(groups_across((p.rows + 3u) / 4u), groups_down((p.rows + 3u) / 4u));
     if (eights <= 64u) hipLaunchKernelGGL((rms_norm_kernel<DTYPE, 64u, 1u>), fours, dim3(256), 0, s, p);
     else if (eights <= 128u) hipLaunchKernelGGL((rms_norm_kernel<DTYPE, 64u, 2u>), fours, dim3(256), 0, s, p);
     else if (eights <= 256u) hipLaunchKernelGGL((rms_norm_kernel<DTYPE, 256u, 1u>), rows, dim3(256), 0, s, p);

@@ -88,6 +88,12 @@ __device__ __forceinline__ void store_eight(void* base, uint32_t dtype, uint64_t
     }
 }
 
+// A launch counts its threads in 32 bits in each dimension, and what is beyond is left out without an error: workgroups that can be more than that come in
+// rows of kAcross (of up to 1024 threads each).
+constexpr uint32_t kAcross = 1u << 21;
+inline uint32_t groups_across(uint64_t groups) { return static_cast<uint32_t>(groups < kAcross ? groups : kAcross); }
+inline uint32_t groups_down(uint64_t groups) { return static_cast<uint32_t>((groups + kAcross - 1u) / kAcross); }
+
 __device__ __forceinline__ uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 
 #endif

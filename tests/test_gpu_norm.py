@@ -93,3 +93,20 @@ def test_weights_of_the_other_type_and_rows_many():
 def test_no_rows():
     out, scales, total = B.rms_norm(torch.zeros(0, 64, device=DEV), torch.ones(64, device=DEV), residual=torch.zeros(0, 64, device=DEV), out_dtype="i8")
     assert out.shape == (0, 64) and scales.shape == (0,) and total.shape == (0, 64)
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 26) + 3, 8), ((1 << 24) + 1, 1032)])
+def test_rows_beyond_one_dimension_of_a_launch(rows, cols):
+    """More rows than 2^32 threads have: every row is written."""
+    some = torch.randn(4096, cols, device=DEV).to(torch.bfloat16)
+    x = some[:1].expand(rows, cols) if cols > 64 else some.repeat(rows // 4096 + 1, 1)[:rows]
+    q, scales = B.quantise_rows(x)
+    want, by = B.quantise_rows(some)
+    torch.cuda.synchronize()
+    for at in (0, 1, rows // 2, (1 << 22) - 1, 1 << 22, 1 << 24, rows - 1):
+        i = 0 if cols > 64 else at % 4096
+        assert torch.equal(q[at], want[i]) and torch.equal(scales[at], by[i]), at
+    if cols > 64:
+        assert torch.equal(scales, by[:1].expand(rows))
+    else:
+        assert torch.equal(scales[:rows // 4096 * 4096].view(-1, 4096), by.expand(rows // 4096, 4096))
