@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheParams p) {
     const uint32_t lanes = 1u << p.lanes_log;                       // 8, 16 or 32
     const uint32_t which = blockIdx.y;
     const uint32_t lane = threadIdx.x & (lanes - 1u);
-    const uint64_t n = (uint64_t(blockIdx.x) * 256u + threadIdx.x) >> p.lanes_log;
+    const uint64_t n = ((uint64_t(blockIdx.z) * kAcross + blockIdx.x) * 256u + threadIdx.x) >> p.lanes_log;
     if (n >= p.vectors) return;                                     // (whole vectors of lanes leave)
     const Vector at = vector_of(p, n);
     int64_t slot = p.slots[at.token];
@@ -133,7 +133,7 @@ template <uint32_t BITS>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheParams p, uint32_t out_dtype) {
     const uint32_t which = blockIdx.y;
     const uint32_t lane = threadIdx.x & ((1u << p.lanes_log) - 1u);
-    const uint64_t n = (uint64_t(blockIdx.x) * 256u + threadIdx.x) >> p.lanes_log;
+    const uint64_t n = ((uint64_t(blockIdx.z) * kAcross + blockIdx.x) * 256u + threadIdx.x) >> p.lanes_log;
     if (n >= p.vectors) return;
     const Vector at = vector_of(p, n);
     const int64_t slot = p.slots[at.token];
@@ -174,7 +174,10 @@ int cache_params(const anszp_cache_t* c, const int64_t* slots, uint64_t n_tokens
     return p.vectors * (c->head_dim / 8u) / 256u >= 1ull << 31 ? ANSZP_E_RANGE : ANSZP_OK;
 }
 
-dim3 grid_of(const CacheParams& p) { return dim3(static_cast<uint32_t>((p.vectors * (p.dim / 8u) + 255u) / 256u), 2); }
+dim3 grid_of(const CacheParams& p) {
+    const uint64_t groups = (p.vectors * (p.dim / 8u) + 255u) / 256u;
+    return dim3(groups_across(groups), 2, groups_down(groups));
+}
 
 }  // namespace
 

@@ -93,3 +93,18 @@ def test_a_cache_of_more_than_4_gib():
     for x, y in zip((k, v), got):
         q, scale, zero = P.quantise(x, 8)
         assert torch.equal(y.cpu(), torch.from_numpy(scale[..., None] * (q.astype(np.float32) - zero[..., None])))
+
+
+def test_vectors_beyond_one_dimension_of_a_launch():
+    """More vectors than 2^32 threads have lanes for.  Few of the tokens are written: the others have a negative slot."""
+    heads, dim, tokens = 65535, 256, 2050
+    cache = B.new_kv_cache(1, 16, heads, dim)
+    k = torch.randn(1, heads, dim, device=DEV).to(torch.bfloat16)
+    slots = torch.full((tokens,), -1, dtype=torch.int64, device=DEV)
+    slots[torch.tensor([0, 1023, 1025, 2047, 2048, 2049])] = torch.tensor([3, 0, 7, 8, 15, 12], device=DEV)
+    B.cache_write(cache, k.expand(tokens, heads, dim), (-k).expand(tokens, heads, dim), slots)
+    less = B.new_kv_cache(1, 16, heads, dim)
+    B.cache_write(less, k.expand(6, heads, dim), (-k).expand(6, heads, dim), slots[slots >= 0])
+    for a, b in ((cache.k, less.k), (cache.v, less.v), (cache.k_params, less.k_params), (cache.v_params, less.v_params)):
+        assert torch.equal(a, b)
+    assert (less.k_params[0, :, [0, 3, 7, 8, 12, 15], 0] > 0).all()
