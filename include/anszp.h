@@ -454,7 +454,7 @@ typedef struct {
     const void*  mul;             /* [device] rows x cols of out_dtype, or NULL                      */
     const void*  residual;        /* [device] rows x cols of out_dtype, or NULL                      */
     void*        out;             /* [device] rows x cols of out_dtype; may be mul or residual (same stride), apart from x and weight */
-    uint64_t     rows, cols;      /* each < 2^31, may be 0                                           */
+    uint64_t     rows, cols;      /* each < 2^31, may be 0; fewer than 2^24 tiles of 64 x 64 together */
     uint64_t     x_stride, weight_stride, mul_stride, residual_stride, out_stride;
     uint32_t     k;               /* 1 .. 2^30 (x in 8 bits: 65536, so that sums fit 32 bits)        */
     uint32_t     x_dtype;         /* ANSZP_OUT_BF16 or ANSZP_I8                                      */

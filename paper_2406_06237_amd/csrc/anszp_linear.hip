@@ -376,7 +376,7 @@ template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t PIECES>
 bool launch_few(const LinearParams& p, hipStream_t s) {
     constexpr uint32_t kWaves = 8u;
     const uint64_t groups_c = (p.cols + 16u * CH - 1u) / (16u * CH), groups_t = (p.rows + 16u * TOK - 1u) / (16u * TOK);
-    if (groups_c >= 1ull << 31 || groups_t > 65535u) return false;
+    if (groups_c * (kWaves * 64u) >= 1ull << 32 || groups_t > 65535u) return false;
     hipLaunchKernelGGL((linear_few_kernel<BYTES, TOK, CH, kWaves, PIECES>), dim3(static_cast<uint32_t>(groups_c), static_cast<uint32_t>(groups_t)), dim3(kWaves * 64u), 0, s, p);
     return true;
 }
@@ -692,7 +692,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
 template <bool BYTES, uint32_t TOK, uint32_t CH, uint32_t WT, uint32_t WC, uint32_t STAGES>
 bool launch_tile(const LinearParams& p, bool direct, hipStream_t s) {
     const uint64_t tiles_c = (p.cols + CH - 1u) / CH, tiles_t = (p.rows + TOK - 1u) / TOK, joins = (p.rows * p.parts_stride / 8u + 255u) / 256u;
-    if (tiles_c * tiles_t >= 1ull << 31 || (p.parts && joins >= 1ull << 31)) return false;
+    if (tiles_c * tiles_t * (WT * WC * 64u) >= 1ull << 32 || (p.parts && joins * 256u >= 1ull << 32)) return false;
     const dim3 grid(static_cast<uint32_t>(tiles_c * tiles_t), p.shares), threads(WT * WC * 64u);
     const uint32_t c = static_cast<uint32_t>(tiles_c), t = static_cast<uint32_t>(tiles_t);
     // Four buffers, three steps' loads under way, where all workgroups that have them find place, two a CU: few others fill a workgroup's waits then.  In
@@ -721,7 +721,7 @@ bool launch(const LinearParams& p, LinearKernel kernel, hipStream_t s) {
         default: break;
     }
     const uint64_t tiles_c = (p.cols + 63u) / 64u, tiles_t = (p.rows + 63u) / 64u;
-    if (tiles_c * tiles_t >= 1ull << 31) return false;
+    if (tiles_c * tiles_t * 256u >= 1ull << 32) return false;               // (what is beyond would be left out without an error)
     hipLaunchKernelGGL(linear_any_kernel<BYTES>, dim3(static_cast<uint32_t>(tiles_c * tiles_t)), dim3(256), 0, s, p, static_cast<uint32_t>(tiles_c));
     return true;
 }

@@ -33,9 +33,11 @@ inline LinearPlan linear_plan(bool eight_bits, uint64_t rows, uint64_t cols, uin
     double least = 1e300;
     const double memory = double(rows + cols) * k_bytes / 4600.0, launch = 1500.0;
     const auto groups = [](uint64_t n, uint32_t of) { return (n + of - 1u) / of; };
+    const uint64_t most_groups = 1ull << 23;               // (a launch leaves out what is beyond 2^32 threads, and the largest of these workgroups have 512)
     struct Few { LinearKernel kernel; uint32_t tok, ch; };
     for (const Few& f : {Few{kFew11, 1u, 1u}, Few{kFew21, 2u, 1u}, Few{kFew22, 2u, 2u}, Few{kFew24, 2u, 4u}}) {
         if (rows > 4096u) break;
+        if (groups(cols, 16u * f.ch) >= most_groups) continue;
         const uint64_t n = groups(groups(cols, 16u * f.ch) * groups(rows, 16u * f.tok), cus);
         const double t = launch + std::max(memory, double(n) * (f.tok + f.ch) * 16.0 * k_bytes / 33.0);
         if (t < least) {
@@ -50,7 +52,8 @@ inline LinearPlan linear_plan(bool eight_bits, uint64_t rows, uint64_t cols, uin
                               {kTile256, 256u, 256u, {1600.0, 2000.0}, {1600.0, 2000.0}, 1u}};
     const uint32_t steps = (k_bytes + kLinearStepBytes - 1u) / kLinearStepBytes, whole = k_bytes / kLinearStepBytes;
     if (std::max(x_stride, w_stride) <= 1u << 23)
-        for (const TileKind& t : tiles)
+        for (const TileKind& t : tiles) {
+            if (groups(cols, t.ch) * groups(rows, t.tok) >= most_groups) continue;
             for (uint32_t s = 1u; s <= t.most_shares && (s == 1u || (may_share && steps >= 4u * s)); s *= 2u) {
                 const uint32_t share_steps = s == 1u ? whole : (steps + s - 1u) / s, shares = s == 1u ? 1u : std::max(1u, (whole + share_steps - 1u) / share_steps);
                 if (s > 1u && shares == 1u) continue;
@@ -65,6 +68,7 @@ inline LinearPlan linear_plan(bool eight_bits, uint64_t rows, uint64_t cols, uin
                     best.workspace = shares > 1u ? uint64_t(shares) * rows * best.parts_stride * 4u : 0u;
                 }
             }
+        }
     return best;
 }
 

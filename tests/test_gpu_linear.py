@@ -133,3 +133,15 @@ def test_nothing_to_do():
     x, w = torch.zeros(0, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(32, 64, dtype=torch.bfloat16, device=DEV)
     assert B.linear(x, w).shape == (0, 32)
     assert B.linear(torch.zeros(3, 64, dtype=torch.bfloat16, device=DEV), w[:0]).shape == (3, 0)
+
+
+@pytest.mark.parametrize("k", [7, 24])
+def test_channels_beyond_one_dimension_of_a_launch(k):
+    """More channels than 2^32 threads of few rows' kernel have: every one is written.  All have the same weights."""
+    x, w = torch.randn(2, 1, k, device=DEV).to(torch.bfloat16)
+    cols = (1 << 27) + 70
+    out = torch.full((1, cols), float("nan"), dtype=torch.bfloat16, device=DEV)
+    B.linear(x, w.expand(cols, k), out=out)
+    want, error = P.linear(x, w)
+    P.assert_within(out[:, :1], want, error + want.abs() * P.HALF_ULP[torch.bfloat16])
+    assert (out == out[0, 0]).all()

@@ -72,3 +72,18 @@ def test_rows_far_apart(plan):
             assert not got[0].startswith("tile")
         for got in plan([_call(5000, 4096, 4096, False, stride=1 << 23)]):
             assert got[0].startswith("tile")
+
+
+def test_a_launch_has_fewer_than_2_to_the_32_threads(plan):
+    """What is beyond is left out without an error.  (The kernel for any sizes has no other to give way to: the call is refused.)"""
+    tiles = {"few11": (16, 16, 512), "few21": (32, 16, 512), "few22": (32, 32, 512), "few24": (32, 64, 512), "tile64": (64, 64, 256), "tile128": (128, 128, 256),
+             "tile192": (192, 256, 512), "tile256": (256, 256, 512)}
+    calls = [_call(r, c, k, e) for r in (1, 16, 33, 300, 4096, 1 << 17, 1 << 21) for c in (1, 4096, 1 << 20, (1 << 26) + 1, (1 << 27) - 15, (1 << 27) + 70, (1 << 28) + 1, (1 << 30) - 63)
+             for k in (8, 16, 64) for e in (False, True) if r * c <= 1 << 35]
+    for call, got in zip(calls, plan(calls)):
+        if got[0] == "any":
+            assert call[3] < 16 or call[1] * call[2] > 1 << 34
+            continue
+        tok, ch, threads = tiles[got[0]]
+        across = -(-call[2] // ch)
+        assert across * (1 if got[0].startswith("few") else -(-call[1] // tok)) * threads < 1 << 32, (call, got)

@@ -228,3 +228,9 @@ def test_a_page_table_of_no_columns_is_the_librarys_to_refuse(calls):
     function, operands = _operands()["attend"]
     function(**{**operands, "pages": torch.zeros(2, 0, dtype=torch.int32)})
     assert calls == ["anszp_attend"]
+
+
+def test_products_of_more_threads_than_a_launch_has():
+    """Refused: a launch would leave them out without an error."""
+    for rows, cols in ((1, 1 << 30), (1 << 30, 64), (1 << 20, 1 << 16)):
+        assert _linear(rows=rows, cols=cols, k=7, out_stride=cols, x_dtype=B.OUT_BF16) == E_RANGE
