@@ -517,7 +517,8 @@ typedef struct {
                                      have seen; its positions are not seen, [1] grows                 */
     void*          workspace;     /* [device] anszp_attend_workspace_bytes, 16-byte aligned, in use until the call is done */
     uint64_t       workspace_bytes;
-    uint64_t       n_tokens, n_seqs;                      /* each < 2^24, may be 0                    */
+    uint64_t       n_tokens, n_seqs;                      /* each < 2^24, may be 0; more than a launch has threads for is E_RANGE, which n_tokens * group + 16 *
+                                     n_seqs < 2^28 and (n_tokens * group + 128 * n_seqs) * heads < 2^30 never are */
     uint64_t       q_token_stride, q_head_stride, out_token_stride, out_head_stride;
     uint32_t       table_width;   /* >= 1; table_width * page_size <= 2^30                           */
     uint32_t       group;         /* query heads per head of the cache, 1 .. 256                     */

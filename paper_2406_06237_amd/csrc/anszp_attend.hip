@@ -867,6 +867,12 @@ bool in_range(const anszp_attend_args_t& a) {
              a.group > 256u || (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || (a.n_tokens * a.group / kTileRows + a.n_seqs) * c.heads >= 1ull << 31);
 }
 
+// A launch leaves out what is beyond 2^32 threads in a dimension, without an error.
+bool fits_a_launch(const anszp_attend_args_t& a, const Shares& s) {
+    const uint64_t groups = s.rows == kTileRows ? s.tiles : uint64_t(s.tiles) * a.cache.heads;
+    return groups * (s.rows == kTileRows || a.cache.head_dim < 256u ? 256u : 512u) < 1ull << 32 && uint64_t(s.tiles) * 256u < 1ull << 32;
+}
+
 uint64_t workspace_of(const anszp_attend_args_t& a, const Shares& s) {
     return s.splits > 1u ? uint64_t(s.splits) * s.tiles * a.cache.heads * s.rows * (a.cache.head_dim + 2u) * sizeof(float) : 0u;
 }
@@ -906,6 +912,7 @@ int anszp_attend(const anszp_attend_args_t* a, void* hip_stream) {
     if (a->n_tokens == 0u || a->n_seqs == 0u) return ANSZP_OK;
     if (!a->q || !a->out || !a->pages || !a->lengths || !a->starts) return ANSZP_E_NULL;
     const Shares s = shares_of(*a);
+    if (!fits_a_launch(*a, s)) return ANSZP_E_RANGE;
     const uint64_t need = workspace_of(*a, s);
     if (need && !a->workspace) return ANSZP_E_NULL;
     if (a->workspace_bytes < need || (reinterpret_cast<uintptr_t>(a->workspace) & 15u)) return ANSZP_E_RANGE;

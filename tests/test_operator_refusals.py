@@ -234,3 +234,12 @@ def test_products_of_more_threads_than_a_launch_has():
     """Refused: a launch would leave them out without an error."""
     for rows, cols in ((1, 1 << 30), (1 << 30, 64), (1 << 20, 1 << 16)):
         assert _linear(rows=rows, cols=cols, k=7, out_stride=cols, x_dtype=B.OUT_BF16) == E_RANGE
+
+
+def test_attention_of_more_threads_than_a_launch_has():
+    """Refused: a launch would leave them out without an error."""
+    for cache, many in ((dict(heads=2), dict(n_tokens=(1 << 24) - 1, n_seqs=1, group=256)),                     # 128 rows a workgroup
+                        (dict(heads=2, head_dim=256), dict(n_tokens=1 << 23, n_seqs=1, group=256)),
+                        (dict(heads=1), dict(n_tokens=64, n_seqs=(1 << 24) - 1, group=1))):                      # 16
+        a = _attend(cache=cache, **many)
+        assert B.lib().anszp_attend(C.addressof(a), None) == E_RANGE, many
