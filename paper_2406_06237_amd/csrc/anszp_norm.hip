@@ -68,15 +68,25 @@ __device__ __forceinline__ void weights_of(const NormParams& p, uint32_t at, uin
     }
 }
 
-// h * g on: times the row's factor, rounded and stored.  8 bits: `factor` is 127 / max|h * g|.
-__device__ __forceinline__ void store_row_part(const NormParams& p, uint64_t row, uint32_t at, uint32_t there, const float (&y)[8], float factor) {
+// What takes h * g to what is stored: times `factor`, or with 8 bits of a row near binary32's least numbers, where 127 / max|h * g| is more than 32 bits
+// hold, times 2^64 before.
+struct Factor {
+    float factor;
+    bool tiny;
+};
+constexpr float kLift = 0x1p64f;
+
+// h * g on: times the row's factor, rounded and stored.
+__device__ __forceinline__ void store_row_part(const NormParams& p, uint64_t row, uint32_t at, uint32_t there, const float (&y)[8], const Factor& by) {
     float v[8];
-    for (uint32_t i = 0; i < 8u; ++i) v[i] = y[i] * factor;
+    for (uint32_t i = 0; i < 8u; ++i) v[i] = y[i] * by.factor;
     const uint64_t to = row * p.out_stride + at;
     if (p.out_dtype != ANSZP_I8) {
         store_eight(p.out, p.out_dtype, to, there, v);
         return;
     }
+    if (by.tiny)
+        for (uint32_t i = 0; i < 8u; ++i) v[i] = __builtin_amdgcn_fmed3f(y[i] * kLift * by.factor, -127.0f, 127.0f);    // (the scale may have been rounded down)
     words2 q = {0u, 0u};
     for (uint32_t i = 0; i < 8u; ++i) q[i >> 2] |= (uint32_t(int32_t(rintf(v[i]))) & 0xFFu) << (8u * (i & 3u));
     int8_t* out = static_cast<int8_t*>(p.out) + to;
@@ -88,14 +98,20 @@ __device__ __forceinline__ void store_row_part(const NormParams& p, uint64_t row
     }
 }
 
-// The factor that takes h * g to what is stored.  A row with an infinity or a NaN has no 8-bit form: its scale is NaN, its symbols 0.
-__device__ __forceinline__ float row_factor(const NormParams& p, const Gathered& g, uint64_t row, bool writes) {
+// 8 bits: 127 / max|h * g|.  A row with an infinity or a NaN has no 8-bit form: its scale is NaN, its symbols 0.  Where the scale or
+// the largest h * g is near binary32's least numbers (below 2^-100), the symbols are y over the scale as it is stored, which may have few bits left.
+__device__ __forceinline__ Factor row_factor(const NormParams& p, const Gathered& g, uint64_t row, bool writes) {
     const float norm = p.normalise ? 1.0f / sqrtf(g.squares * p.inverse_cols + p.eps) : 1.0f;
-    if (p.out_dtype != ANSZP_I8) return norm;
-    const float most = g.most;
+    if (p.out_dtype != ANSZP_I8) return {norm, false};
     const bool sound = g.poison == 0.0f;
-    if (writes) p.out_scales[row] = sound ? most * norm * (1.0f / 127.0f) : __builtin_nanf("");
-    return sound && most > 0.0f ? 127.0f / most : 0.0f;
+    float scale = g.most * norm * (1.0f / 127.0f), factor = sound && g.most > 0.0f ? 127.0f / g.most : 0.0f;
+    const bool tiny = sound && g.most < 1.0f && fminf(scale, g.most) < 0x1p-100f;
+    if (tiny) {
+        scale = g.most * kLift * norm * (1.0f / 127.0f) * (1.0f / kLift);
+        factor = scale > 0.0f ? norm / (scale * kLift) : 0.0f;
+    }
+    if (writes) p.out_scales[row] = sound ? scale : __builtin_nanf("");
+    return {factor, tiny};
 }
 
 // Rows of at most 8 * NV * THREADS elements.  Workgroups of several wavefronts have a row, or (THREADS = 64) each wavefront has one.
@@ -128,7 +144,7 @@ __global__ __launch_bounds__(THREADS == 64u ? 256u : THREADS) void rms_norm_kern
         }
         if (p.total) store_eight(p.total, DTYPE, row * p.total_stride + at, there, h);
     }
-    const float factor = row_factor(p, over_row<THREADS>(mine), row, t == 0u);
+    const Factor factor = row_factor(p, over_row<THREADS>(mine), row, t == 0u);
     for (uint32_t v = 0; v < NV; ++v) {
         const uint32_t at = (v * THREADS + t) * 8u;
         if (at < p.cols) store_row_part(p, row, at, p.cols - at, g[v], factor);
@@ -141,7 +157,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormParams p) {
     const uint64_t row = uint64_t(blockIdx.y) * kAcross + blockIdx.x;
     if (row >= p.rows) return;
     Gathered mine = {0.0f, 0.0f, 0.0f};
-    float factor = 0.0f;
+    Factor factor = {0.0f, false};
     for (uint32_t pass = 0; pass < 2u; ++pass) {
         for (uint64_t from = threadIdx.x * 8u; from < p.cols; from += 8192u) {
             const uint32_t at = uint32_t(from), there = p.cols - at;

@@ -95,6 +95,33 @@ def test_no_rows():
     assert out.shape == (0, 64) and scales.shape == (0,) and total.shape == (0, 64)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [8, 100, 4096, 20000])
+def test_rows_near_the_least_numbers_in_eight_bits(cols, dtype):
+    """Down to the least number of binary32, where 127 / max|y| is more than 32 bits hold: the symbols are round(y / s) all the same."""
+    x, _, w = _inputs(7, cols, torch.float32)
+    sizes = torch.tensor([1e-36, 1e-37, 2e-38, 1e-39, 1e-41, 1e-43, 3e-45], dtype=torch.float64, device=DEV)
+    x = x.double() / x.double().abs().amax(-1, keepdim=True)
+    tiny = (x * sizes[:, None]).to(dtype)
+    plain = (P.wide(tiny), *B.quantise_rows(tiny), torch.zeros(7, dtype=torch.float64))
+    # the same by small weights behind rows of ordinary size
+    rows = x.to(dtype)
+    by = 1 / torch.sqrt((P.wide(rows) ** 2).mean(-1) + EPS)
+    normed = []
+    for size in sizes.tolist():
+        small = (w.double() * size).to(dtype)
+        q, s, _ = B.rms_norm(rows, small, EPS, out_dtype="i8")
+        normed.append((P.rms_norm(rows, small, EPS, None)[0], q, s, by * 2.0 ** -150))
+    for y, q, s, product in (plain, *normed):
+        most = y.abs().amax(-1)
+        # s is rounded to a multiple of 2^-149, and 127 of it may miss the row's largest by 127 halves of that; so is the product with a weight before
+        P.assert_within(s, most / 127, (most * SUM + product) / 127 + 2.0 ** -150)
+        bound = P.wide(s)[:, None] * (0.5 + 2.0 ** -12) + y.abs() * SUM + 127 * 2.0 ** -150
+        assert ((P.wide(q) * P.wide(s)[:, None] - y).abs() <= torch.maximum(bound, torch.where(P.wide(s) == 0, most, 0.0)[:, None])).all()
+        assert (q[s == 0] == 0).all() and (q >= -127).all()
+        assert ((q.cpu() > 0) <= (y > 0)).all() and ((q.cpu() < 0) <= (y < 0)).all()
+
+
 @pytest.mark.parametrize("rows,cols", [((1 << 26) + 3, 8), ((1 << 24) + 1, 1032)])
 def test_rows_beyond_one_dimension_of_a_launch(rows, cols):
     """More rows than 2^32 threads have: every row is written."""
