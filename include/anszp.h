@@ -415,7 +415,7 @@ int anszp_conv_fused(const anszp_conv_args_t* args, void* hip_stream);
 
 /* Root-mean-square norm with the residual's addition: h = x + residual, y = h * (mean(h^2) + eps)^(-1/2) * weight; out is y
  * rounded to its type, or with ANSZP_I8 round(y / s) with s = max|y| / 127 of the row in out_scales (0 for a row of zeros; a row
- * that holds an infinity or a NaN has NaN for a scale and zeros).  Sums in 32 bits, from h before it is rounded. */
+ * that holds an infinity or a NaN, or whose y does, has NaN for a scale and zeros).  Sums in 32 bits, from h before it is rounded: |h| below 2^63 / sqrt(cols). */
 typedef struct {
     const void* x;                /* [device] rows x cols of dtype                                   */
     const void* residual;         /* [device] the same, or NULL for none                             */

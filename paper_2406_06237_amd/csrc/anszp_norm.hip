@@ -98,12 +98,12 @@ __device__ __forceinline__ void store_row_part(const NormParams& p, uint64_t row
     }
 }
 
-// 8 bits: 127 / max|h * g|.  A row with an infinity or a NaN has no 8-bit form: its scale is NaN, its symbols 0.  Where the scale or
+// 8 bits: 127 / max|h * g|.  A row with an infinity or a NaN, in h * g or behind the norm, has no 8-bit form: its scale is NaN, its symbols 0.  Where the scale or
 // the largest h * g is near binary32's least numbers (below 2^-100), the symbols are y over the scale as it is stored, which may have few bits left.
 __device__ __forceinline__ Factor row_factor(const NormParams& p, const Gathered& g, uint64_t row, bool writes) {
     const float norm = p.normalise ? 1.0f / sqrtf(g.squares * p.inverse_cols + p.eps) : 1.0f;
     if (p.out_dtype != ANSZP_I8) return {norm, false};
-    const bool sound = g.poison == 0.0f;
+    const bool sound = g.poison == 0.0f && g.most * norm < __builtin_inff();
     float scale = g.most * norm * (1.0f / 127.0f), factor = sound && g.most > 0.0f ? 127.0f / g.most : 0.0f;
     const bool tiny = sound && g.most < 1.0f && fminf(scale, g.most) < 0x1p-100f;
     if (tiny) {

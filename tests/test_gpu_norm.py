@@ -137,3 +137,16 @@ def test_rows_beyond_one_dimension_of_a_launch(rows, cols):
         assert torch.equal(scales, by[:1].expand(rows))
     else:
         assert torch.equal(scales[:rows // 4096 * 4096].view(-1, 4096), by.expand(rows // 4096, 4096))
+
+
+@pytest.mark.parametrize("cols", [64, 4096, 20000])
+def test_rows_that_pass_the_largest_number_behind_the_norm(cols):
+    """Rows and weights are numbers, their product behind the norm is not: no scale, no symbols; one beside them has its own."""
+    x = torch.full((3, cols), 0.5, device=DEV)
+    x[1] = 2.0 ** -30
+    w = torch.full((cols,), 3e38, device=DEV)
+    q, s, _ = B.rms_norm(x, w, 1e-5, out_dtype="i8")
+    assert torch.isfinite(s).tolist() == [True, True, True] and (q == 127).all()
+    x[2, 1:] = 0                                                       # its norm is sqrt(cols) / 0.5
+    q, s, _ = B.rms_norm(x, w, 1e-5, out_dtype="i8")
+    assert torch.isnan(s).tolist() == [False, False, True] and (q[:2] == 127).all() and (q[2] == 0).all()
