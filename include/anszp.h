@@ -514,7 +514,8 @@ typedef struct {
     const int32_t* starts;        /* [device] n_seqs + 1, from 0 to n_tokens, never falling; what is out of range is
                                      clamped, as lengths are; queries of no sequence are left unwritten */
     uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for a page beyond the cache that a query would
-                                     have seen; its positions are not seen, [1] grows                 */
+                                     have seen; its positions are not seen, [1] grows; and for a length out of range of a
+                                     sequence with new tokens, which moves their positions, [1] grows by 1 */
     void*          workspace;     /* [device] anszp_attend_workspace_bytes, 16-byte aligned, in use until the call is done */
     uint64_t       workspace_bytes;
     uint64_t       n_tokens, n_seqs;                      /* each < 2^24, may be 0; more than a launch has threads for is E_RANGE, which n_tokens * group + 16 *

@@ -56,6 +56,7 @@ struct AttendParams {
 struct Tile {
     uint32_t seq, first_token, n_new, first_row, n_rows;    // n_rows 0: there is no such tile
     int32_t length;                                         // of the sequence
+    bool clamped;                                           // it was given as one that the page table, or the cache, has no room for
 };
 
 __device__ __forceinline__ void flag(const AttendParams& p) {
@@ -68,7 +69,7 @@ __device__ __forceinline__ void flag(const AttendParams& p) {
 // Sequences have ceil(n_new * group / rows) tiles each; every wavefront counts through them, 64 sequences at a time.
 __device__ Tile find_tile(const AttendParams& p, uint32_t tile, uint32_t rows) {
     const uint32_t lane = threadIdx.x & 63u;
-    Tile t = {0u, 0u, 0u, 0u, 0u, 0};
+    Tile t = {0u, 0u, 0u, 0u, 0u, 0, false};
     uint32_t before = 0u;
     for (uint32_t s0 = 0; s0 < p.n_seqs; s0 += 64u) {
         const uint32_t s = s0 + lane;
@@ -98,6 +99,7 @@ __device__ Tile find_tile(const AttendParams& p, uint32_t tile, uint32_t rows) {
             const int32_t given = p.lengths[t.seq];
             t.length = given < 0 ? 0 : given > most ? int32_t(most) : given;
             if (p.n_pages == 0u) t.length = 0;
+            t.clamped = t.length != given;
             return t;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
@@ -191,6 +193,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendParams p) {
     const uint32_t head = blockIdx.y, split = blockIdx.z;
     const Tile t = find_tile(p, blockIdx.x, kTileRows);
     if (t.n_rows == 0u) return;
+    if (t.clamped && t.first_row == 0u && head == 0u && split == 0u && threadIdx.x == 0u) flag(p);      // (once for a sequence)
     const int32_t seen = seen_by(p, t);
     const int32_t begin = int32_t(split * p.span), end = min(seen, begin + int32_t(p.span));
     const uint64_t part = (uint64_t(split) * p.n_tiles + blockIdx.x) * p.heads + head;
@@ -461,6 +464,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
     const uint32_t split = blockIdx.y;
     const Tile t = find_tile(p, tile, kRows);
     if (t.n_rows == 0u) return;
+    if (t.clamped && t.first_row == 0u && head == 0u && split == 0u && threadIdx.x == 0u) flag(p);
     const int32_t begin = int32_t(split * p.span), end = min(seen_by(p, t), begin + int32_t(p.span));
     const uint64_t part = (uint64_t(split) * p.n_tiles + tile) * p.heads + head;
     if (p.splits > 1u && begin >= end) {

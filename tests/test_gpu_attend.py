@@ -270,3 +270,19 @@ def test_later_tokens_of_any_size(dim, bits, by):
             seen = 210 - new + i + 1
             error[i] += seen * 2.0 ** -34 * 2 * scales[:seen].max() * (2 ** bits - 1)
         P.assert_within(got, plain, error + plain.abs() * 2.0 ** -24, (group, new))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_lengths_that_the_table_has_no_room_for(new):
+    """They count as what the table holds, or as 0, and the status says so."""
+    cache, q, table, lengths, starts = _case([64, 20], [new, min(new, 20)], 2, 2)
+    want = B.attend(q, cache, table, lengths, starts)
+    assert cache.status.tolist() == [0, 0]
+    lengths[0] = 65
+    assert torch.equal(B.attend(q, cache, table, lengths, starts), want)
+    assert cache.status[0].item() == B.ST_BAD_DESC and cache.status[1].item() == 1
+    cache.status.zero_()
+    lengths[1] = -1
+    got = B.attend(q, cache, table, lengths, starts)
+    assert torch.equal(got[:new], want[:new]) and (got[new:] == 0).all()
+    assert cache.status[0].item() == B.ST_BAD_DESC and cache.status[1].item() == 2
