@@ -845,6 +845,8 @@ CACHE_BITS, CACHE_HEAD_DIMS = (8, 4), (64, 128, 256)
 
 def _want(t, name: str, device, shape: tuple, *dtypes):
     """A tensor on `device` of the given shape (None: any size) and one of the dtypes, its last dimension contiguous; raises ValueError."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, but is on {t.device}")
     if t.dtype not in dtypes:

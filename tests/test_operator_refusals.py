@@ -243,3 +243,10 @@ def test_attention_of_more_threads_than_a_launch_has():
                         (dict(heads=1), dict(n_tokens=64, n_seqs=(1 << 24) - 1, group=1))):                      # 16
         a = _attend(cache=cache, **many)
         assert B.lib().anszp_attend(C.addressof(a), None) == E_RANGE, many
+
+
+def test_a_norm_without_a_weight_is_refused(calls):
+    function, operands = _operands()["norm"]
+    with pytest.raises(ValueError, match="weight"):
+        function(**{**operands, "weight": None})
+    assert calls == []
