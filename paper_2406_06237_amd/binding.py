@@ -858,6 +858,13 @@ def _want(t, name: str, device, shape: tuple, *dtypes):
     return t.data_ptr()
 
 
+def _word(n: int, name: str) -> int:
+    """A size that the library takes as a word of 32 bits (ctypes would cut a larger one to them); raises ValueError."""
+    if n >= 1 << 32:
+        raise ValueError(f"{name} must fit 32 bits, but is {n}")
+    return n
+
+
 def _out_type(torch, out_dtype: str, *others):
     if out_dtype not in ("f32", "bf16", *others):
         raise ValueError(f"out_dtype must be one of {('f32', 'bf16', *others)}, but is {out_dtype!r}")
@@ -887,7 +894,7 @@ def _norm(where: str, x, weight, eps: float, residual, total, out_dtype: str, no
     out = torch.empty((rows, cols), dtype=_out_type(torch, out_dtype, "i8"), device=dev)
     scales = torch.empty(rows, dtype=torch.float32, device=dev) if out_dtype == "i8" else None
     a.out, a.out_scales = out.data_ptr(), scales.data_ptr() if scales is not None else None
-    a.rows, a.cols, a.x_stride, a.out_stride = rows, cols, x.stride(0), cols
+    a.rows, a.cols, a.x_stride, a.out_stride = rows, _word(cols, "x's columns"), x.stride(0), cols
     a.dtype, a.out_dtype, a.normalise, a.eps = _CODE_OF[str(x.dtype)], _CODE_OF[str(out.dtype)], normalise, eps
     _enqueue(where, lib().anszp_rms_norm, dev, C.addressof(a))
     return out, scales, total
@@ -942,7 +949,7 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
         a.mul, a.mul_stride = _want(mul, "mul", dev, (rows, cols), out.dtype), mul.stride(0)
     if residual is not None:
         a.residual, a.residual_stride = _want(residual, "residual", dev, (rows, cols), out.dtype), residual.stride(0)
-    a.rows, a.cols, a.k, a.x_stride, a.weight_stride, a.out_stride = rows, cols, k, x.stride(0), weight.stride(0), out.stride(0)
+    a.rows, a.cols, a.k, a.x_stride, a.weight_stride, a.out_stride = rows, cols, _word(k, "x's columns"), x.stride(0), weight.stride(0), out.stride(0)
     a.x_dtype, a.out_dtype, a.zero_point, a.activation, a.scale = _CODE_OF[str(x.dtype)], _CODE_OF[str(out.dtype)], zero_point, FN_CODES[activation], scale
     L = lib()
     need = L.anszp_linear_workspace_bytes(C.addressof(a))
@@ -996,7 +1003,8 @@ def _cache_arg(torch, cache: KvCache, a=None) -> CacheArg:
     a.v_params = _want(cache.v_params, "the cache's v_params", dev, (pages, heads, page_size, 2), torch.float32)
     if not (k.is_contiguous() and cache.v.is_contiguous() and cache.k_params.is_contiguous() and cache.v_params.is_contiguous()):
         raise ValueError("a cache's tensors must be contiguous")
-    a.n_pages, a.page_size, a.heads, a.head_dim, a.bits = pages, page_size, heads, cache.head_dim, cache.bits
+    a.n_pages, a.page_size, a.heads, a.bits = pages, _word(page_size, "the cache's page"), _word(heads, "the cache's heads"), cache.bits
+    a.head_dim = _word(cache.head_dim, "the cache's head")
     return a
 
 
@@ -1066,7 +1074,7 @@ def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = N
         out = torch.empty(q.shape, dtype=_out_type(torch, out_dtype), device=dev)
     a.out = _want(out, "out", dev, tuple(q.shape), torch.float32, torch.bfloat16)
     a.status = _status_ptr(torch, cache)
-    a.n_tokens, a.n_seqs, a.table_width, a.group = q.shape[0], n_seqs, width, q.shape[1] // c.heads
+    a.n_tokens, a.n_seqs, a.table_width, a.group = q.shape[0], n_seqs, _word(width, "the page table's width"), _word(q.shape[1] // c.heads, "q's heads per head of the cache")
     a.q_token_stride, a.q_head_stride, a.out_token_stride, a.out_head_stride = q.stride(0), q.stride(1), out.stride(0), out.stride(1)
     a.out_dtype, a.scale = _CODE_OF[str(out.dtype)], c.head_dim ** -0.5 if scale is None else scale
     L = lib()

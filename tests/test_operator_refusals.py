@@ -250,3 +250,21 @@ def test_a_norm_without_a_weight_is_refused(calls):
     with pytest.raises(ValueError, match="weight"):
         function(**{**operands, "weight": None})
     assert calls == []
+
+
+def test_sizes_of_32_bits_and_more(calls):
+    """The library's sizes are words of 32 bits: a longer row, table or page is refused, not cut to what is left of its number.  (Tensors without memory: nothing here is read.)"""
+    on = lambda *shape, dtype=BF16: torch.empty(shape, dtype=dtype, device="meta")  # noqa: E731
+    long = (1 << 32) + 64
+    cache = B.KvCache(on(3, 2, 16, 64, dtype=torch.uint8), on(3, 2, 16, 2, dtype=torch.float32), on(3, 2, 16, 64, dtype=torch.uint8), on(3, 2, 16, 2, dtype=torch.float32))
+    tall = B.KvCache(on(1, 2, long, 64, dtype=torch.uint8), on(1, 2, long, 2, dtype=torch.float32), on(1, 2, long, 64, dtype=torch.uint8), on(1, 2, long, 2, dtype=torch.float32))
+    wide = B.KvCache(on(1, long, 16, 64, dtype=torch.uint8), on(1, long, 16, 2, dtype=torch.float32), on(1, long, 16, 64, dtype=torch.uint8), on(1, long, 16, 2, dtype=torch.float32))
+    ints = lambda *shape: on(*shape, dtype=torch.int32)  # noqa: E731
+    for call in (lambda: B.rms_norm(on(1, long), on(long)), lambda: B.quantise_rows(on(1, long)),
+                 lambda: B.linear(on(1, long), on(1, long)), lambda: B.linear(on(1, long, dtype=torch.int8), on(1, long, dtype=torch.uint8)),
+                 lambda: B.attend(on(1, 2, 64), cache, ints(1, long), ints(1), ints(2)), lambda: B.attend(on(1, 2 * long, 64), cache, ints(1, 1), ints(1), ints(2)),
+                 lambda: B.attend(on(1, 2, 64), tall, ints(1, 1), ints(1), ints(2)), lambda: B.attend(on(1, 2 * long, 64), wide, ints(1, 1), ints(1), ints(2)),
+                 lambda: B.cache_read(tall, on(1, dtype=torch.int64)), lambda: B.cache_write(wide, on(1, long, 64), on(1, long, 64), on(1, dtype=torch.int64))):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert calls == []
