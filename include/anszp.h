@@ -432,7 +432,7 @@ typedef struct {
     uint32_t    normalise;        /* 0: y = h (weight and eps are not read)                          */
     float       eps;
 } anszp_norm_args_t;
-/* Errors: E_NULL, E_RANGE, E_HIP. */
+/* Errors: E_NULL, E_RANGE (also for an output that meets an operand it may not), E_HIP. */
 int anszp_rms_norm(const anszp_norm_args_t* args, void* hip_stream);
 
 /* activations of anszp_linear */
@@ -467,7 +467,7 @@ typedef struct {
 } anszp_linear_args_t;
 /* [host only] Bytes of workspace with which a call is fastest (0: none); reads sizes only, no pointers. */
 uint64_t anszp_linear_workspace_bytes(const anszp_linear_args_t* args);
-/* Errors: E_NULL, E_RANGE (also for a workspace that is too small), E_HIP. */
+/* Errors: E_NULL, E_RANGE (also for a workspace that is too small, and for an output that meets an operand it may not), E_HIP. */
 int anszp_linear(const anszp_linear_args_t* args, void* hip_stream);
 
 /* A paged cache of keys and values in 8 or 4 bits.  A slot is a token's place: page * page_size + token in page.  A vector (one

@@ -763,6 +763,11 @@ extern "C" int anszp_linear(const anszp_linear_args_t* a, void* hip_stream) {
     if (rc) return rc;
     if (a->rows == 0 || a->cols == 0) return ANSZP_OK;
     if (!a->x || !a->weight || !a->out) return ANSZP_E_NULL;
+    const uint64_t size = a->out_dtype == ANSZP_OUT_BF16 ? 2u : 4u, width = a->cols * size;
+    const Rows out = {a->out, a->rows, a->out_stride * size, width};
+    if (meet(out, {p.x, p.rows, p.x_stride, p.k_bytes}) || meet(out, {p.w, p.cols, p.w_stride, p.k_bytes}) ||
+        meet_elsewhere(out, {a->mul, a->rows, a->mul_stride * size, width}) || meet_elsewhere(out, {a->residual, a->rows, a->residual_stride * size, width}))
+        return ANSZP_E_RANGE;
     const LinearPlan plan = plan_of(*a, p, a->workspace != nullptr);
     if (plan.workspace && (a->workspace_bytes < plan.workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u))) return ANSZP_E_RANGE;
     p.shares = plan.shares;

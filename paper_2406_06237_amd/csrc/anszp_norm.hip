@@ -209,6 +209,10 @@ extern "C" int anszp_rms_norm(const anszp_norm_args_t* a, void* hip_stream) {
     if (a->rows > 1 && (a->out_stride < a->cols || (a->total && a->total_stride < a->cols))) return ANSZP_E_RANGE;
     if (a->rows == 0) return ANSZP_OK;
     if (!a->x || !a->out || (a->normalise && !a->weight) || (eight_bits && !a->out_scales)) return ANSZP_E_NULL;
+    const uint64_t size = a->dtype == ANSZP_OUT_BF16 ? 2u : 4u, out_size = eight_bits ? 1u : a->out_dtype == ANSZP_OUT_BF16 ? 2u : 4u, width = a->cols * size;
+    const Rows out = {a->out, a->rows, a->out_stride * out_size, a->cols * out_size}, total = {a->total, a->rows, a->total_stride * size, width};
+    const Rows x = {a->x, a->rows, a->x_stride * size, width}, residual = {a->residual, a->rows, a->residual_stride * size, width};
+    if (meet(out, x) || meet(out, residual) || meet(out, total) || meet_elsewhere(total, x) || meet_elsewhere(total, residual)) return ANSZP_E_RANGE;
     NormParams p = {a->x, a->residual, a->total, a->weight, a->out, a->out_scales, a->rows, a->x_stride, a->residual_stride, a->total_stride, a->out_stride,
                     a->cols, a->out_dtype, a->weight_dtype, a->normalise ? 1u : 0u, a->eps, 1.0f / static_cast<float>(a->cols)};
     if (a->dtype == ANSZP_OUT_F32) launch<ANSZP_OUT_F32>(p, static_cast<hipStream_t>(hip_stream));

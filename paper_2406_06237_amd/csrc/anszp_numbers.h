@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "anszp.h"
 
@@ -93,6 +94,27 @@ __device__ __forceinline__ void store_eight(void* base, uint32_t dtype, uint64_t
 constexpr uint32_t kAcross = 1u << 21;
 inline uint32_t groups_across(uint64_t groups) { return static_cast<uint32_t>(groups < kAcross ? groups : kAcross); }
 inline uint32_t groups_down(uint64_t groups) { return static_cast<uint32_t>((groups + kAcross - 1u) / kAcross); }
+
+// Rows of an operand, in bytes.
+struct Rows {
+    const void* at;
+    uint64_t rows, stride, width;
+};
+// Whether two operands surely have memory in common.  (Rows of one may lie between the other's, as columns of one buffer do.  Of rows of two strides the first ones
+// are looked at.)
+inline bool meet(Rows a, Rows b) {
+    if (!a.at || !b.at || a.rows == 0u || b.rows == 0u) return false;
+    if (reinterpret_cast<uintptr_t>(b.at) < reinterpret_cast<uintptr_t>(a.at)) std::swap(a, b);
+    if (a.rows == 1u) a.stride = a.width;
+    if (b.rows == 1u) b.stride = b.width;
+    const uint64_t apart = reinterpret_cast<uintptr_t>(b.at) - reinterpret_cast<uintptr_t>(a.at);
+    if (apart >= (a.rows - 1u) * a.stride + a.width) return false;
+    if (a.stride <= a.width) return true;
+    const uint64_t row = apart / a.stride, behind = apart % a.stride, run = b.stride <= b.width ? (b.rows - 1u) * b.stride + b.width : b.width;
+    return behind < a.width || (behind + run > a.stride && row + 1u < a.rows);
+}
+// ... though an output may be the operand itself, row for row.
+inline bool meet_elsewhere(const Rows& out, const Rows& in) { return !(out.at == in.at && (out.rows <= 1u || out.stride == in.stride)) && meet(out, in); }
 
 __device__ __forceinline__ uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
 

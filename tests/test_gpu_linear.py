@@ -145,3 +145,23 @@ def test_channels_beyond_one_dimension_of_a_launch(k):
     want, error = P.linear(x, w)
     P.assert_within(out[:, :1], want, error + want.abs() * P.HALF_ULP[torch.bfloat16])
     assert (out == out[0, 0]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 40, 600])
+def test_columns_of_one_buffer(rows):
+    """Operands and output between each other's rows; an output over its operands is refused."""
+    k, cols = 64, 72
+    buffer = torch.randn(rows, k + 2 * cols, device=DEV).to(torch.bfloat16)
+    w = torch.randn(cols, k, device=DEV).to(torch.bfloat16)
+    x, out, residual = buffer[:, :k], buffer[:, k:k + cols], buffer[:, k + cols:]
+    want = B.linear(x.clone(), w, residual=residual.clone())
+    B.linear(x, w, residual=residual, out=out)
+    assert torch.equal(out, want)
+    for over in (buffer[:, k - 1:k - 1 + cols], buffer[:, k + cols - 8:k + 2 * cols - 8]):
+        with pytest.raises(B.AnszpError, match="out of range"):
+            B.linear(x, w, residual=residual, out=over)
+    square = buffer[:, :k].contiguous()
+    with pytest.raises(B.AnszpError, match="out of range"):
+        B.linear(square, w[:k], out=square)
+    with pytest.raises(B.AnszpError, match="out of range"):
+        B.rms_norm(x, w[0], residual=residual[:, :k], total=buffer[:, 1:k + 1])

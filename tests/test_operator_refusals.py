@@ -268,3 +268,22 @@ def test_sizes_of_32_bits_and_more(calls):
         with pytest.raises(ValueError, match="32 bits"):
             call()
     assert calls == []
+
+
+FAR = 1 << 30                                          # so far behind PTR that nothing meets
+
+
+@pytest.mark.parametrize("change", [
+    dict(x=PTR), dict(weight=PTR), dict(x=PTR + 4 * 128 - 1), dict(x=PTR - 4 * 64 + 1), dict(weight=PTR + 2), dict(weight=PTR - 64 * 64 + 2),
+    dict(mul=PTR + 2, mul_stride=64), dict(residual=PTR + 128, residual_stride=64), dict(residual=PTR, residual_stride=80, out_stride=64),
+    dict(out_stride=128, residual=PTR + 100, residual_stride=128), dict(out_stride=128, x=PTR + 256 + 127, x_stride=256), dict(rows=1, x=PTR + 60), dict(cols=1, out_stride=1, weight=PTR + 6)])
+def test_products_over_their_operands(change):
+    """An output that meets x or the weights, or mul or the residual elsewhere than row for row."""
+    assert _linear(**{**dict(x=PTR + FAR, weight=PTR + 2 * FAR), **change}) == E_RANGE
+
+
+@pytest.mark.parametrize("change", [
+    dict(out=PTR), dict(out=PTR + 100), dict(residual=PTR + 3 * FAR, residual_stride=64, out=PTR + 3 * FAR + 511), dict(total=PTR + FAR, total_stride=64),
+    dict(total=PTR + 2, total_stride=64), dict(total=PTR, total_stride=70), dict(residual=PTR + 3 * FAR, residual_stride=64, total=PTR + 3 * FAR + 128, total_stride=64)])
+def test_norms_over_their_operands(change):
+    assert _norm(**{**dict(out=PTR + FAR, weight=PTR + 2 * FAR, out_scales=PTR + 4 * FAR), **change}) == E_RANGE
