@@ -385,7 +385,7 @@ typedef struct {
     uint32_t             y_dtype;        /* ANSZP_OUT_F32, or ANSZP_OUT_BF16 (the fp32 result rounded
                                             to nearest even)                                      */
     uint32_t             x_layout;       /* ANSZP_ACT_*; ANSZP_ACT_C8 needs cin to be a multiple of 8 */
-    uint32_t             y_layout;       /* ANSZP_FN_*                                           */
+    uint32_t             y_layout;       /* ANSZP_ACT_*                                            */
     uint32_t*            status;         /* [device] 2 words, as for anszp_decode                 */
 } anszp_conv_args_t;
 
