@@ -286,3 +286,29 @@ def test_lengths_that_the_table_has_no_room_for(new):
     got = B.attend(q, cache, table, lengths, starts)
     assert torch.equal(got[:new], want[:new]) and (got[new:] == 0).all()
     assert cache.status[0].item() == B.ST_BAD_DESC and cache.status[1].item() == 2
+
+
+def test_weights_of_a_peaked_softmax_in_chunks():
+    """Of many rows, too: one token with nearly all the weight and no value to speak of, so that the small weights make the result."""
+    case = _case([400], [130], 1, 1, 64, 16)
+    cache, q, table = case[0], case[1], case[2]
+    q[:] = q[0]
+    sink = (int(table[0, 0]), 0, 0)
+    cache.k_params[..., 0] *= 0.05
+    cache.k[sink] = torch.where(q[0, 0] > 0, 255, 0).to(torch.uint8)
+    cache.k_params[sink] = torch.tensor([0.02, 128.0], device=DEV)
+    cache.v_params[sink] = torch.tensor([0.0, 0.0], device=DEV)
+    _check(case, "f32", scale=0.05)
+
+
+@pytest.mark.parametrize("by", [4.0, 0.25, 16.0])
+@pytest.mark.parametrize("dim,bits", WIDTHS)
+def test_value_scales_that_rise_and_fall_in_chunks(dim, bits, by):
+    """By a factor every 64 tokens, so that what a row has seen is passed in most steps, and in the last ones by tokens that some rows do not see."""
+    lengths, news = [500, 333], [100, 160]
+    case = _case(lengths, news, 1, 2, dim, 32, bits)
+    cache, table = case[0], case[2]
+    for s, n in enumerate(lengths):
+        at = torch.arange(n, device=DEV)
+        cache.v_params[table[s, at // 32].long(), 0, at % 32, 0] *= by ** (at // 64).float()
+    _check(case, "f32", what=by)
