@@ -442,10 +442,10 @@ __device__ __forceinline__ void loads_ahead() {
 // operands once for all wavefronts: each thread turns some of the next step's bytes, which it asked for a step ahead, into fp16 in LDS while
 // others still multiply, keys [token][dimension], values [dimension][token] with the eight tokens that a lane feeds (4 g .. 4 g + 3 of both halves of
 // 32) side by side.  Otherwise as above.  Heads of 64 and 128 have four wavefronts of 32 rows, two such workgroups a CU; eight wavefronts of 32 halve
-// what a row costs in staging, but all of a CU's wait for one barrier (16 sequences of 2048 tokens: 615 TFLOP/s rather than 693).  Heads of 256 leave room
-// for 16 rows a wavefront and need the eight: two chunks of 700 tokens 84 us rather than 97.
-// Sixteen sequences of 2048 new tokens behind up to 2048 more, 32 heads over 8 of 128, take 1690 us, 800 TFLOP/s (a large product 1330 to 1530): the
-// vector unit is at work for 52 % of the time, the matrix units for 26.
+// what a row costs in staging, but all of a CU's wait for one barrier (16 sequences of 2048 tokens: 0.89 of the rate).  Heads of 256 leave room
+// for 16 rows a wavefront and need the eight: two chunks of 700 tokens 78 us rather than 102 with four of 32.
+// Sixteen sequences of 2048 new tokens behind up to 2048 more, 32 heads over 8 of 128, take 1740 us, 775 TFLOP/s (a large product 1330 to 1530): the
+// vector unit is at work for 60 % of the time, the matrix units for 33.
 template <uint32_t D, uint32_t BITS, uint32_t T, uint32_t RT, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParams p) {
     static_assert(T == 64u, "a lane looks at one token of a step");
@@ -720,7 +720,7 @@ __global__ __launch_bounds__(WAVES * 64u, 2) void attend_tile_kernel(AttendParam
 #pragma unroll
                 for (uint32_t b = 0; b < RT; ++b) acc[e][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, weights[b]), acc[e][b], 0, 0, 0);
             }
-            if constexpr (kTiles > 4u) loads_ahead<kTiles, RT, 0>();                    // (of four tiles all loads would be ahead: 84 us rather than 79)
+            loads_ahead<kTiles, RT, 0>();
         }
     };
     const int32_t steps = (max(0, end - begin) + int32_t(T) - 1) / int32_t(T);
@@ -834,18 +834,21 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
 
 // Above so many rows per sequence and head of the cache, on average, attend_tile_kernel is the faster one: it reads tokens once for 128 rows, not 16, but
 // vectors of few bytes are no work for attend_rows_kernel.  16 sequences of 2000 to 4000 tokens, 8 heads, few rows' kernel and many rows', us:
-//   128 x 8 bits: 16 rows 42 and 57, 32 rows 59 and 61, 48 rows 70 and 64, 128 rows 138 and 96
-//   256 x 8 bits: 16 rows 62 and 84, 32 rows 88 and 88, 48 rows 110 and 92
-//   64 x 8 bits:  32 rows 38 and 50, 64 rows 52 and 66, 128 rows 83 and 79
-//   128 x 4 bits: 32 rows 44 and 60, 64 rows 64 and 80, 128 rows 104 and 94
+//   128 x 8 bits: 16 rows 42 and 61, 32 rows 58 and 63, 48 rows 69 and 67, 128 rows 131 and 100
+//   256 x 8 bits: 16 rows 61 and 85, 32 rows 89 and 89, 48 rows 107 and 93
+//   64 x 8 bits:  32 rows 37 and 52, 64 rows 50 and 68, 128 rows 81 and 81
+//   128 x 4 bits: 32 rows 44 and 64, 64 rows 60 and 85, 128 rows 97 and 97
+// (An average: single tokens beside a chunk take the chunk's kernel.  32 of them behind 18500 to 65000 tokens, 8 heads of four queries, take 578 us, a chunk of 1531
+// 92, both in one call 1974.)
 uint64_t few_rows_of(const anszp_cache_t& c) { return c.head_dim * c.bits / 8u <= 64u ? 96u : 32u; }
 
 // How the tokens are shared out: enough workgroups to fill the chip, of at least 256 tokens each; and where there are more than that, shares of a
 // length, since sequences differ in theirs and the longest would end last.  A share costs its workgroup's start and its part of the join, so many workgroups
 // have longer ones (us, with a share for 1408 and for 2816 tokens):
-//   48 sequences of 17 to 4100 tokens, 32 heads in 4 bits 131 and 127 (184 with one workgroup for all of a sequence's tokens), in 8 bits 184 and 181;
-//   200 of 10 to 2000, 8 heads in 4 bits 85 and 74;    64 of 100 to 4000, 8 heads of four queries in 8 bits 81 and 87;    16, 32 heads in 4 bits 51 and 54.
-// The lengths are on the device: what the page tables can hold counts.
+//   48 sequences of 17 to 4100 tokens, 32 heads in 4 bits 123 and 120 (123 with one workgroup for all of a sequence's tokens), in 8 bits 180 and 180 (190 with one);
+//   200 of 10 to 2000, 8 heads in 4 bits 73.5 and 62.7;    64 of 100 to 4000, 8 heads of four queries in 8 bits 69 and 76;    16, 32 heads in 4 bits 44 and 46.6.
+// The lengths are on the device: what the page tables can hold counts, and a table wider than its sequences makes longer shares (8 heads of four queries, a table
+// for 4000 tokens and one for 65500: one sequence of 4000 tokens 11 and 16.5 us, four 20 and 22, 64 of 100 to 4000 69 and 82).
 struct Shares {
     uint32_t rows, tiles, splits, span;     // rows of a tile: attend_rows_kernel's, or attend_tile_kernel's
 };
