@@ -504,7 +504,8 @@ int anszp_cache_read(const anszp_cache_t* cache, void* k, void* v, uint32_t dtyp
  *   out = sum_t softmax_t(scale * q . k_t) v_t        a query that sees nothing (a position below 0): zeros
  * Query head h reads the cache's head h / group.  Position t of sequence s is in page pages[s * table_width + t / page_size].
  * Sums and statistics in fp32; queries go into the matrix instructions in fp16 scaled by a power of two per row, keys and values
- * exactly, weights in fp16 with a scale that keeps 11 bits of each down to 2^-23 of the largest. */
+ * exactly, weights in fp16 with a scale that keeps 11 bits of each (with F32 output too) down to 2^-23 of the largest that the query sees.
+ * Sums are held at up to 2^15 times a value for each token: values below 2^113 / length in size. */
 typedef struct {
     anszp_cache_t  cache;
     const void*    q;             /* [device] n_tokens x (heads * group) x head_dim, bf16            */

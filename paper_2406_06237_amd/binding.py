@@ -835,6 +835,7 @@ def pack_layers_device(symbols_dev, layer_sizes: Sequence[int], freqs_dev, table
 
 
 # --------------------------------------------------------------------------- operators that run decoded layers as a model
+# (Weights arrive frozen: no call has a gradient, and operands that ask for one get none.)
 I8 = 3
 _CODE_OF = {"torch.float32": OUT_F32, "torch.bfloat16": OUT_BF16, "torch.int8": I8}
 _FLOATS = {"f32": OUT_F32, "bf16": OUT_BF16}
@@ -918,7 +919,7 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
     """anszp_linear on torch's current stream: act(scale * x_scales[r] * channel_scales[c] * (x @ w^T) + bias) * mul + residual.
     x [rows, k] and weight [cols, k] in bf16, or x int8 and weight uint8 symbols, w = symbol - zero_point; x_scales [rows],
     channel_scales and bias [cols] fp32; mul and residual [rows, cols] of the output's type.  activation: "none", "relu",
-    "gelu" or "silu".  Returns out (which may be mul or residual itself)."""
+    "gelu" or "silu".  Returns out (which may be mul or residual itself, row for row, and may not meet them otherwise, x or weight)."""
     torch = _torch()
     dev = x.device
     if out_dtype in _FLOATS and activation in FN_CODES:
@@ -1050,7 +1051,9 @@ def cache_read(cache: KvCache, slots, out_dtype: str = "bf16"):
 def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = None, out_dtype: str = "bf16", out=None):
     """anszp_attend on torch's current stream: q [tokens, heads * group, head_dim] bf16, the new tokens of all sequences one sequence
     behind the other, their keys and values in the cache already; pages [sequences, width] int32, lengths [sequences] int32 (new tokens
-    included), starts [sequences + 1] int32.  scale: 1 / sqrt(head_dim) if not given.  Returns out, q's shape."""
+    included), starts [sequences + 1] int32.  scale: 1 / sqrt(head_dim) if not given.  Returns out, q's shape; rows of no sequence keep what was in
+    `out`, or in a new one's memory.  A page, or a length of a sequence with new tokens, that is not there is told by the cache's status.  Long chunks and
+    single tokens are faster in a call each: one call takes one kernel for all."""
     torch = _torch()
     dev = q.device
     if out_dtype in _FLOATS:

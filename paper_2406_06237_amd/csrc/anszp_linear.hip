@@ -386,7 +386,8 @@ bool launch_few(const LinearParams& p, hipStream_t s) {
 // piece of neighbouring rows meet all 64 banks.
 // DIRECT: rows begin at multiples of 16 bytes, and steps go from memory to LDS without passing through registers; a wavefront's load fills 8
 // rows end to end, each lane asking for the piece that belongs where its 16 bytes land.  Otherwise, and for what is left of k behind the last
-// whole step, pieces are loaded to registers, with zeros behind the end of a row.
+// whole step, pieces are loaded to registers, with zeros behind the end of a row.  256 x 256 tiles have too few for that (42 spill in 8 bits, 18 in bf16):
+// 8192 x 4096 x 4096 takes 252 us in bf16 and 148 in 8 bits, with k of 4095 289 and 225.
 typedef __attribute__((ext_vector_type(16))) float floatx16;
 typedef __attribute__((ext_vector_type(16))) int32_t intx16;
 template <bool BYTES>

@@ -1,7 +1,8 @@
 // Which kernel a matrix product takes, and whether k goes in shares (internal to the library; host only, no HIP).
 //
 // A call is estimated for each kernel and the least estimate taken.  The estimates are fits of what calls of 1 to 8192 rows with 128 to 11008
-// channels and k from 300 to 11008 took on an MI355X, in ns, and meet those within a fifth mostly:
+// channels and k from 300 to 11008 took on an MI355X, in ns, and meet those within a fifth mostly (not where more small tiles are than find
+// place, four a CU, and a few are left for a second round, nor where rows begin off multiples of 16 bytes):
 //   few rows       a CU takes in about 33 bytes a ns of rows of weights and activations (each as often as tiles need it), one workgroup
 //                  after the other: 16 x 4096 x 11008 in bf16 22 us;
 //   tiles          a step of 128 bytes of k takes at least `alone`, and `each` for every workgroup a CU has at a time (bf16, 8 bits): small tiles fill
