@@ -509,7 +509,7 @@ int anszp_cache_read(const anszp_cache_t* cache, void* k, void* v, uint32_t dtyp
 typedef struct {
     anszp_cache_t  cache;
     const void*    q;             /* [device] n_tokens x (heads * group) x head_dim, bf16            */
-    void*          out;           /* [device] the same shape, of out_dtype, contiguous in head_dim   */
+    void*          out;           /* [device] the same shape, of out_dtype, contiguous in head_dim, rows apart */
     const int32_t* pages;         /* [device] n_seqs x table_width                                   */
     const int32_t* lengths;       /* [device] n_seqs, 0 .. table_width * page_size                   */
     const int32_t* starts;        /* [device] n_seqs + 1, from 0 to n_tokens, never falling; what is out of range is

@@ -918,6 +918,7 @@ int anszp_attend(const anszp_attend_args_t* a, void* hip_stream) {
     if (!in_range(*a)) return ANSZP_E_RANGE;
     if (a->n_tokens == 0u || a->n_seqs == 0u) return ANSZP_OK;
     if (!a->q || !a->out || !a->pages || !a->lengths || !a->starts) return ANSZP_E_NULL;
+    if ((a->n_tokens > 1u && a->out_token_stride < a->cache.head_dim) || (a->cache.heads * a->group > 1u && a->out_head_stride < a->cache.head_dim)) return ANSZP_E_RANGE;
     const Shares s = shares_of(*a);
     if (!fits_a_launch(*a, s)) return ANSZP_E_RANGE;
     const uint64_t need = workspace_of(*a, s);

@@ -287,3 +287,10 @@ def test_products_over_their_operands(change):
     dict(total=PTR + 2, total_stride=64), dict(total=PTR, total_stride=70), dict(residual=PTR + 3 * FAR, residual_stride=64, total=PTR + 3 * FAR + 128, total_stride=64)])
 def test_norms_over_their_operands(change):
     assert _norm(**{**dict(out=PTR + FAR, weight=PTR + 2 * FAR, out_scales=PTR + 4 * FAR), **change}) == E_RANGE
+
+
+@pytest.mark.parametrize("change", [dict(n_tokens=2, out_token_stride=0), dict(n_tokens=2, out_token_stride=63), dict(out_head_stride=0), dict(out_head_stride=63),
+                                    dict(group=2, cache=dict(heads=1), out_head_stride=0)])
+def test_attention_into_rows_over_each_other(change):
+    """Rows of the output that share memory would hold one query's result or another's."""
+    assert B.lib().anszp_attend(C.addressof(_attend(**change)), None) == E_RANGE
