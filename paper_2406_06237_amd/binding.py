@@ -918,7 +918,7 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
            mul=None, residual=None, out_dtype: str = "bf16", out=None):
     """anszp_linear on torch's current stream: act(scale * x_scales[r] * channel_scales[c] * (x @ w^T) + bias) * mul + residual.
     x [rows, k] and weight [cols, k] in bf16, or x int8 and weight uint8 symbols, w = symbol - zero_point; x_scales [rows],
-    channel_scales and bias [cols] fp32; mul and residual [rows, cols] of the output's type.  activation: "none", "relu",
+    channel_scales and bias [cols] fp32; mul and residual [rows, cols] of the output's type (out's own, if it is given).  activation: "none", "relu",
     "gelu" or "silu".  Returns out (which may be mul or residual itself, row for row, and may not meet them otherwise, x or weight)."""
     torch = _torch()
     dev = x.device
@@ -937,8 +937,9 @@ def linear(x, weight, x_scales=None, zero_point: int = 0, scale: float = 1.0, ch
         raise ValueError(f"activation must be one of {tuple(FN_CODES)}, but is {activation!r}")
     if not 0 <= zero_point <= 255 or (zero_point and x.dtype != torch.int8):
         raise ValueError("zero_point is the symbols' own: 0 to 255, and 0 for weights in bf16")
+    out_type = _out_type(torch, out_dtype)
     if out is None:
-        out = torch.empty((rows, cols), dtype=_out_type(torch, out_dtype), device=dev)
+        out = torch.empty((rows, cols), dtype=out_type, device=dev)
     a.out = _want(out, "out", dev, (rows, cols), torch.float32, torch.bfloat16)
     if x_scales is not None:
         a.x_scales = _want(x_scales, "x_scales", dev, (rows,), torch.float32)
@@ -1073,8 +1074,9 @@ def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = N
         raise ValueError("pages must be contiguous")
     a.lengths = _want(lengths, "lengths", dev, (n_seqs,), torch.int32)
     a.starts = _want(starts, "starts", dev, (n_seqs + 1,), torch.int32)
+    out_type = _out_type(torch, out_dtype)
     if out is None:
-        out = torch.empty(q.shape, dtype=_out_type(torch, out_dtype), device=dev)
+        out = torch.empty(q.shape, dtype=out_type, device=dev)
     a.out = _want(out, "out", dev, tuple(q.shape), torch.float32, torch.bfloat16)
     a.status = _status_ptr(torch, cache)
     a.n_tokens, a.n_seqs, a.table_width, a.group = q.shape[0], n_seqs, _word(width, "the page table's width"), _word(q.shape[1] // c.heads, "q's heads per head of the cache")

@@ -294,3 +294,13 @@ def test_norms_over_their_operands(change):
 def test_attention_into_rows_over_each_other(change):
     """Rows of the output that share memory would hold one query's result or another's."""
     assert B.lib().anszp_attend(C.addressof(_attend(**change)), None) == E_RANGE
+
+
+@pytest.mark.parametrize("which,out", [("linear", torch.zeros(3, 32, dtype=BF16)), ("attend", torch.zeros(4, 6, 64, dtype=BF16))])
+def test_a_type_that_is_none_beside_an_output(calls, which, out):
+    """The output's own type counts, and a name that is no type's is refused all the same."""
+    function, operands = _operands()[which]
+    for name in ("i8", "fp8", None):
+        with pytest.raises(ValueError, match="out_dtype"):
+            function(**{**operands, "out": out, "out_dtype": name})
+    assert calls == []
