@@ -532,6 +532,123 @@ uint64_t anszp_attend_workspace_bytes(const anszp_attend_args_t* args);
 /* Errors: E_NULL, E_RANGE (also for a workspace that is too small), E_HIP. */
 int anszp_attend(const anszp_attend_args_t* args, void* hip_stream);
 
+/* ---- a serving step around them: tokens placed in the cache, looked up, adapted to their requests, drawn ----
+ * The conventions are those of the operators above. */
+
+/* New tokens placed in a paged cache.  Sequence s holds lengths[s] tokens in the pages of its row of the table, and gets new_tokens[s].
+ * Free pages are a stack, free_pages[0 .. n_free - 1]; P is the page's size.
+ *   old = 0 where ends[s], whose ceil(lengths[s] / P) pages go on the stack, sequence by sequence in their order, else lengths[s];
+ *   need = ceil((old + new) / P) - ceil(old / P) pages are taken from the stack's end, in the sequences' order, and written to the table.
+ * A sequence gets nothing (its length stays, its slots are -1) where the stack has not as many pages as it and those before it need, or
+ * new_tokens[s] is negative or more than its row of the table or n_tokens has room for; lengths out of range are treated alike (those of a
+ * sequence that ends are clamped).  Apart from lengths_out, n_free_out, the table's entries behind the pages that a sequence holds and the
+ * stack's behind n_free nothing is changed, so a call may be made again. */
+typedef struct {
+    int32_t*       pages;         /* [device] n_seqs x table_width                                   */
+    const int32_t* lengths;       /* [device] n_seqs, 0 .. table_width * page_size                   */
+    int32_t*       lengths_out;   /* [device] n_seqs: old + new; may be lengths                      */
+    const int32_t* new_tokens;    /* [device] n_seqs                                                 */
+    const int32_t* ends;          /* [device] n_seqs, 0: goes on; or NULL: all do                    */
+    int32_t*       free_pages;    /* [device] free_room                                              */
+    const int32_t* n_free;        /* [device] one number, 0 .. free_room                             */
+    int32_t*       n_free_out;    /* [device] one number; may be n_free                              */
+    int64_t*       slots;         /* [device] n_tokens: the new tokens' slots, one sequence behind the other; -1 behind the last */
+    int32_t*       owners;        /* [device] n_tokens: the sequence each is of, -1 behind the last; or NULL */
+    int32_t*       starts;        /* [device] n_seqs + 1: as anszp_attend takes them                 */
+    uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for a sequence that gets nothing though it asks, numbers out of
+                                     range, a page below 0, pages that overflow the stack; [1] grows */
+    void*          workspace;     /* [device] anszp_place_workspace_bytes, 16-byte aligned, in use until the call is done */
+    uint64_t       workspace_bytes;
+    uint64_t       n_seqs, n_tokens, free_room;           /* < 2^24, < 2^31, < 2^31; may be 0        */
+    uint32_t       table_width;   /* >= 1; table_width * page_size <= 2^30                           */
+    uint32_t       page_size;     /* a power of two from 16 to 65536                                 */
+} anszp_place_args_t;
+/* [host only] Bytes of workspace a call takes; reads sizes only, no pointers. */
+uint64_t anszp_place_workspace_bytes(const anszp_place_args_t* args);
+/* Errors: E_NULL, E_RANGE (also for a workspace that is too small, and for an output that meets another operand), E_HIP. */
+int anszp_place(const anszp_place_args_t* args, void* hip_stream);
+
+/* Tokens looked up: out[t] = scale * row_scales[id] * (weight[id] - zero_point), id = tokens[t], with weights as symbols (Sec. II-B), or
+ * scale * weight[id] with weights in bf16.  Zeros for a token below 0, and for one beyond the vocabulary (ANSZP_ST_BAD_DESC, counted). */
+typedef struct {
+    const int64_t* tokens;        /* [device] n_tokens                                               */
+    const void*    weight;        /* [device] vocabulary x cols: symbols, or bf16                    */
+    const float*   row_scales;    /* [device] vocabulary, or NULL; with symbols only                 */
+    void*          out;           /* [device] n_tokens x cols of out_dtype, apart from the inputs    */
+    uint32_t*      status;        /* [device] 2 words, or NULL                                       */
+    uint64_t       n_tokens, vocabulary;                  /* each < 2^31, may be 0                   */
+    uint64_t       weight_stride, out_stride;
+    uint32_t       cols;          /* 1 .. 2^31 - 1                                                   */
+    uint32_t       weight_dtype;  /* ANSZP_OUT_U8 (symbols) or ANSZP_OUT_BF16                        */
+    uint32_t       zero_point;    /* 0 .. 255; with symbols only                                     */
+    uint32_t       out_dtype;     /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    float          scale;
+} anszp_embed_args_t;
+/* Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_embed(const anszp_embed_args_t* args, void* hip_stream);
+
+/* Low-rank adapters beside a product: with i = ids[r] the adapter of row r,
+ *   out = act(base + scales[i] * x_scales[r] * (x[r] a[i]^T) b[i]^T) * mul + residual
+ * and without the middle term for a row that has none.  base is what anszp_linear gives without its epilogue.  Sums in fp32; what lies between the
+ * two products is held to 2^-18 for bf16 outputs, in all its 24 bits for fp32 ones.  A row's result depends on its own adapter alone; where
+ * that or x holds an infinity or a NaN, it has infinities or NaN. */
+typedef struct {
+    const void*    x;             /* [device] rows x k of x_dtype                                    */
+    const void*    a;             /* [device] adapters x rank x k, bf16                              */
+    const void*    b;             /* [device] adapters x cols x rank, bf16                           */
+    const int32_t* ids;           /* [device] rows; below 0: no adapter                              */
+    const float*   x_scales;      /* [device] rows, or NULL                                          */
+    const float*   scales;        /* [device] adapters, or NULL                                      */
+    const void*    base;          /* [device] rows x cols of base_dtype                              */
+    const void*    mul;           /* [device] rows x cols of out_dtype, or NULL                      */
+    const void*    residual;      /* [device] rows x cols of out_dtype, or NULL                      */
+    void*          out;           /* [device] rows x cols of out_dtype; may be base (of the same type), mul or residual (same stride), apart from the rest */
+    uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for an id beyond the adapters, whose row has none then, counted */
+    void*          workspace;     /* [device] anszp_adapt_workspace_bytes, 16-byte aligned, in use until the call is done */
+    uint64_t       workspace_bytes;
+    uint64_t       rows, cols;    /* < 2^28, < 2^31, may be 0; fewer than 2^24 tiles of 16 x 256 together */
+    uint64_t       x_stride, a_stride, a_row_stride, b_stride, b_row_stride, base_stride, mul_stride, residual_stride, out_stride;
+    uint32_t       adapters;      /* < 2^24, may be 0                                                */
+    uint32_t       k;             /* 1 .. 2^30                                                       */
+    uint32_t       rank;          /* 1 .. 256                                                        */
+    uint32_t       x_dtype;       /* ANSZP_OUT_BF16 or ANSZP_I8                                      */
+    uint32_t       base_dtype;    /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    uint32_t       out_dtype;     /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    uint32_t       activation;    /* ANSZP_FN_*                                                      */
+} anszp_adapt_args_t;
+/* [host only] Bytes of workspace a call takes (0: none); reads sizes only, no pointers. */
+uint64_t anszp_adapt_workspace_bytes(const anszp_adapt_args_t* args);
+/* Errors: E_NULL, E_RANGE (also for a workspace that is too small, and for an output that meets an operand it may not), E_HIP. */
+int anszp_adapt(const anszp_adapt_args_t* args, void* hip_stream);
+
+/* The next token of each row from its logits l.  In the order of falling l (equal ones: the lower token first), with w = exp((l - max l) /
+ * temperature), a row keeps the shortest of these beginnings: its first top_k tokens (0 and below: all); of those the shortest that has at least top_p of
+ * their weight, one token at least (1 and above: all); those with w >= min_p (0: all; 1 and above: those equal to the first).  It draws the
+ * first token at which the sum of the kept weights, in the same order, passes uniform * (all of it); uniforms are in [0, 1), others
+ * count as the nearest.  A temperature of 0 draws the first token.  Each setting is one number for all rows, or one for each.  A row that holds a NaN, or
+ * nothing above -infinity, or has a temperature below 0 or NaN, has token -1 and a chance of 0; +infinities share a row alone.
+ * Weights are exact to 2^-43, sums of them too (for vocabularies above 2^18, to 2^-61 of the vocabulary's size); a token below 2^-44 of the first weighs nothing.  No result depends on the
+ * order of additions. */
+typedef struct {
+    const void*    logits;        /* [device] rows x vocabulary of dtype                             */
+    const float*   uniforms;      /* [device] rows                                                   */
+    const float*   temperatures;  /* [device] rows, or NULL: `temperature` for all; likewise the next three */
+    const int32_t* top_ks;
+    const float*   top_ps;
+    const float*   min_ps;
+    int64_t*       tokens;        /* [device] rows                                                   */
+    float*         chances;       /* [device] rows: what part of the kept weight the token has, or NULL */
+    uint64_t       rows;          /* < 2^31, may be 0                                                */
+    uint64_t       logits_stride;
+    uint32_t       vocabulary;    /* 1 .. 2^24                                                       */
+    uint32_t       dtype;         /* ANSZP_OUT_F32 or ANSZP_OUT_BF16                                 */
+    float          temperature;   /* >= 0                                                            */
+    int32_t        top_k;         /* >= 0                                                            */
+    float          top_p, min_p;  /* >= 0                                                            */
+} anszp_sample_args_t;
+/* Errors: E_NULL, E_RANGE, E_HIP. */
+int anszp_sample(const anszp_sample_args_t* args, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -98,6 +98,39 @@ class AttendArgs(C.Structure):
                 ("out_dtype", C.c_uint32), ("scale", C.c_float)]
 
 
+class PlaceArgs(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("lengths", C.c_void_p), ("lengths_out", C.c_void_p), ("new_tokens", C.c_void_p),
+                ("ends", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p), ("n_free_out", C.c_void_p),
+                ("slots", C.c_void_p), ("owners", C.c_void_p), ("starts", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64), ("n_seqs", C.c_uint64), ("n_tokens", C.c_uint64), ("free_room", C.c_uint64),
+                ("table_width", C.c_uint32), ("page_size", C.c_uint32)]
+
+
+class EmbedArgs(C.Structure):
+    _fields_ = [("tokens", C.c_void_p), ("weight", C.c_void_p), ("row_scales", C.c_void_p), ("out", C.c_void_p), ("status", C.c_void_p),
+                ("n_tokens", C.c_uint64), ("vocabulary", C.c_uint64), ("weight_stride", C.c_uint64), ("out_stride", C.c_uint64),
+                ("cols", C.c_uint32), ("weight_dtype", C.c_uint32), ("zero_point", C.c_uint32), ("out_dtype", C.c_uint32),
+                ("scale", C.c_float)]
+
+
+class AdaptArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("a", C.c_void_p), ("b", C.c_void_p), ("ids", C.c_void_p), ("x_scales", C.c_void_p),
+                ("scales", C.c_void_p), ("base", C.c_void_p), ("mul", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p),
+                ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("rows", C.c_uint64),
+                ("cols", C.c_uint64), ("x_stride", C.c_uint64), ("a_stride", C.c_uint64), ("a_row_stride", C.c_uint64),
+                ("b_stride", C.c_uint64), ("b_row_stride", C.c_uint64), ("base_stride", C.c_uint64), ("mul_stride", C.c_uint64),
+                ("residual_stride", C.c_uint64), ("out_stride", C.c_uint64), ("adapters", C.c_uint32), ("k", C.c_uint32),
+                ("rank", C.c_uint32), ("x_dtype", C.c_uint32), ("base_dtype", C.c_uint32), ("out_dtype", C.c_uint32),
+                ("activation", C.c_uint32)]
+
+
+class SampleArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("uniforms", C.c_void_p), ("temperatures", C.c_void_p), ("top_ks", C.c_void_p),
+                ("top_ps", C.c_void_p), ("min_ps", C.c_void_p), ("tokens", C.c_void_p), ("chances", C.c_void_p), ("rows", C.c_uint64),
+                ("logits_stride", C.c_uint64), ("vocabulary", C.c_uint32), ("dtype", C.c_uint32), ("temperature", C.c_float),
+                ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
+
+
 class AnszpError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -110,7 +143,8 @@ EXPORTS = ["anszp_version", "anszp_strerror", "anszp_normalize_freqs", "anszp_bu
            "anszp_dequant_zp", "anszp_conv_fused", "anszp_pack_layer_device",
            "anszp_plan_bytes", "anszp_plan_decode", "anszp_decode_planned", "anszp_decode_static_plan",
            "anszp_pack_layers_device", "anszp_pack_scratch_bytes", "anszp_pack_set_device", "anszp_test_set_spin_limit",
-           "anszp_rms_norm", "anszp_linear_workspace_bytes", "anszp_linear", "anszp_cache_check", "anszp_cache_write", "anszp_cache_read", "anszp_attend_workspace_bytes", "anszp_attend"]
+           "anszp_rms_norm", "anszp_linear_workspace_bytes", "anszp_linear", "anszp_cache_check", "anszp_cache_write", "anszp_cache_read", "anszp_attend_workspace_bytes", "anszp_attend",
+           "anszp_place_workspace_bytes", "anszp_place", "anszp_embed", "anszp_adapt_workspace_bytes", "anszp_adapt", "anszp_sample"]
 
 
 def lib():
@@ -167,6 +201,9 @@ def lib():
         L.anszp_attend_workspace_bytes.argtypes = [C.c_void_p]
         L.anszp_attend_workspace_bytes.restype = C.c_uint64
         L.anszp_attend.argtypes = [C.c_void_p, C.c_void_p]
+        L.anszp_place_workspace_bytes.argtypes = L.anszp_adapt_workspace_bytes.argtypes = [C.c_void_p]
+        L.anszp_place_workspace_bytes.restype = L.anszp_adapt_workspace_bytes.restype = C.c_uint64
+        L.anszp_place.argtypes = L.anszp_embed.argtypes = L.anszp_adapt.argtypes = L.anszp_sample.argtypes = [C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -1089,3 +1126,176 @@ def attend(q, cache: KvCache, pages, lengths, starts, scale: Optional[float] = N
         a.workspace, a.workspace_bytes = workspace.data_ptr(), need
     _enqueue("anszp_attend", L.anszp_attend, dev, C.addressof(a))
     return out
+
+
+# --------------------------------------------------------------------------- a serving step around them
+class Placed(NamedTuple):
+    """What place_tokens gives: slots int64 [n_tokens] for cache_write, starts [sequences + 1] and lengths [sequences] for attend, owners [n_tokens] (the sequence
+    that each token is of; -1, as its slot, behind the last) and n_free [1], all int32 but the slots."""
+    slots: object
+    starts: object
+    lengths: object
+    owners: object
+    n_free: object
+
+
+def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: int, ends=None, lengths_out=None, n_free_out=None, status=None) -> Placed:
+    """anszp_place on torch's current stream: sequences that hold lengths[s] tokens get new[s] more, in pages from the end of the stack free[:n_free].  pages int32
+    [sequences, width] (contiguous), lengths, new and ends int32 [sequences], free int32 [room for all pages], n_free int32 [1]; n_tokens: as many slots are made, at least
+    the sum of new.  A sequence with a number other than 0 in ends gives its pages back first and begins anew.  pages and free are written in place where
+    nothing was held; lengths_out and n_free_out may be lengths and n_free themselves.  A sequence for which there is no room gets nothing: its slots are -1, its
+    length stays, and the status (two int32 words) says so."""
+    torch = _torch()
+    dev = pages.device
+    result = _call("anszp_place", "place_tokens", dev, pages, page_size, lengths, new, free, n_free, n_tokens, ends, lengths_out, n_free_out, status, calls=_operator_calls)
+    if result is not None:
+        return Placed(*result)
+    _device_index(torch, dev)
+    a = PlaceArgs()
+    a.pages = _want(pages, "pages", dev, (None, None), torch.int32)
+    n, width = pages.shape
+    if not pages.is_contiguous():
+        raise ValueError("pages must be contiguous")
+    a.lengths, a.new_tokens = _want(lengths, "lengths", dev, (n,), torch.int32), _want(new, "new", dev, (n,), torch.int32)
+    a.free_pages, a.n_free = _want(free, "free", dev, (None,), torch.int32), _want(n_free, "n_free", dev, (1,), torch.int32)
+    if ends is not None:
+        a.ends = _want(ends, "ends", dev, (n,), torch.int32)
+    if not 0 <= n_tokens < 1 << 31:
+        raise ValueError(f"n_tokens must be from 0 to 2^31 - 1, but is {n_tokens}")
+    if not 0 <= page_size < 1 << 32:
+        raise ValueError(f"page_size must be a power of two from 16 to 65536, but is {page_size}")
+    if lengths_out is None:
+        lengths_out = torch.empty(n, dtype=torch.int32, device=dev)
+    if n_free_out is None:
+        n_free_out = torch.empty(1, dtype=torch.int32, device=dev)
+    a.lengths_out, a.n_free_out = _want(lengths_out, "lengths_out", dev, (n,), torch.int32), _want(n_free_out, "n_free_out", dev, (1,), torch.int32)
+    if status is not None:
+        a.status = _want(status, "status", dev, (2,), torch.int32)
+    slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+    owners, starts = torch.empty(n_tokens, dtype=torch.int32, device=dev), torch.empty(n + 1, dtype=torch.int32, device=dev)
+    a.slots, a.owners, a.starts = slots.data_ptr(), owners.data_ptr(), starts.data_ptr()
+    a.n_seqs, a.n_tokens, a.free_room, a.table_width, a.page_size = n, n_tokens, free.shape[0], _word(width, "the page table's width"), page_size
+    L = lib()
+    need = L.anszp_place_workspace_bytes(C.addressof(a))
+    if need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+    _enqueue("anszp_place", L.anszp_place, dev, C.addressof(a))
+    return Placed(slots, starts, lengths_out, owners, n_free_out)
+
+
+def embed(tokens, weight, zero_point: int = 0, row_scales=None, scale: float = 1.0, out_dtype: str = "bf16", out=None, status=None):
+    """anszp_embed on torch's current stream: rows scale * row_scales[id] * (weight[id] - zero_point) of the tokens int64 [n], weight uint8 symbols [vocabulary, cols] and
+    row_scales fp32 [vocabulary], or scale * weight[id] of a weight in bf16.  Zeros for tokens below 0, and for those beyond the vocabulary, which the
+    status (two int32 words) tells."""
+    torch = _torch()
+    dev = tokens.device
+    if out_dtype in _FLOATS:
+        result = _call("anszp_embed", "embed", dev, tokens, weight, zero_point, row_scales, scale, _FLOATS[out_dtype], out, status, calls=_operator_calls)
+        if result is not None:
+            return result
+    _device_index(torch, dev)
+    a = EmbedArgs()
+    a.tokens = _want(tokens, "tokens", dev, (None,), torch.int64)
+    a.weight = _want(weight, "weight", dev, (None, None), torch.uint8, torch.bfloat16)
+    n, (vocabulary, cols) = tokens.shape[0], weight.shape
+    symbols = weight.dtype == torch.uint8
+    if not 0 <= zero_point <= 255 or (zero_point and not symbols):
+        raise ValueError("zero_point is the symbols' own: 0 to 255, and 0 for weights in bf16")
+    if row_scales is not None:
+        if not symbols:
+            raise ValueError("row_scales are the symbols' own: none for weights in bf16")
+        a.row_scales = _want(row_scales, "row_scales", dev, (vocabulary,), torch.float32)
+    out_type = _out_type(torch, out_dtype)
+    if out is None:
+        out = torch.empty((n, cols), dtype=out_type, device=dev)
+    a.out = _want(out, "out", dev, (n, cols), torch.float32, torch.bfloat16)
+    if status is not None:
+        a.status = _want(status, "status", dev, (2,), torch.int32)
+    a.n_tokens, a.vocabulary, a.weight_stride, a.out_stride, a.cols = n, vocabulary, weight.stride(0), out.stride(0), _word(cols, "weight's columns")
+    a.weight_dtype, a.zero_point, a.out_dtype, a.scale = OUT_U8 if symbols else OUT_BF16, zero_point, _CODE_OF[str(out.dtype)], scale
+    _enqueue("anszp_embed", lib().anszp_embed, dev, C.addressof(a))
+    return out
+
+
+def adapt(base, x, a, b, ids, x_scales=None, scales=None, activation: str = "none", mul=None, residual=None, out_dtype: str = "bf16", out=None, status=None):
+    """anszp_adapt on torch's current stream: act(base + scales[i] * x_scales[r] * (x[r] @ a[i]^T) @ b[i]^T) * mul + residual with i = ids[r], and nothing added to base
+    for ids below 0.  base [rows, cols] fp32 or bf16 (what linear gives without its epilogue), x [rows, k] bf16 or int8, a [adapters, rank, k] and b
+    [adapters, cols, rank] bf16, ids int32 [rows], x_scales fp32 [rows], scales fp32 [adapters]; mul and residual [rows, cols] of the output's type (out's own, if it is
+    given).  Returns out (which may be base, of the same type, mul or residual itself).  An id beyond the adapters counts as none, and the status (two int32 words) tells."""
+    torch = _torch()
+    dev = base.device
+    if out_dtype in _FLOATS and activation in FN_CODES:
+        result = _call("anszp_adapt", "adapt", dev, base, x, a, b, ids, x_scales, scales, FN_CODES[activation], mul, residual, _FLOATS[out_dtype], out, status,
+                       calls=_operator_calls)
+        if result is not None:
+            return result
+    _device_index(torch, dev)
+    args = AdaptArgs()
+    args.base = _want(base, "base", dev, (None, None), torch.float32, torch.bfloat16)
+    rows, cols = base.shape
+    args.x = _want(x, "x", dev, (rows, None), torch.bfloat16, torch.int8)
+    k = x.shape[1]
+    args.a = _want(a, "a", dev, (None, None, k), torch.bfloat16)
+    n, rank, _ = a.shape
+    args.b = _want(b, "b", dev, (n, cols, rank), torch.bfloat16)
+    args.ids = _want(ids, "ids", dev, (rows,), torch.int32)
+    if activation not in FN_CODES:
+        raise ValueError(f"activation must be one of {tuple(FN_CODES)}, but is {activation!r}")
+    out_type = _out_type(torch, out_dtype)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=out_type, device=dev)
+    args.out = _want(out, "out", dev, (rows, cols), torch.float32, torch.bfloat16)
+    if x_scales is not None:
+        args.x_scales = _want(x_scales, "x_scales", dev, (rows,), torch.float32)
+    if scales is not None:
+        args.scales = _want(scales, "scales", dev, (n,), torch.float32)
+    if mul is not None:
+        args.mul, args.mul_stride = _want(mul, "mul", dev, (rows, cols), out.dtype), mul.stride(0)
+    if residual is not None:
+        args.residual, args.residual_stride = _want(residual, "residual", dev, (rows, cols), out.dtype), residual.stride(0)
+    if status is not None:
+        args.status = _want(status, "status", dev, (2,), torch.int32)
+    args.rows, args.cols, args.adapters, args.k, args.rank = rows, cols, _word(n, "the adapters' number"), _word(k, "x's columns"), _word(rank, "the rank")
+    args.x_stride, args.a_stride, args.a_row_stride, args.b_stride, args.b_row_stride = x.stride(0), a.stride(0), a.stride(1), b.stride(0), b.stride(1)
+    args.base_stride, args.out_stride = base.stride(0), out.stride(0)
+    args.x_dtype, args.base_dtype, args.out_dtype, args.activation = *(_CODE_OF[str(t.dtype)] for t in (x, base, out)), FN_CODES[activation]
+    L = lib()
+    need = L.anszp_adapt_workspace_bytes(C.addressof(args))
+    if need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        args.workspace, args.workspace_bytes = workspace.data_ptr(), need
+    _enqueue("anszp_adapt", L.anszp_adapt, dev, C.addressof(args))
+    return out
+
+
+def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None):
+    """anszp_sample on torch's current stream: a token for each row of logits [rows, vocabulary] fp32 or bf16, drawn by uniforms fp32 [rows] from [0, 1) among what
+    top_k, top_p and min_p leave, in the order of falling logits; a temperature of 0 takes the largest.  temperature, top_p and min_p are numbers or fp32 [rows], top_k is a
+    number or int32 [rows].  Returns (tokens int64 [rows], which is `out` where that is given; chances fp32 [rows], the token's part of what was
+    left); a row that has no token (a NaN, nothing above -infinity) has -1 and 0."""
+    torch = _torch()
+    dev = logits.device
+    results = _call("anszp_sample", "sample", dev, logits, uniforms, temperature, top_k, top_p, min_p, out, calls=_operator_calls)
+    if results is not None:
+        return results
+    _device_index(torch, dev)
+    a = SampleArgs()
+    a.logits = _want(logits, "logits", dev, (None, None), torch.float32, torch.bfloat16)
+    rows, vocabulary = logits.shape
+    a.uniforms = _want(uniforms, "uniforms", dev, (rows,), torch.float32)
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
+        if isinstance(value, torch.Tensor):
+            setattr(a, name + "s", _want(value, name, dev, (rows,), dtype))
+        elif not value >= 0 or (name == "top_k" and not (isinstance(value, int) and value < 1 << 31)):
+            raise ValueError(f"{name} must be {'a whole number' if name == 'top_k' else 'a number'} from 0 on, or a tensor of one for each row, but is {value!r}")
+        else:
+            setattr(a, name, value)
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int64, device=dev)
+    a.tokens = _want(out, "out", dev, (rows,), torch.int64)
+    chances = torch.empty(rows, dtype=torch.float32, device=dev)
+    a.chances = chances.data_ptr()
+    a.rows, a.logits_stride, a.vocabulary, a.dtype = rows, logits.stride(0), _word(vocabulary, "the vocabulary"), _CODE_OF[str(logits.dtype)]
+    _enqueue("anszp_sample", lib().anszp_sample, dev, C.addressof(a))
+    return out, chances

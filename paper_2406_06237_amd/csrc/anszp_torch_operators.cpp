@@ -4,6 +4,7 @@
 // They return their tensors, the library's error code, or None where they decline.  The interpreter lock is held only while Python
 // objects are read and made.
 #include <ATen/ATen.h>
+#include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <climits>
@@ -177,6 +178,137 @@ py::object attend(const at::Tensor& q, const at::Tensor& ck, const at::Tensor& c
     return rc ? failed(rc) : py::cast(*out);
 }
 
+bool ints(const at::Tensor& t, const at::Device& on, int64_t n) { return vector(t, on, n) && t.scalar_type() == at::kInt; }
+bool floats(const at::Tensor& t, const at::Device& on, int64_t n) { return vector(t, on, n) && t.scalar_type() == at::kFloat; }
+
+py::object place_tokens(const at::Tensor& pages, int64_t page_size, const at::Tensor& lengths, const at::Tensor& fresh, const at::Tensor& free, const at::Tensor& n_free,
+                        int64_t n_tokens, const Maybe& ends, Maybe lengths_out, Maybe n_free_out, const Maybe& status, uint64_t stream) {
+    const at::Device on = pages.device();
+    if (pages.dim() != 2 || pages.scalar_type() != at::kInt || !pages.is_contiguous() || pages.size(1) > 1ll << 30 || page_size < 0 || page_size > 65536 || n_tokens < 0 ||
+        n_tokens >= 1ll << 31 || free.dim() != 1 || free.size(0) >= 1ll << 31)
+        return none();
+    const int64_t n = pages.size(0);
+    if (!ints(lengths, on, n) || !ints(fresh, on, n) || !ints(free, on, free.size(0)) || !ints(n_free, on, 1) || (ends && !ints(*ends, on, n)) ||
+        (lengths_out && !ints(*lengths_out, on, n)) || (n_free_out && !ints(*n_free_out, on, 1)) || (status && !ints(*status, on, 2)))
+        return none();
+    at::Tensor slots, owners, starts;
+    const int rc = unlocked([&] {
+        slots = at::empty({n_tokens}, pages.options().dtype(at::kLong));
+        owners = at::empty({n_tokens}, pages.options());
+        starts = at::empty({n + 1}, pages.options());
+        if (!lengths_out) lengths_out = at::empty({n}, pages.options());
+        if (!n_free_out) n_free_out = at::empty({1}, pages.options());
+        anszp_place_args_t a = {};
+        a.pages = data<int32_t>(pages); a.lengths = data<int32_t>(lengths); a.lengths_out = address<int32_t>(lengths_out); a.new_tokens = data<int32_t>(fresh);
+        a.ends = address<int32_t>(ends); a.free_pages = data<int32_t>(free); a.n_free = data<int32_t>(n_free); a.n_free_out = address<int32_t>(n_free_out);
+        a.slots = data<int64_t>(slots); a.owners = data<int32_t>(owners); a.starts = data<int32_t>(starts); a.status = address<uint32_t>(status);
+        a.n_seqs = uint64_t(n); a.n_tokens = uint64_t(n_tokens); a.free_room = uint64_t(free.size(0)); a.table_width = uint32_t(pages.size(1)); a.page_size = uint32_t(page_size);
+        at::Tensor workspace;
+        a.workspace_bytes = anszp_place_workspace_bytes(&a);
+        if (a.workspace_bytes) {
+            workspace = at::empty({int64_t(a.workspace_bytes)}, pages.options().dtype(at::kByte));
+            a.workspace = workspace.data_ptr();
+        }
+        return anszp_place(&a, stream_of(stream));
+    });
+    return rc ? failed(rc) : py::object(py::make_tuple(slots, starts, *lengths_out, owners, *n_free_out));
+}
+
+py::object embed(const at::Tensor& tokens, const at::Tensor& weight, int64_t zero_point, const Maybe& row_scales, double scale, int out_code, Maybe out, const Maybe& status,
+                 uint64_t stream) {
+    const at::Device on = tokens.device();
+    const bool symbols = weight.scalar_type() == at::kByte;
+    if (tokens.dim() != 1 || tokens.scalar_type() != at::kLong || !packed(tokens) || weight.dim() != 2 || weight.device() != on || !packed(weight) ||
+        (!symbols && weight.scalar_type() != at::kBFloat16) || zero_point < 0 || zero_point > (symbols ? 255 : 0) || weight.size(1) >= 1ll << 31 ||
+        (row_scales && (!symbols || !floats(*row_scales, on, weight.size(0)))) || (status && !ints(*status, on, 2)))
+        return none();
+    const int64_t n = tokens.size(0), cols = weight.size(1);
+    if (out && (!matrix(*out, on, n, cols) || !is_float(*out))) return none();
+    const int rc = unlocked([&] {
+        if (!out) out = at::empty({n, cols}, weight.options().dtype(out_code == ANSZP_OUT_F32 ? at::kFloat : at::kBFloat16));
+        anszp_embed_args_t a = {};
+        a.tokens = data<int64_t>(tokens); a.weight = weight.data_ptr(); a.row_scales = address<float>(row_scales); a.out = out->data_ptr(); a.status = address<uint32_t>(status);
+        a.n_tokens = uint64_t(n); a.vocabulary = uint64_t(weight.size(0)); a.weight_stride = rows_apart(weight); a.out_stride = rows_apart(*out); a.cols = uint32_t(cols);
+        a.weight_dtype = symbols ? ANSZP_OUT_U8 : ANSZP_OUT_BF16; a.zero_point = uint32_t(zero_point); a.out_dtype = code_of(*out); a.scale = float(scale);
+        return anszp_embed(&a, stream_of(stream));
+    });
+    return rc ? failed(rc) : py::cast(*out);
+}
+
+py::object adapt(const at::Tensor& base, const at::Tensor& x, const at::Tensor& wa, const at::Tensor& wb, const at::Tensor& ids, const Maybe& x_scales, const Maybe& scales,
+                 uint32_t activation, const Maybe& mul, const Maybe& residual, int out_code, Maybe out, const Maybe& status, uint64_t stream) {
+    const at::Device on = base.device();
+    if (base.dim() != 2 || !is_float(base) || !packed(base) || x.dim() != 2 || wa.dim() != 3 || wb.dim() != 3) return none();
+    const int64_t rows = base.size(0), cols = base.size(1), k = x.size(1), n = wa.size(0), rank = wa.size(1);
+    if (!matrix(x, on, rows, k) || (x.scalar_type() != at::kChar && x.scalar_type() != at::kBFloat16) || wa.device() != on || wb.device() != on ||
+        wa.scalar_type() != at::kBFloat16 || wb.scalar_type() != at::kBFloat16 || wa.size(2) != k || wb.size(0) != n || wb.size(1) != cols || wb.size(2) != rank ||
+        !packed(wa) || !packed(wb) || !ints(ids, on, rows) || k >= 1ll << 31 || rank > 256 || n >= 1ll << 24)
+        return none();
+    if (out && (!matrix(*out, on, rows, cols) || !is_float(*out))) return none();
+    const at::ScalarType type = out ? out->scalar_type() : out_code == ANSZP_OUT_F32 ? at::kFloat : at::kBFloat16;
+    for (const Maybe* t : {&mul, &residual})
+        if (*t && (!matrix(**t, on, rows, cols) || (*t)->scalar_type() != type)) return none();
+    if ((x_scales && !floats(*x_scales, on, rows)) || (scales && !floats(*scales, on, n)) || (status && !ints(*status, on, 2))) return none();
+    const int rc = unlocked([&] {
+        if (!out) out = at::empty({rows, cols}, base.options().dtype(type));
+        anszp_adapt_args_t a = {};
+        a.x = x.data_ptr(); a.a = wa.data_ptr(); a.b = wb.data_ptr(); a.ids = data<int32_t>(ids); a.x_scales = address<float>(x_scales); a.scales = address<float>(scales);
+        a.base = base.data_ptr(); a.mul = address(mul); a.residual = address(residual); a.out = out->data_ptr(); a.status = address<uint32_t>(status);
+        a.rows = uint64_t(rows); a.cols = uint64_t(cols); a.x_stride = rows_apart(x); a.a_stride = rows_apart(wa); a.a_row_stride = uint64_t(wa.stride(1));
+        a.b_stride = rows_apart(wb); a.b_row_stride = uint64_t(wb.stride(1)); a.base_stride = rows_apart(base); a.mul_stride = mul ? rows_apart(*mul) : 0u;
+        a.residual_stride = residual ? rows_apart(*residual) : 0u; a.out_stride = rows_apart(*out); a.adapters = uint32_t(n); a.k = uint32_t(k); a.rank = uint32_t(rank);
+        a.x_dtype = code_of(x); a.base_dtype = code_of(base); a.out_dtype = code_of(*out); a.activation = activation;
+        at::Tensor workspace;
+        a.workspace_bytes = anszp_adapt_workspace_bytes(&a);
+        if (a.workspace_bytes) {
+            workspace = at::empty({int64_t(a.workspace_bytes)}, base.options().dtype(at::kByte));
+            a.workspace = workspace.data_ptr();
+        }
+        return anszp_adapt(&a, stream_of(stream));
+    });
+    return rc ? failed(rc) : py::cast(*out);
+}
+
+// A setting is a number for all rows, or a tensor with one for each; false: neither.
+bool setting(const py::object& given, const at::Device& on, int64_t rows, at::ScalarType type, Maybe& each, double& all) {
+    if (THPVariable_Check(given.ptr())) {
+        each = THPVariable_Unpack(given.ptr());
+        return vector(*each, on, rows) && each->scalar_type() == type;
+    }
+    if (!PyFloat_Check(given.ptr()) && !PyLong_Check(given.ptr())) return false;
+    all = PyFloat_AsDouble(given.ptr());
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return type == at::kFloat || (all >= 0.0 && all < 2147483648.0 && PyLong_Check(given.ptr()));
+}
+
+py::object sample(const at::Tensor& logits, const at::Tensor& uniforms, const py::object& temperature, const py::object& top_k, const py::object& top_p, const py::object& min_p,
+                  Maybe tokens, uint64_t stream) {
+    const at::Device on = logits.device();
+    if (logits.dim() != 2 || !is_float(logits) || !packed(logits) || logits.size(1) > 1ll << 24) return none();
+    const int64_t rows = logits.size(0);
+    Maybe temperatures, top_ks, top_ps, min_ps;
+    double t = 1.0, k = 0.0, tp = 1.0, mp = 0.0;
+    if (!floats(uniforms, on, rows) || !setting(temperature, on, rows, at::kFloat, temperatures, t) || !setting(top_k, on, rows, at::kInt, top_ks, k) ||
+        !setting(top_p, on, rows, at::kFloat, top_ps, tp) || !setting(min_p, on, rows, at::kFloat, min_ps, mp) || !(t >= 0.0) || !(tp >= 0.0) || !(mp >= 0.0))
+        return none();
+    if (tokens && (!vector(*tokens, on, rows) || tokens->scalar_type() != at::kLong)) return none();
+    at::Tensor chances;
+    const int rc = unlocked([&] {
+        if (!tokens) tokens = at::empty({rows}, logits.options().dtype(at::kLong));
+        chances = at::empty({rows}, logits.options().dtype(at::kFloat));
+        anszp_sample_args_t a = {};
+        a.logits = logits.data_ptr(); a.uniforms = data<float>(uniforms); a.temperatures = address<float>(temperatures); a.top_ks = address<int32_t>(top_ks);
+        a.top_ps = address<float>(top_ps); a.min_ps = address<float>(min_ps); a.tokens = address<int64_t>(tokens); a.chances = data<float>(chances);
+        a.rows = uint64_t(rows); a.logits_stride = rows_apart(logits); a.vocabulary = uint32_t(logits.size(1)); a.dtype = code_of(logits);
+        a.temperature = float(t); a.top_k = int32_t(k); a.top_p = float(tp); a.min_p = float(mp);
+        return anszp_sample(&a, stream_of(stream));
+    });
+    return rc ? failed(rc) : py::object(py::make_tuple(*tokens, chances));
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_anszp_operators, m) {
@@ -185,4 +317,8 @@ PYBIND11_MODULE(_anszp_operators, m) {
     m.def("cache_write", &cache_write);
     m.def("cache_read", &cache_read);
     m.def("attend", &attend);
+    m.def("place_tokens", &place_tokens);
+    m.def("embed", &embed);
+    m.def("adapt", &adapt);
+    m.def("sample", &sample);
 }

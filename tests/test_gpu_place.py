@@ -1,0 +1,101 @@
+"""GPU: new tokens placed in a paged cache: tables, stacks, lengths, starts, owners and slots equal to a program's that goes through the sequences one by one."""
+import random
+
+import pytest
+import torch
+
+import serving_plain as P
+from paper_2406_06237_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def ints(a):
+    return torch.tensor(a, dtype=torch.int32, device=DEV)
+
+
+def _state(rng, n, page, most, spare, width=None):
+    lengths = [rng.choice((0, page, rng.randint(0, most))) for _ in range(n)]
+    width = width or -(-most // page) + 3
+    counts = [-(-length // page) for length in lengths]
+    deal = rng.sample(range(sum(counts) + spare), sum(counts) + spare)
+    pages, at = [[-7] * width for _ in range(n)], 0
+    for row, c in zip(pages, counts):
+        row[:c] = deal[at:at + c]
+        at += c
+    return pages, lengths, deal[at:] + [-9] * at, spare
+
+
+def _check(pages, page, lengths, new, free, n_free, n_tokens, ends=None, in_place=False):
+    want = P.place(pages, page, lengths, new, free, n_free, n_tokens, ends)
+    table, held, stack, count, status = torch.tensor(pages, dtype=torch.int32, device=DEV).view(len(pages), -1), ints(lengths), ints(free), ints([n_free]), ints([0, 0])
+    kept = dict(lengths_out=held, n_free_out=count) if in_place else {}
+    got = B.place_tokens(table, page, held, ints(new), stack, count, n_tokens, ends=None if ends is None else ints(ends), status=status, **kept)
+    slots, starts, after, owners, left, want_table, want_stack, told = want
+    assert got.slots.dtype == torch.int64 and got.slots.tolist() == slots
+    assert got.starts.tolist() == starts and got.lengths.tolist() == after and got.owners.tolist() == owners and got.n_free.tolist() == [left]
+    assert table.tolist() == want_table and stack.tolist() == want_stack
+    assert status.tolist() == ([1, told] if told else [0, 0])
+    assert (got.lengths is held) == in_place and (in_place or (held.tolist() == list(lengths) and count.tolist() == [n_free]))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,page,most,new", [(1, 16, 40, 1), (1, 64, 3000, 2999), (16, 64, 4000, 1), (63, 16, 200, 300), (64, 32, 100, 5), (65, 256, 1000, 700), (300, 16, 50, 90),
+                                             (1023, 16, 20, 1), (1025, 16, 40, 20), (3000, 16, 33, 3)])
+def test_any_step(n, page, most, new, in_place):
+    for seed in range(4):
+        rng = random.Random(seed * 1000 + n)
+        fresh = [rng.choice((0, 1, rng.randint(0, new))) for _ in range(n)]
+        ends = None if seed == 0 else [int(rng.random() < 0.3) * rng.choice((1, -5)) for _ in range(n)]
+        # enough pages, a few, none
+        spare = (sum(fresh) // page + 2 * n, sum(fresh) // page + 2 * n, rng.randint(0, 9), 0)[seed]
+        pages, lengths, free, n_free = _state(rng, n, page, most, spare, -(-(most + new) // page) + 1)
+        _check(pages, page, lengths, fresh, free, n_free, sum(fresh) + rng.choice((0, 1, 77)), ends, in_place)
+
+
+def test_a_sequence_begins_anew_in_pages_that_it_gave_back():
+    _check([[3, 5, 1]], 16, [40], [33], [-1] * 3, 0, 33, [1])
+    _check([[3, 5, 1], [0, 2, 4]], 16, [40, 16], [48, 5], [-1] * 4, 0, 60, [1, 0])
+
+
+@pytest.mark.parametrize("new,n_tokens", [([5, -1, 3], 9), ([5, 100, 3], 200), ([5, 4, 3], 11), ([5, 4, 3], 4), ([0, 0, 0], 0), ([2**31 - 1, 2**31 - 1, 1], 5)])
+def test_sequences_that_get_nothing(new, n_tokens):
+    """Fewer than none, more than a row of the table has room for, more than there are slots: the others get theirs."""
+    _check([[0, 1, -7], [2, -7, -7], [-7, -7, -7]], 16, [20, 16, 0], new, [3, 4, 5, 6, 7, -9], 5, n_tokens)
+
+
+def test_pages_run_out():
+    """A sequence that needs none of them goes on behind one that got none."""
+    _check([[0, -7], [1, -7], [2, -7], [3, -7]], 16, [16, 3, 16, 16], [1, 13, 1, 1], [9, 8, -1, -1], 1, 20)
+
+
+def test_no_sequences_and_no_tokens():
+    got = B.place_tokens(torch.empty(0, 4, dtype=torch.int32, device=DEV), 16, ints([]), ints([]), ints([1, 2]), ints([2]), 3)
+    assert got.slots.tolist() == [-1] * 3 and got.starts.tolist() == [0] and got.owners.tolist() == [-1] * 3 and got.n_free.tolist() == [2]
+    got = B.place_tokens(ints([[1]]), 16, ints([4]), ints([0]), ints([]), ints([0]), 0)
+    assert got.slots.shape == (0,) and got.starts.tolist() == [0, 0] and got.lengths.tolist() == [4]
+
+
+def test_numbers_out_of_range_are_told():
+    """Lengths that no table has, a stack that is larger than its room or overflows, pages below 0: nothing outside is touched."""
+    status = ints([0, 0])
+    table, stack = ints([[4, 5], [6, 7], [-3, -3]]), ints([1, 2, 3])
+    got = B.place_tokens(table, 16, ints([33, -1, 5]), ints([1, 1, 2]), stack, ints([77]), 8, status=status)
+    assert got.slots.tolist() == [-1] * 8 and got.lengths.tolist() == [33, -1, 7] and got.n_free.tolist() == [3] and got.owners.tolist() == [0, 1, 2, 2] + [-1] * 4
+    assert status.tolist() == [1, 5] and table.tolist() == [[4, 5], [6, 7], [-3, -3]] and stack.tolist() == [1, 2, 3]
+    status.zero_()
+    got = B.place_tokens(table, 16, ints([2**31 - 1, -5, 5]), ints([0, 17, 0]), stack, ints([2]), 20, ends=ints([1, 1, 0]), status=status)
+    # (of the first one's pages one finds room, the second gives none back)
+    assert stack.tolist() == [1, 2, 4] and status.tolist() == [1, 3] and got.lengths.tolist() == [0, 17, 5] and got.n_free.tolist() == [1]
+    assert table.tolist() == [[4, 5], [4, 2], [-3, -3]] and got.slots.tolist() == [4 * 16 + i for i in range(16)] + [2 * 16] + [-1] * 3
+
+
+def test_on_another_stream():
+    rng = random.Random(5)
+    pages, lengths, free, n_free = _state(rng, 40, 16, 100, 90)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _check(pages, 16, lengths, [7] * 40, free, n_free, 280)
+    side.synchronize()
