@@ -2,7 +2,7 @@
 //   h = scales[i] * x_scales[r] * a[i] x[r]              out = act(base + b[i] h) * mul + residual
 // and no adapter's part for ids below 0.  Two launches: h from all of k, then the output's columns.
 //
-// Rows come in tiles of 16, and a tile is worked through once for each adapter that its rows have: one for a prompt, up to sixteen for a step of as
+// Rows come in tiles of 64, and a tile is worked through once for each adapter that its rows have: one for a prompt, up to 64 for a step of as
 // many requests.  What a row has from other rows' adapters is never selected, so that nothing in them, an infinity or a NaN, reaches it.  x and a are bf16 (8-bit rows are exact in
 // it), their sums in 32 bits.  h goes into the second product as two bf16 numbers, to 2^-18 of it, for bf16 outputs, and as three, all of it, for fp32 ones: a number rounded
 // to bf16 leaves a rest that is exact.
@@ -28,45 +28,60 @@ struct AdaptParams {
     const void* residual;
     void* out;
     float* h;                           // [part of k][row][rank up to a multiple of 8]
+    uint16_t* terms_of_h;               // of many rows, [row][width]
     uint32_t* status;
     uint64_t x_stride, a_stride, a_row_stride, b_stride, b_row_stride, base_stride, mul_stride, residual_stride, out_stride;    // x's in bytes
     uint64_t rows, cols;
-    uint32_t adapters, k, rank, rank_room, base_dtype, out_dtype, activation;
+    uint32_t adapters, k, rank, rank_room, activation;
     uint32_t slots, groups, parts;      // workgroups that share a tile's adapters, groups of ranks, parts of k
     uint32_t blocks, terms;             // blocks of 8 ranks a term of h has, terms
-    uint32_t across;                    // workgroups that a row's columns take
+    uint32_t across, width;             // workgroups that a row's columns take; a row of h's terms
+    const uint8_t* x_last;              // where the last 16 bytes of each begin
+    const uint8_t* a_last;
+    const uint8_t* b_last;
 };
 
 __device__ __forceinline__ bf16x8 as_bf16(words4 w) { return __builtin_bit_cast(bf16x8, w); }
 
-// Sixteen consecutive elements of a row of bf16 or of signed bytes, as two operands; zeros behind its end.
+// The first `there` bytes of 16 (0 and below: none), zeros behind them.
+__device__ __forceinline__ words4 first_bytes(words4 w, int32_t there) {
+#pragma unroll
+    for (int32_t i = 0; i < 4; ++i) {
+        const int32_t n = there - 4 * i;
+        w[i] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+    }
+    return w;
+}
+// 16 bytes of which the first `there` are an operand's, whose last 16 begin at `last`: nothing behind them is read, and what lies between its rows counts as zeros.
+// (Ends of rows one element at a time take a way of the program each, and so many registers that few wavefronts are left.)
+__device__ __forceinline__ words4 careful(const uint8_t* at, int32_t there, const uint8_t* last) {
+    const uint64_t over = at > last ? uint64_t(at - last) : 0u;
+    const words4 w = *reinterpret_cast<const words4_any*>(at - over);
+    uint64_t lo = uint64_t(w[1]) << 32 | w[0], hi = uint64_t(w[3]) << 32 | w[2];
+    const uint32_t by = uint32_t(over < 16u ? over : 16u) * 8u;
+    lo = by >= 64u ? (by >= 128u ? 0u : hi >> (by - 64u)) : by ? lo >> by | hi << (64u - by) : lo;
+    hi = by >= 64u ? 0u : hi >> by;
+    return first_bytes(words4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)}, there);
+}
+
+// Sixteen consecutive elements of a row of bf16 or of signed bytes, as two operands.
 template <bool BYTES>
 struct Sixteen {
     words4 lo, hi;
-    __device__ __forceinline__ void load(const uint8_t* row, uint32_t at, uint32_t there) {
-        if constexpr (BYTES) {
-            const uint8_t* p = row + at;
-            hi = words4{0u, 0u, 0u, 0u};
-            if (there >= 16u) {
-                lo = *reinterpret_cast<const words4_any*>(p);
-            } else {
-                lo = words4{0u, 0u, 0u, 0u};
-                for (uint32_t i = 0; i < 16u; ++i)
-                    if (i < there) lo[i >> 2] |= uint32_t(p[i]) << (8u * (i & 3u));
-            }
-        } else {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + at;
-            Eight<ANSZP_OUT_BF16> a, b;
-            a.load(p, 0u, there);
-            b.load(p, 8u, there > 8u ? there - 8u : 0u);
-            lo = a.w;
-            hi = b.w;
-        }
+    __device__ __forceinline__ void load(const uint8_t* at) {
+        lo = *reinterpret_cast<const words4_any*>(at);
+        if constexpr (!BYTES) hi = *reinterpret_cast<const words4_any*>(at + 16);
+    }
+    // where fewer than 16 are there
+    __device__ __forceinline__ void load(const uint8_t* at, int32_t there, const uint8_t* last) {
+        lo = careful(at, BYTES ? there : 2 * there, last);
+        if constexpr (!BYTES) hi = careful(at + 16, 2 * there - 16, last);
     }
     // A whole number below 2^8 in size fits bf16, so the upper half of its binary32 is all of it.
     __device__ __forceinline__ bf16x8 operand(uint32_t half) const {
         if constexpr (BYTES) {
             words4 w;
+#pragma unroll
             for (uint32_t i = 0; i < 4u; ++i) {
                 const uint32_t four = lo[half * 2u + (i >> 1)], at = 16u * (i & 1u);
                 const float a = float(int32_t(four << (24u - at)) >> 24), b = float(int32_t(four << (16u - at)) >> 24);
@@ -90,66 +105,111 @@ __device__ __forceinline__ int32_t id_of(const AdaptParams& p, uint64_t row, boo
     return -1;
 }
 
-// work(adapter, lanes that have it) for each adapter that the first `n` lanes' rows have.
-template <class Work>
-__device__ __forceinline__ void each_adapter(int32_t id, uint32_t n, Work work) {
-    uint64_t left = __ballot(id >= 0 && (threadIdx.x & 63u) < n);
-    while (left) {
+// The adapters that a tile of 64 rows has, one after the other, by the lanes (a row each) that have them.
+struct Adapters {
+    int32_t id;
+    uint64_t left, lanes;
+    __device__ __forceinline__ explicit Adapters(int32_t of_row) : id(of_row), left(__ballot(of_row >= 0)), lanes(0u) {}
+    // the next one, or -1
+    __device__ __forceinline__ int32_t next() {
+        if (!left) return -1;
         const int32_t one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        const uint64_t same = __ballot(id == one) & left;
-        left &= ~same;
-        work(uint32_t(one), same);
+        lanes = __ballot(id == one);
+        left &= ~lanes;
+        return one;
     }
-}
+};
 
-// h of 16 rows and up to 16 * RANKS ranks.  ROWS: a wavefront has a tile of rows of its own; else the four of a workgroup share a tile's k.
-template <bool BYTES, bool ROWS, uint32_t RANKS>
-__global__ __launch_bounds__(256) void adapt_down_kernel(AdaptParams p) {
+// h of 64 rows and up to 16 * RANKS ranks; the four wavefronts share a part of k and add up what they have.
+template <bool BYTES, uint32_t RANKS>
+__global__ __launch_bounds__(256, 2) void adapt_down_kernel(AdaptParams p) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint32_t slot = blockIdx.y / p.groups, group = blockIdx.y - slot * p.groups, part = blockIdx.z;
-    const uint64_t first = (uint64_t(blockIdx.x) * (ROWS ? 4u : 1u) + (ROWS ? wave : 0u)) * 16u;
-    if (ROWS && first >= p.rows) return;
-    const int32_t id = id_of(p, first + c, false);
-    const uint32_t steps = (p.k + 63u) / 64u, share = ROWS ? part : part * 4u + wave, shares = ROWS ? p.parts : p.parts * 4u;
+    const uint64_t first = uint64_t(blockIdx.x) * 64u;
+    const uint32_t steps = (p.k + 63u) / 64u, share = part * 4u + wave, shares = p.parts * 4u;
     const uint32_t begin = uint32_t(uint64_t(steps) * share / shares), end = uint32_t(uint64_t(steps) * (share + 1u) / shares);
-    const uint64_t row = least(first + c, p.rows - 1u);
-    const uint8_t* const x = p.x + row * p.x_stride;
-    __shared__ floatx4 sums[ROWS ? 1u : 4u][ROWS ? 1u : RANKS][64];
-    uint32_t turn = 0u;
-    each_adapter(id, 16u, [&](uint32_t one, uint64_t) __attribute__((always_inline)) {
-        if (turn++ % p.slots != slot) return;
-        const uint16_t* a[RANKS];
-        for (uint32_t t = 0; t < RANKS; ++t) a[t] = p.a + one * p.a_stride + least((group * RANKS + t) * 16u + c, p.rank - 1u) * p.a_row_stride;
-        floatx4 sum[RANKS] = {};
-        const auto step = [&](uint32_t s) __attribute__((always_inline)) {
-            const uint32_t at = s * 64u + g * 16u, there = at < p.k ? p.k - at : 0u;
-            Sixteen<BYTES> xs;
-            Sixteen<false> as[RANKS];
-            xs.load(x, at, there);
-            for (uint32_t t = 0; t < RANKS; ++t) as[t].load(reinterpret_cast<const uint8_t*>(a[t]), at, there);
-            for (uint32_t half = 0; half < 2u; ++half)
-                for (uint32_t t = 0; t < RANKS; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs.operand(half), as[t].operand(half), sum[t], 0, 0, 0);
-        };
-        for (uint32_t s = begin; s < end; ++s) step(s);
-        if constexpr (!ROWS) {
-            __syncthreads();
-            for (uint32_t t = 0; t < RANKS; ++t) sums[wave][t][lane] = sum[t];
-            __syncthreads();
-            if (wave != 0u) return;
-            for (uint32_t w = 1; w < 4u; ++w)
-                for (uint32_t t = 0; t < RANKS; ++t) sum[t] += sums[w][t][lane];
-        }
+    __shared__ floatx4 sums[4][4][RANKS][64];
+    const float x_scale = p.x_scales ? p.x_scales[least(first + lane, p.rows - 1u)] : 1.0f;
+    Adapters adapters(id_of(p, first + lane, false));
+    const uint8_t* x[4];
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r) x[r] = p.x + least(first + r * 16u + c, p.rows - 1u) * p.x_stride;
+    for (uint32_t turn = 0;; ++turn) {
+        const int32_t one = adapters.next();
+        if (one < 0) break;
+        if (turn % p.slots != slot) continue;
+        const uint8_t* a[RANKS];
+#pragma unroll
+        for (uint32_t t = 0; t < RANKS; ++t) a[t] = reinterpret_cast<const uint8_t*>(p.a + uint64_t(one) * p.a_stride + least((group * RANKS + t) * 16u + c, p.rank - 1u) * p.a_row_stride);
         const float by = p.scales ? p.scales[one] : 1.0f;
+        bool has[4];
+#pragma unroll
+        for (uint32_t r = 0; r < 4u; ++r) has[r] = (adapters.lanes >> (16u * r) & 0xFFFFu) != 0u;
+        floatx4 sum[4][RANKS] = {};
+        struct Step {
+            Sixteen<BYTES> x[4];
+            Sixteen<false> a[RANKS];
+        } now, then;
+        const auto load = [&](Step& to, uint32_t s) __attribute__((always_inline)) {
+            const uint32_t at = s * 64u + g * 16u;
+#pragma unroll
+            for (uint32_t t = 0; t < RANKS; ++t) to.a[t].load(a[t] + at * 2u);
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r)
+                if (has[r]) to.x[r].load(x[r] + at * (BYTES ? 1u : 2u));
+        };
+        const auto multiply = [&](const Step& with) __attribute__((always_inline)) {
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r) {
+                if (!has[r]) continue;
+#pragma unroll
+                for (uint32_t half = 0; half < 2u; ++half) {
+                    const bf16x8 xs = with.x[r].operand(half);
+#pragma unroll
+                    for (uint32_t t = 0; t < RANKS; ++t) sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs, with.a[t].operand(half), sum[r][t], 0, 0, 0);
+                }
+            }
+        };
+        // (the step in which k ends is one of its own, behind the others)
+        const uint32_t last = end * 64u > p.k ? end - 1u : end;
+        if (begin < last) load(now, begin);
+        for (uint32_t s = begin; s < last; s += 2u) {
+            if (s + 1u < last) load(then, s + 1u);
+            multiply(now);
+            if (s + 2u < last) load(now, s + 2u);
+            if (s + 1u < last) multiply(then);
+        }
+        if (begin < end && last < end) {
+            const uint32_t at = last * 64u + g * 16u;
+            const int32_t there = int32_t(p.k) - int32_t(at);
+#pragma unroll
+            for (uint32_t t = 0; t < RANKS; ++t) now.a[t].load(a[t] + at * 2u, there, p.a_last);
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r)
+                if (has[r]) now.x[r].load(x[r] + at * (BYTES ? 1u : 2u), there, p.x_last);
+            multiply(now);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < 4u; ++r)
+#pragma unroll
+            for (uint32_t t = 0; t < RANKS; ++t)
+                if (has[r]) sums[wave][r][t][lane] = sum[r][t];
+        __syncthreads();
+        if (!(adapters.lanes >> (16u * wave) & 0xFFFFu)) continue;
+#pragma unroll
         for (uint32_t i = 0; i < 4u; ++i) {
-            const uint32_t n = 4u * g + i;
-            if (__shfl(id, n) != int32_t(one)) continue;
-            const float scale = p.x_scales ? by * p.x_scales[first + n] : by;
+            const uint32_t n = wave * 16u + 4u * g + i;
+            const float scale = by * __shfl(x_scale, n);
+            if (!(adapters.lanes >> n & 1u)) continue;
+#pragma unroll
             for (uint32_t t = 0; t < RANKS; ++t) {
                 const uint32_t rank = (group * RANKS + t) * 16u + c;
-                if (rank < p.rank) p.h[(part * p.rows + first + n) * p.rank_room + rank] = scale * sum[t][i];
+                const float all = (sums[0][wave][t][lane][i] + sums[1][wave][t][lane][i]) + (sums[2][wave][t][lane][i] + sums[3][wave][t][lane][i]);
+                if (rank < p.rank) p.h[(part * p.rows + first + n) * p.rank_room + rank] = scale * all;
             }
         }
-    });
+    }
 }
 
 // The nearest bf16 (of a number that would become infinite the one below it, so that what is left is a number).
@@ -157,113 +217,443 @@ __device__ __forceinline__ uint16_t part_of(float h) {
     return !(__builtin_fabsf(h) < 0x1p127f) ? uint16_t(__builtin_bit_cast(uint32_t, h) >> 16) | (h != h ? 0x40u : 0u) : to_bf16(h);
 }
 
-// 64 columns a wavefront, 16 * TILES rows a workgroup.  In the instructions' terms b's rows are the rows, in an order that leaves each lane with 16
-// consecutive columns of its row.
-template <uint32_t TILES>
-__global__ __launch_bounds__(256) void adapt_up_kernel(AdaptParams p) {
-    extern __shared__ __attribute__((aligned(16))) uint16_t terms_of_h[];                           // [row][term][block][8], 8 more behind a row
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
-    const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
-    const uint64_t first = uint64_t(tile) * (16u * TILES), from = uint64_t(piece) * 256u + wave * 64u;
-    const uint32_t steps = (p.blocks * p.terms + 3u) / 4u, width = steps * 32u + 8u;
-    const int32_t id = id_of(p, first + (lane & (16u * TILES - 1u)), piece == 0u && wave == 0u && lane < 16u * TILES);
-    for (uint32_t n = threadIdx.x; n < 16u * TILES * steps * 32u; n += 256u) {
-        const uint32_t r = n / (steps * 32u), at = n - r * (steps * 32u), block = at / 8u, term = block / p.blocks, rank = (block - term * p.blocks) * 8u + (at & 7u);
-        float h = 0.0f;
-        if (first + r < p.rows && rank < p.rank && term < p.terms) {
-            const int32_t own = p.ids[first + r];
-            if (own >= 0 && uint32_t(own) < p.adapters)
-                for (uint32_t s = 0; s < p.parts; ++s) h += p.h[(s * p.rows + first + r) * p.rank_room + rank];
-            for (uint32_t t = 0; t < term; ++t) h = __builtin_fabsf(h) < __builtin_inff() ? h - bf16_low(part_of(h)) : 0.0f;
+// Block `block` of a row's terms, [term][block][8] behind `to`: the parts of k added up, in all terms; the blocks behind all of them are zeros.
+__device__ __forceinline__ void write_terms(const AdaptParams& p, uint64_t row, uint32_t block, uint16_t* to) {
+    if (block >= p.blocks && block < p.blocks * p.terms) return;
+    float h[8] = {};
+    if (block < p.blocks && block * 8u < p.rank && row < p.rows && uint32_t(p.ids[row]) < p.adapters) {
+        const float* const from = p.h + row * p.rank_room + block * 8u;
+        const uint64_t apart = p.rows * p.rank_room;
+        // (four under way together; behind the last one it is read again, and not added)
+        for (uint32_t s = 0; s < p.parts; s += 4u) {
+            floatx4 lo[4], hi[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) {
+                const float* at = from + (s + i < p.parts ? s + i : p.parts - 1u) * apart;
+                lo[i] = reinterpret_cast<const floatx4*>(at)[0];
+                hi[i] = reinterpret_cast<const floatx4*>(at)[1];
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+                for (uint32_t n = 0; n < 4u; ++n) {
+                    h[n] += s + i < p.parts ? lo[i][n] : 0.0f;
+                    h[n + 4u] += s + i < p.parts ? hi[i][n] : 0.0f;
+                }
         }
-        terms_of_h[r * width + at] = part_of(h);
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) h[i] = block * 8u + i < p.rank ? h[i] : 0.0f;
     }
-    __syncthreads();
-    if (from >= p.cols) return;
-    int32_t own[TILES];
-    for (uint32_t r = 0; r < TILES; ++r) own[r] = __shfl(id, r * 16u + c);
-    floatx4 sum[TILES][4] = {};
-    each_adapter(id, 16u * TILES, [&](uint32_t one, uint64_t lanes) __attribute__((always_inline)) {
-        floatx4 part[TILES][4] = {};
-        const uint16_t* b[4];
-        for (uint32_t t = 0; t < 4u; ++t) b[t] = p.b + one * p.b_stride + least(from + (c >> 2) * 16u + t * 4u + (c & 3u), p.cols - 1u) * p.b_row_stride;
-        for (uint32_t s = 0; s < steps; ++s) {
-            const uint32_t block = (s * 4u + g) % p.blocks * 8u, there = block < p.rank ? p.rank - block : 0u;
-            Eight<ANSZP_OUT_BF16> w[4];
-            for (uint32_t t = 0; t < 4u; ++t) w[t].load(b[t], block, there);
-            for (uint32_t r = 0; r < TILES; ++r) {
-                if (!(lanes >> (16u * r) & 0xFFFFu)) continue;
-                const bf16x8 h = *reinterpret_cast<const bf16x8*>(terms_of_h + (r * 16u + c) * width + s * 32u + g * 8u);
-                for (uint32_t t = 0; t < 4u; ++t) part[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w[t].w), h, part[r][t], 0, 0, 0);
+    for (uint32_t term = 0; term < (block < p.blocks ? p.terms : 1u); ++term) {
+        words4 w;
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            const uint16_t part = part_of(h[i]);
+            w[i >> 1] = i & 1u ? w[i >> 1] | uint32_t(part) << 16 : part;
+            h[i] = __builtin_fabsf(h[i]) < __builtin_inff() ? h[i] - bf16_low(part) : 0.0f;
+        }
+        *reinterpret_cast<words4*>(to + (term * p.blocks + block) * 8u) = w;
+    }
+}
+
+// ... of 64 rows to LDS, 16 bytes more a row.
+__device__ __forceinline__ void terms_to_lds(const AdaptParams& p, uint64_t first, uint16_t* to) {
+    for (uint32_t n = threadIdx.x; n < 64u * (p.width / 8u); n += 256u) write_terms(p, first + (n & 63u), n >> 6, to + (n & 63u) * (p.width + 8u));
+}
+
+// 8 consecutive elements of an operand that has as many in a row.
+template <uint32_t DTYPE>
+__device__ __forceinline__ Eight<DTYPE> eight(const void* base, uint64_t at) {
+    Eight<DTYPE> to;
+    const uint8_t* const from = static_cast<const uint8_t*>(base) + at * (DTYPE == ANSZP_OUT_BF16 ? 2u : 4u);
+    if constexpr (DTYPE == ANSZP_OUT_BF16) {
+        to.w = *reinterpret_cast<const words4_any*>(from);
+    } else {
+        to.w[0] = *reinterpret_cast<const words4_any*>(from);
+        to.w[1] = *reinterpret_cast<const words4_any*>(from + 16);
+    }
+    return to;
+}
+// The 8 columns that a lane with the ones from `col` on works at: where fewer are left the last 8 of the row, of which it stores its own.
+struct Eighth {
+    uint64_t at;
+    uint32_t skip;                      // columns that are another lane's, 8: all are
+    __device__ __forceinline__ Eighth(uint64_t col, uint64_t cols) : at(least(col, cols - 8u)), skip(col < cols ? uint32_t(col - at) : 8u) {}
+};
+template <uint32_t BASE, uint32_t OUT>
+__device__ __forceinline__ void finish(const AdaptParams& p, uint64_t row, const Eighth& cols, const Eight<BASE>& base, const Eight<OUT>& beside, bool adds, const float (&sum)[8]) {
+    float v[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) v[i] = adds ? base[i] + sum[i] : base[i];
+    const auto each = [&](uint32_t activation) __attribute__((always_inline)) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) v[i] = activated(v[i], activation);
+    };
+    switch (p.activation) {                                         // (once for the eight, not for each)
+        case ANSZP_FN_RELU: each(ANSZP_FN_RELU); break;
+        case ANSZP_FN_GELU: each(ANSZP_FN_GELU); break;
+        case ANSZP_FN_SILU: each(ANSZP_FN_SILU); break;
+        default: break;
+    }
+    if (p.mul) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) v[i] *= beside[i];
+    }
+    if (p.residual) {
+        if (p.mul) {
+            const Eight<OUT> residual = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) v[i] += residual[i];
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) v[i] += beside[i];
+        }
+    }
+    const uint64_t at = row * p.out_stride + cols.at;
+    if (cols.skip == 0u) {
+        store_eight(p.out, OUT, at, 8u, v);
+        return;
+    }
+#pragma unroll
+    for (uint32_t i = 1; i < 8u; ++i) {
+        if (i < cols.skip) continue;
+        if constexpr (OUT == ANSZP_OUT_BF16) static_cast<uint16_t*>(p.out)[at + i] = to_bf16(v[i]);
+        else static_cast<float*>(p.out)[at + i] = v[i];
+    }
+}
+// Eight ranks of a row of b: block `block` of it.
+template <bool WHOLE>
+__device__ __forceinline__ words4 ranks_of(const AdaptParams& p, const uint16_t* row, uint32_t block) {
+    const uint8_t* const at = reinterpret_cast<const uint8_t*>(row + block * 8u);
+    if constexpr (WHOLE) return *reinterpret_cast<const words4_any*>(at);
+    else return careful(at, 2 * (int32_t(p.rank) - int32_t(block) * 8), p.b_last);
+}
+// Steps of the second product, each of four blocks of ranks; short terms share one.
+template <uint32_t OUT>
+__device__ __forceinline__ uint32_t steps_of(const AdaptParams& p) {
+    return p.blocks < 4u ? (p.blocks * (OUT == ANSZP_OUT_BF16 ? 2u : 3u) + 3u) / 4u : p.blocks / 4u;
+}
+__device__ __forceinline__ uint32_t block_of(const AdaptParams& p, uint32_t step, uint32_t g) { return p.blocks < 4u ? g & (p.blocks - 1u) : step * 4u + g; }
+
+// The ids of a tile's rows, one a lane; rows that are not there have the last one's.
+__device__ __forceinline__ int32_t tile_ids(const AdaptParams& p, uint64_t first, bool tells) {
+    const uint64_t row = first + (threadIdx.x & 63u);
+    return id_of(p, least(row, p.rows - 1u), tells && row < p.rows);
+}
+
+// The parts of k added up and h's terms, [row][term][block][8] with zeros where there is none, for many rows; a block a thread.
+__global__ __launch_bounds__(256) void adapt_terms_kernel(AdaptParams p) {
+    const uint32_t room = p.width / 8u;
+    const uint64_t n = uint64_t(blockIdx.x) * 256u + threadIdx.x, row = n / room;
+    const uint32_t block = uint32_t(n - row * room);
+    if (row < p.rows) write_terms(p, row, block, p.terms_of_h + row * p.width);
+}
+
+// Many rows: 16 of them and 128 columns a wavefront, 64 of them a workgroup, which has b's rows of its columns in LDS.  In the instructions' terms h's rows are the rows and
+// every eighth of b's a column, so that a lane ends up with 8 consecutive columns of four rows and 16 lanes with a row's 128: operands and results move 256
+// bytes of a row (of bf16) at a time.
+template <uint32_t BASE, uint32_t OUT, bool WHOLE>
+__global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 || OUT == ANSZP_OUT_BF16 ? 3 : 2) void adapt_up_kernel(AdaptParams p) {
+    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u;
+    extern __shared__ __attribute__((aligned(16))) uint16_t b_rows[];                              // [column / 8 in steps of 8][block][8], 8 more behind a row
+    const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4, wave = threadIdx.x >> 6;
+    const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
+    const uint64_t top = uint64_t(tile) * 64u, first = least(top + wave * 16u, p.rows - 1u);
+    const int32_t id = tile_ids(p, top, piece == 0u && wave == 0u);
+    const Eighth cols(uint64_t(piece) * 128u + c * 8u, p.cols);
+    const uint32_t rows = uint32_t(least(p.rows - top, 64u)), steps = steps_of<OUT>(p), width = p.blocks * 8u + 8u;
+    const uint16_t* const h_at = p.terms_of_h + least(first + c, p.rows - 1u) * p.width + g * 8u;
+    uint64_t left = ~0ull >> (64u - rows);
+    bool staged = false;
+    while (left) {
+        const int32_t one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const uint64_t same = __ballot(id == one) & left;
+        const uint32_t mine = uint32_t(same >> (wave * 16u)) & 0xFFFFu;
+        left &= ~same;
+        // (a turn works out its addresses itself: the compiler would do it once, for the turns that hardly ever come, and keep 40 registers for them)
+        uint32_t row_of = wave * 16u + 4u * g, thread = threadIdx.x;
+        asm volatile("" : "+v"(row_of), "+v"(thread));
+        // (out may be one of the operands, so what a row has is asked for before anything of it is stored)
+        Eight<BASE> base[4];
+        Eight<OUT> beside[4];
+        if (mine) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) {
+                const uint64_t row = least(top + row_of + i, p.rows - 1u);
+                base[i] = eight<BASE>(p.base, row * p.base_stride + cols.at);
+                if (p.mul) beside[i] = eight<OUT>(p.mul, row * p.mul_stride + cols.at);
+                else if (p.residual) beside[i] = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
             }
         }
-        for (uint32_t r = 0; r < TILES; ++r)
-            for (uint32_t t = 0; t < 4u; ++t) sum[r][t] = own[r] == int32_t(one) ? part[r][t] : sum[r][t];
-    });
-    for (uint32_t r = 0; r < TILES; ++r) {
-        const uint64_t row = first + r * 16u + c;
-        if (row >= p.rows) continue;
-        for (uint32_t half = 0; half < 2u; ++half) {
-            const uint64_t col = from + g * 16u + half * 8u;
-            if (col >= p.cols) continue;
-            const uint32_t there = p.cols - col < 8u ? uint32_t(p.cols - col) : 8u;
-            Some<8u> base, mul, residual;
-            base.load(p.base, p.base_dtype, row * p.base_stride + col, there);
-            if (p.mul) mul.load(p.mul, p.out_dtype, row * p.mul_stride + col, there);
-            if (p.residual) residual.load(p.residual, p.out_dtype, row * p.residual_stride + col, there);
-            float v[8];
-            for (uint32_t i = 0; i < 8u; ++i) {
-                v[i] = base.at(p.base_dtype, i);
-                if (own[r] >= 0) v[i] += sum[r][half * 2u + (i >> 2)][i & 3u];
-                v[i] = activated(v[i], p.activation);
-                if (p.mul) v[i] *= mul.at(p.out_dtype, i);
-                if (p.residual) v[i] += residual.at(p.out_dtype, i);
+        floatx4 sum[8] = {};
+        if (one >= 0) {
+            if (staged) __syncthreads();
+            staged = true;
+            const uint16_t* const b = p.b + uint64_t(one) * p.b_stride;
+            for (uint32_t n = thread; n < 128u * p.blocks; n += 1024u) {
+                words4 w[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i) {
+                    const uint32_t at = n + i * 256u, j = at / p.blocks, block = at - j * p.blocks;
+                    if (at < 128u * p.blocks) w[i] = ranks_of<WHOLE>(p, b + (least(uint64_t(piece) * 128u + (j & ~7u), p.cols - 8u) + (j & 7u)) * p.b_row_stride, block);
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i) {
+                    const uint32_t at = n + i * 256u, j = at / p.blocks, block = at - j * p.blocks;
+                    if (at < 128u * p.blocks) *reinterpret_cast<words4*>(b_rows + ((j & 7u) * 16u + (j >> 3)) * width + block * 8u) = w[i];
+                }
             }
-            store_eight(p.out, p.out_dtype, row * p.out_stride + col, there, v);
+            __syncthreads();
+            if (mine) {
+                for (uint32_t s = 0; s < steps; ++s) {
+                    const uint16_t* const b_at = b_rows + c * width + block_of(p, s, g) * 8u;
+                    const auto multiply = [&](uint32_t behind) __attribute__((always_inline)) {
+                        const bf16x8 h = as_bf16(*reinterpret_cast<const words4*>(h_at + s * 32u + behind));
+#pragma unroll
+                        for (uint32_t t = 0; t < 8u; ++t)
+                            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, *reinterpret_cast<const bf16x8*>(b_at + t * 16u * width), sum[t], 0, 0, 0);
+                    };
+                    multiply(0u);
+                    if (p.blocks < 4u) continue;
+#pragma unroll
+                    for (uint32_t u = 1; u < kTerms; ++u) multiply(u * p.blocks * 8u);
+                }
+            }
+        }
+        if (!mine || cols.skip == 8u) continue;
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            if (!(mine >> (4u * g + i) & 1u)) continue;
+            const float v[8] = {sum[0][i], sum[1][i], sum[2][i], sum[3][i], sum[4][i], sum[5][i], sum[6][i], sum[7][i]};
+            finish<BASE, OUT>(p, top + row_of + i, cols, base[i], beside[i], one >= 0, v);
         }
     }
 }
 
+// Few rows: 64 of them and 32 columns a workgroup, whose wavefronts have every fourth of the rows' adapters, with the rows they are of.  In the instructions'
+// terms b's rows are the rows, in an order that leaves each lane with 8 consecutive columns of its row.  Four pieces of adapters are under way, so that a wavefront
+// waits for memory once, not for each.
+template <uint32_t BASE, uint32_t OUT, bool WHOLE>
+__global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
+    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u;
+    extern __shared__ __attribute__((aligned(16))) uint16_t terms_of_h[];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
+    const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
+    const uint64_t first = uint64_t(tile) * 64u;
+    const int32_t id = tile_ids(p, first, piece == 0u && wave == 0u);
+    uint32_t of_wave = lane & 3u;                                   // (rows without an adapter are anyone's)
+    {
+        uint32_t turn = 0u;
+        Adapters adapters(id);
+        while (adapters.next() >= 0) {
+            if (adapters.lanes >> lane & 1u) of_wave = turn & 3u;
+            ++turn;
+        }
+    }
+    // A piece of an adapter: four blocks of its ranks.
+    struct Piece {
+        words4 b[2];
+        int32_t one;
+        uint32_t s;
+        uint64_t lanes;
+    } ring[4];
+    const uint32_t steps = steps_of<OUT>(p);
+    const Eighth cols(uint64_t(piece) * 32u + g * 8u, p.cols), cols_of_b(uint64_t(piece) * 32u + (c >> 2) * 8u, p.cols);
+    const uint16_t* const b_at = p.b + (cols_of_b.at + (c & 3u)) * p.b_row_stride;
+    Adapters adapters(of_wave == wave ? id : -1);
+    int32_t asked = -1;
+    uint32_t asked_at = steps;
+    const auto ask = [&](Piece& to) __attribute__((always_inline)) {
+        if (++asked_at >= steps) {
+            asked = adapters.next();
+            asked_at = 0u;
+        }
+        to.one = asked;
+        to.s = asked_at;
+        to.lanes = adapters.lanes;
+        if (asked < 0) return;
+#pragma unroll
+        for (uint32_t t = 0; t < 2u; ++t) to.b[t] = ranks_of<WHOLE>(p, b_at + uint64_t(asked) * p.b_stride + t * 4u * p.b_row_stride, block_of(p, asked_at, g));
+    };
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) ask(ring[i]);
+    int32_t own[4];
+    bool mine[4];
+    Eight<BASE> base[4];
+    Eight<OUT> beside[4];
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r) {
+        const uint64_t row = least(first + r * 16u + c, p.rows - 1u);
+        own[r] = __shfl(id, r * 16u + c);
+        mine[r] = __shfl(of_wave, r * 16u + c) == wave && first + r * 16u + c < p.rows;
+        base[r] = eight<BASE>(p.base, row * p.base_stride + cols.at);
+        if (p.mul) beside[r] = eight<OUT>(p.mul, row * p.mul_stride + cols.at);
+        else if (p.residual) beside[r] = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
+    }
+    terms_to_lds(p, first, terms_of_h);
+    // (out may be one of the operands: what another wavefront stores has been read by all behind this, too)
+    __syncthreads();
+    const uint16_t* const h_at = terms_of_h + c * (p.width + 8u) + g * 8u;
+    floatx4 sum[4][2] = {}, part[4][2] = {};
+    for (bool more = true; more;) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            Piece& now = ring[i];
+            if (now.one < 0) {
+                more = false;
+                break;
+            }
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r) {
+                if (!(now.lanes >> (16u * r) & 0xFFFFu)) continue;
+                const auto multiply = [&](uint32_t behind) __attribute__((always_inline)) {
+                    const bf16x8 h = *reinterpret_cast<const bf16x8*>(h_at + r * 16u * (p.width + 8u) + now.s * 32u + behind);
+#pragma unroll
+                    for (uint32_t t = 0; t < 2u; ++t) part[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(now.b[t]), h, part[r][t], 0, 0, 0);
+                };
+                multiply(0u);
+                if (p.blocks >= 4u) {
+#pragma unroll
+                    for (uint32_t u = 1; u < kTerms; ++u) multiply(u * p.blocks * 8u);
+                }
+            }
+            if (now.s + 1u == steps) {
+#pragma unroll
+                for (uint32_t r = 0; r < 4u; ++r)
+#pragma unroll
+                    for (uint32_t t = 0; t < 2u; ++t) {
+                        sum[r][t] = own[r] == now.one ? part[r][t] : sum[r][t];
+                        part[r][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                    }
+            }
+            ask(now);
+        }
+    }
+    if (cols.skip == 8u) return;
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r) {
+        if (!mine[r]) continue;
+        const float v[8] = {sum[r][0][0], sum[r][0][1], sum[r][0][2], sum[r][0][3], sum[r][1][0], sum[r][1][1], sum[r][1][2], sum[r][1][3]};
+        finish<BASE, OUT>(p, first + r * 16u + c, cols, base[r], beside[r], own[r] >= 0, v);
+    }
+}
+
+// Operands of fewer than 16 bytes, and rows of fewer than 8 columns: an element a thread.
+template <bool BYTES>
+__global__ __launch_bounds__(256) void adapt_down_any_kernel(AdaptParams p) {
+    const uint64_t n = uint64_t(blockIdx.x) * 256u + threadIdx.x, row = n / p.rank;
+    const uint32_t rank = uint32_t(n - row * p.rank);
+    if (row >= p.rows) return;
+    const int32_t one = id_of(p, row, false);
+    if (one < 0) return;
+    float sum = 0.0f;
+    for (uint32_t i = 0; i < p.k; ++i) {
+        const uint8_t* const x = p.x + row * p.x_stride;
+        const float v = BYTES ? float(reinterpret_cast<const int8_t*>(x)[i]) : bf16_low(reinterpret_cast<const uint16_t*>(x)[i]);
+        sum = fmaf(v, bf16_low(p.a[uint64_t(one) * p.a_stride + rank * p.a_row_stride + i]), sum);
+    }
+    p.h[row * p.rank_room + rank] = (p.scales ? p.scales[one] : 1.0f) * (p.x_scales ? p.x_scales[row] : 1.0f) * sum;
+}
+template <uint32_t BASE, uint32_t OUT>
+__global__ __launch_bounds__(256) void adapt_up_any_kernel(AdaptParams p) {
+    const uint64_t n = uint64_t(blockIdx.x) * 256u + threadIdx.x, row = n / p.cols, col = n - row * p.cols;
+    if (row >= p.rows) return;
+    const int32_t one = id_of(p, row, col == 0u);
+    const auto value = [](const void* at, uint32_t dtype, uint64_t i) __attribute__((always_inline)) {
+        return dtype == ANSZP_OUT_BF16 ? bf16_low(static_cast<const uint16_t*>(at)[i]) : static_cast<const float*>(at)[i];
+    };
+    float v = 0.0f;
+    if (one >= 0)
+        for (uint32_t i = 0; i < p.rank; ++i) {
+            float h = 0.0f;
+            for (uint32_t s = 0; s < p.parts; ++s) h += p.h[(s * p.rows + row) * p.rank_room + i];
+            v = fmaf(h, bf16_low(p.b[uint64_t(one) * p.b_stride + col * p.b_row_stride + i]), v);
+        }
+    const float base = value(p.base, BASE, row * p.base_stride + col);
+    v = activated(one >= 0 ? base + v : base, p.activation);
+    if (p.mul) v *= value(p.mul, OUT, row * p.mul_stride + col);
+    if (p.residual) v += value(p.residual, OUT, row * p.residual_stride + col);
+    if constexpr (OUT == ANSZP_OUT_BF16) static_cast<uint16_t*>(p.out)[row * p.out_stride + col] = to_bf16(v);
+    else static_cast<float*>(p.out)[row * p.out_stride + col] = v;
+}
+
 struct Plan {
-    bool rows;                          // a wavefront a tile of rows
     uint32_t ranks;                     // 16s of ranks a workgroup has
-    uint32_t slots, groups, parts;
-    uint64_t workspace;
+    uint32_t slots, groups, parts, blocks, terms, width;
+    bool few, any_down, any_up;         // few rows; operands too short for the kernels of tiles
+    uint64_t sums, workspace;           // bytes of the sums of k's parts, of all
 };
 
 int adapt_check(const anszp_adapt_args_t& a) {
     if ((a.x_dtype != ANSZP_OUT_BF16 && a.x_dtype != ANSZP_I8) || (a.base_dtype != ANSZP_OUT_F32 && a.base_dtype != ANSZP_OUT_BF16) ||
-        (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || a.activation > ANSZP_FN_SILU || a.k == 0 || a.k > 1u << 30 || a.rank == 0 || a.rank > 256u ||
+        (a.out_dtype != ANSZP_OUT_F32 && a.out_dtype != ANSZP_OUT_BF16) || a.activation > ANSZP_FN_SILU || a.k == 0 || a.k > 1u << 30 || a.rank == 0 || a.rank > 128u ||
         a.rows >= 1ull << 28 || a.cols >= 1ull << 31 || a.adapters >= 1u << 24)
         return ANSZP_E_RANGE;
     if (a.rows > 1 && a.out_stride < a.cols) return ANSZP_E_RANGE;
     return ANSZP_OK;
 }
 
+// Bytes from an operand's first element to its last.
+uint64_t bytes_of_x(const anszp_adapt_args_t& a) { return ((a.rows > 1 ? (a.rows - 1u) * a.x_stride : 0u) + a.k) * (a.x_dtype == ANSZP_I8 ? 1u : 2u); }
+uint64_t bytes_of(const anszp_adapt_args_t& a, uint64_t stride, uint64_t rows, uint64_t row_stride, uint64_t width) {
+    return a.adapters ? ((a.adapters > 1u ? (a.adapters - 1ull) * stride : 0u) + (rows > 1u ? (rows - 1u) * row_stride : 0u) + width) * 2u : 0u;
+}
+
 Plan plan_of(const anszp_adapt_args_t& a) {
     Plan q = {};
-    if (a.adapters == 0u) return q;
-    const uint32_t tiles = static_cast<uint32_t>((a.rows + 15u) / 16u), steps = (a.k + 63u) / 64u, sixteens = (a.rank + 15u) / 16u;
+    if (a.adapters == 0u) {
+        q.blocks = q.terms = 1u;
+        q.width = 32u;
+        return q;
+    }
+    const uint32_t tiles = static_cast<uint32_t>((a.rows + 63u) / 64u), steps = (a.k + 63u) / 64u, sixteens = (a.rank + 15u) / 16u;
     q.ranks = sixteens <= 1u ? 1u : sixteens <= 2u ? 2u : 4u;
     q.groups = (sixteens + q.ranks - 1u) / q.ranks;
-    q.rows = tiles >= 64u;
-    q.slots = q.rows ? 1u : static_cast<uint32_t>(a.rows < 16u ? a.rows : 16u);
+    // (a step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose turn does not come leave at once)
+    const uint32_t likely = a.rows < 512u ? static_cast<uint32_t>(a.rows < 64u ? a.rows : 64u) : 1u;
+    q.slots = a.rows < 512u ? likely : a.rows < 4096u ? 8u : 2u;
     if (q.slots > a.adapters) q.slots = a.adapters;
-    const uint32_t groups = (q.rows ? (tiles + 3u) / 4u : tiles * q.slots) * q.groups, most = q.rows ? (steps + 3u) / 4u : (steps + 7u) / 8u;
+    const uint32_t groups = tiles * (likely < q.slots ? likely : q.slots) * q.groups, most = (steps + 7u) / 8u;
     q.parts = (2u * device_cus() + groups - 1u) / groups;
     if (q.parts > 16u) q.parts = 16u;
     if (q.parts > most) q.parts = most;
-    q.workspace = (q.parts * a.rows * ((a.rank + 7u) / 8u * 8u) * 4u + 15u) & ~15ull;
+    q.any_down = bytes_of_x(a) < 16u || bytes_of(a, a.a_stride, a.rank, a.a_row_stride, a.k) < 16u;
+    q.any_up = a.cols < 8u || bytes_of(a, a.b_stride, a.cols, a.b_row_stride, a.rank) < 16u;
+    if (q.any_down) q.parts = 1u;
+    const uint32_t blocks = (a.rank + 7u) / 8u;
+    q.few = q.any_up || (a.rows <= 256u && a.adapters >= 4u);
+    q.terms = a.out_dtype == ANSZP_OUT_BF16 ? 2u : 3u;
+    q.blocks = blocks <= 2u ? blocks : (blocks + 3u) / 4u * 4u;     // (a step of the second product has four blocks: of one term, or of several short ones)
+    q.width = (q.blocks * q.terms + 3u) / 4u * 32u;
+    q.sums = (q.parts * a.rows * blocks * 32u + 15u) & ~15ull;
+    q.workspace = q.sums + (q.few ? 0u : a.rows * q.width * 2u);
     return q;
 }
 
-template <bool BYTES, bool ROWS>
+template <bool BYTES>
 void launch_down(const AdaptParams& p, const Plan& q, hipStream_t s) {
-    const uint32_t tiles = static_cast<uint32_t>((p.rows + 15u) / 16u);
-    const dim3 grid(ROWS ? (tiles + 3u) / 4u : tiles, q.slots * q.groups, q.parts), threads(256);
-    if (q.ranks == 1u) hipLaunchKernelGGL((adapt_down_kernel<BYTES, ROWS, 1u>), grid, threads, 0, s, p);
-    else if (q.ranks == 2u) hipLaunchKernelGGL((adapt_down_kernel<BYTES, ROWS, 2u>), grid, threads, 0, s, p);
-    else hipLaunchKernelGGL((adapt_down_kernel<BYTES, ROWS, 4u>), grid, threads, 0, s, p);
+    if (q.any_down) {
+        hipLaunchKernelGGL(adapt_down_any_kernel<BYTES>, dim3(static_cast<uint32_t>((p.rows * p.rank + 255u) / 256u)), dim3(256), 0, s, p);
+        return;
+    }
+    const dim3 grid(static_cast<uint32_t>((p.rows + 63u) / 64u), q.slots * q.groups, q.parts), threads(256);
+    if (q.ranks == 1u) hipLaunchKernelGGL((adapt_down_kernel<BYTES, 1u>), grid, threads, 0, s, p);
+    else if (q.ranks == 2u) hipLaunchKernelGGL((adapt_down_kernel<BYTES, 2u>), grid, threads, 0, s, p);
+    else hipLaunchKernelGGL((adapt_down_kernel<BYTES, 4u>), grid, threads, 0, s, p);
+}
+
+template <uint32_t BASE, uint32_t OUT, bool WHOLE>
+void launch_up(AdaptParams& p, bool few, hipStream_t s) {
+    const uint32_t tiles = static_cast<uint32_t>((p.rows + 63u) / 64u);
+    p.across = static_cast<uint32_t>(few ? (p.cols + 31u) / 32u : (p.cols + 127u) / 128u);
+    if (few) hipLaunchKernelGGL((adapt_up_few_kernel<BASE, OUT, WHOLE>), dim3(p.across * tiles), dim3(256), 64u * (p.width + 8u) * 2u, s, p);
+    else hipLaunchKernelGGL((adapt_up_kernel<BASE, OUT, WHOLE>), dim3(p.across * tiles), dim3(256), 128u * (p.blocks * 8u + 8u) * 2u, s, p);
+}
+template <uint32_t BASE, uint32_t OUT>
+void launch_up(AdaptParams& p, bool any, bool few, hipStream_t s) {
+    if (any) hipLaunchKernelGGL((adapt_up_any_kernel<BASE, OUT>), dim3(static_cast<uint32_t>((p.rows * p.cols + 255u) / 256u)), dim3(256), 0, s, p);
+    else if (p.rank % (p.blocks < 4u ? 8u : 32u) == 0u) launch_up<BASE, OUT, true>(p, few, s);          // (no block of ranks ends early)
+    else launch_up<BASE, OUT, false>(p, few, s);
 }
 
 }  // namespace
@@ -287,7 +677,7 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
         meet(out, {a->a, 1, 0, ((a->adapters - 1ull) * a->a_stride + (a->rank - 1ull) * a->a_row_stride + a->k) * (a->adapters ? 2u : 0u)}) ||
         meet(out, {a->b, 1, 0, ((a->adapters - 1ull) * a->b_stride + (a->cols - 1ull) * a->b_row_stride + a->rank) * (a->adapters ? 2u : 0u)}))
         return ANSZP_E_RANGE;
-    if ((a->rows + 15u) / 16u * ((a->cols + 255u) / 256u) >= 1ull << 24) return ANSZP_E_RANGE;          // (threads that one launch has not)
+    if ((a->rows + 63u) / 64u * ((a->cols + 31u) / 32u) >= 1ull << 24) return ANSZP_E_RANGE;          // (threads that one launch has not)
     const Plan q = plan_of(*a);
     if (q.workspace && !a->workspace) return ANSZP_E_NULL;
     if (q.workspace && (a->workspace_bytes < q.workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u))) return ANSZP_E_RANGE;
@@ -298,21 +688,24 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
     p.x_stride = a->x_stride * x_size; p.a_stride = a->a_stride; p.a_row_stride = a->a_row_stride; p.b_stride = a->b_stride; p.b_row_stride = a->b_row_stride;
     p.base_stride = a->base_stride; p.mul_stride = a->mul_stride; p.residual_stride = a->residual_stride; p.out_stride = a->out_stride;
     p.rows = a->rows; p.cols = a->cols; p.adapters = a->adapters; p.k = a->k; p.rank = a->rank; p.rank_room = (a->rank + 7u) / 8u * 8u;
-    p.base_dtype = a->base_dtype; p.out_dtype = a->out_dtype; p.activation = a->activation;
+    p.activation = a->activation;
     p.slots = q.slots; p.groups = q.groups; p.parts = q.parts;
-    p.across = static_cast<uint32_t>((a->cols + 255u) / 256u);
-    const uint32_t blocks = (a->rank + 7u) / 8u;
-    p.terms = a->out_dtype == ANSZP_OUT_BF16 ? 2u : 3u;
-    p.blocks = blocks <= 2u ? blocks : (blocks + 3u) / 4u * 4u;     // (a step of the second product has four blocks: of one term, or of several short ones)
+    p.blocks = q.blocks; p.terms = q.terms; p.width = q.width;
+    p.x_last = p.x + bytes_of_x(*a) - 16u;
+    p.a_last = reinterpret_cast<const uint8_t*>(p.a) + bytes_of(*a, a->a_stride, a->rank, a->a_row_stride, a->k) - 16u;
+    p.b_last = reinterpret_cast<const uint8_t*>(p.b) + bytes_of(*a, a->b_stride, a->cols, a->b_row_stride, a->rank) - 16u;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (q.workspace) {
-        if (bytes && q.rows) launch_down<true, true>(p, q, s);
-        else if (bytes) launch_down<true, false>(p, q, s);
-        else if (q.rows) launch_down<false, true>(p, q, s);
-        else launch_down<false, false>(p, q, s);
+        p.terms_of_h = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a->workspace) + q.sums);
+        if (bytes) launch_down<true>(p, q, s);
+        else launch_down<false>(p, q, s);
+        if (!q.few) hipLaunchKernelGGL(adapt_terms_kernel, dim3(static_cast<uint32_t>((a->rows * (q.width / 8u) + 255u) / 256u)), dim3(256), 0, s, p);
     }
-    const uint32_t row_bytes = ((p.blocks * p.terms + 3u) / 4u * 32u + 8u) * 2u;
-    if (a->rows >= 1024u && 64u * row_bytes <= 65536u) hipLaunchKernelGGL(adapt_up_kernel<4u>, dim3(p.across * static_cast<uint32_t>((a->rows + 63u) / 64u)), dim3(256), 64u * row_bytes, s, p);
-    else hipLaunchKernelGGL(adapt_up_kernel<1u>, dim3(p.across * static_cast<uint32_t>((a->rows + 15u) / 16u)), dim3(256), 16u * row_bytes, s, p);
+    const bool any = q.any_up || a->cols < 8u;                      // (also where there are no adapters)
+    const bool base_short = a->base_dtype == ANSZP_OUT_BF16, out_short = a->out_dtype == ANSZP_OUT_BF16;
+    if (base_short && out_short) launch_up<ANSZP_OUT_BF16, ANSZP_OUT_BF16>(p, any, q.few, s);
+    else if (base_short) launch_up<ANSZP_OUT_BF16, ANSZP_OUT_F32>(p, any, q.few, s);
+    else if (out_short) launch_up<ANSZP_OUT_F32, ANSZP_OUT_BF16>(p, any, q.few, s);
+    else launch_up<ANSZP_OUT_F32, ANSZP_OUT_F32>(p, any, q.few, s);
     return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
 }

@@ -242,7 +242,7 @@ py::object adapt(const at::Tensor& base, const at::Tensor& x, const at::Tensor& 
     const int64_t rows = base.size(0), cols = base.size(1), k = x.size(1), n = wa.size(0), rank = wa.size(1);
     if (!matrix(x, on, rows, k) || (x.scalar_type() != at::kChar && x.scalar_type() != at::kBFloat16) || wa.device() != on || wb.device() != on ||
         wa.scalar_type() != at::kBFloat16 || wb.scalar_type() != at::kBFloat16 || wa.size(2) != k || wb.size(0) != n || wb.size(1) != cols || wb.size(2) != rank ||
-        !packed(wa) || !packed(wb) || !ints(ids, on, rows) || k >= 1ll << 31 || rank > 256 || n >= 1ll << 24)
+        !packed(wa) || !packed(wb) || !ints(ids, on, rows) || k >= 1ll << 31 || rank > 128 || n >= 1ll << 24)
         return none();
     if (out && (!matrix(*out, on, rows, cols) || !is_float(*out))) return none();
     const at::ScalarType type = out ? out->scalar_type() : out_code == ANSZP_OUT_F32 ? at::kFloat : at::kBFloat16;
