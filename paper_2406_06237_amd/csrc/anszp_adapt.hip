@@ -33,7 +33,7 @@ struct AdaptParams {
     uint64_t x_stride, a_stride, a_row_stride, b_stride, b_row_stride, base_stride, mul_stride, residual_stride, out_stride;    // x's in bytes
     uint64_t rows, cols;
     uint32_t adapters, k, rank, rank_room, activation;
-    uint32_t slots, groups, parts;      // workgroups that share a tile's adapters, groups of ranks, parts of k
+    uint32_t slots, groups, parts;      // workgroups that share a tile's rows, groups of ranks, parts of k
     uint32_t blocks, terms;             // blocks of 8 ranks a term of h has, terms
     uint32_t across, width;             // workgroups that a row's columns take; a row of h's terms
     const uint8_t* x_last;              // where the last 16 bytes of each begin
@@ -64,35 +64,17 @@ __device__ __forceinline__ words4 careful(const uint8_t* at, int32_t there, cons
     return first_bytes(words4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)}, there);
 }
 
-// Sixteen consecutive elements of a row of bf16 or of signed bytes, as two operands.
-template <bool BYTES>
-struct Sixteen {
-    words4 lo, hi;
-    __device__ __forceinline__ void load(const uint8_t* at) {
-        lo = *reinterpret_cast<const words4_any*>(at);
-        if constexpr (!BYTES) hi = *reinterpret_cast<const words4_any*>(at + 16);
-    }
-    // where fewer than 16 are there
-    __device__ __forceinline__ void load(const uint8_t* at, int32_t there, const uint8_t* last) {
-        lo = careful(at, BYTES ? there : 2 * there, last);
-        if constexpr (!BYTES) hi = careful(at + 16, 2 * there - 16, last);
-    }
-    // A whole number below 2^8 in size fits bf16, so the upper half of its binary32 is all of it.
-    __device__ __forceinline__ bf16x8 operand(uint32_t half) const {
-        if constexpr (BYTES) {
-            words4 w;
+// Eight signed bytes as an operand.  A whole number below 2^8 in size fits bf16, so the upper half of its binary32 is all of it.
+__device__ __forceinline__ bf16x8 bf16_of_bytes(words2 bytes) {
+    words4 w;
 #pragma unroll
-            for (uint32_t i = 0; i < 4u; ++i) {
-                const uint32_t four = lo[half * 2u + (i >> 1)], at = 16u * (i & 1u);
-                const float a = float(int32_t(four << (24u - at)) >> 24), b = float(int32_t(four << (16u - at)) >> 24);
-                w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
-            }
-            return as_bf16(w);
-        } else {
-            return as_bf16(half ? hi : lo);
-        }
+    for (uint32_t i = 0; i < 4u; ++i) {
+        const uint32_t four = bytes[i >> 1], at = 16u * (i & 1u);
+        const float lo = float(int32_t(four << (24u - at)) >> 24), hi = float(int32_t(four << (16u - at)) >> 24);
+        w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
     }
-};
+    return as_bf16(w);
+}
 
 __device__ __forceinline__ int32_t id_of(const AdaptParams& p, uint64_t row, bool tells) {
     if (row >= p.rows) return -1;
@@ -120,93 +102,116 @@ struct Adapters {
     }
 };
 
-// h of 64 rows and up to 16 * RANKS ranks; the four wavefronts share a part of k and add up what they have.
+// h of 64 rows and up to 16 * RANKS ranks, 16 rows a wavefront.  128 bytes of each row of x and as much of k of a's rows go to LDS at a time, in pieces of 16 bytes end to
+// end (operands taken from memory as the instructions want them are 16 bytes of 16 rows for every 16 lanes, and a CU looks up four times the lines: 33 us for
+// 8192 rows of 4096 bytes and rank 64, this 20); two times of them are under way beside the one in LDS.
 template <bool BYTES, uint32_t RANKS>
-__global__ __launch_bounds__(256, 2) void adapt_down_kernel(AdaptParams p) {
+__global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
+    constexpr uint32_t kAtOnce = BYTES ? 128u : 64u, kRowOfA = kAtOnce * 2u, kPiecesOfA = RANKS * 16u * kRowOfA / 16u, kEachOfA = (kPiecesOfA + 255u) / 256u;
+    __shared__ __attribute__((aligned(16))) uint8_t xs[2][64][128u + 16u], as[2][16u * RANKS][kRowOfA + 16u];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint32_t slot = blockIdx.y / p.groups, group = blockIdx.y - slot * p.groups, part = blockIdx.z;
     const uint64_t first = uint64_t(blockIdx.x) * 64u;
-    const uint32_t steps = (p.k + 63u) / 64u, share = part * 4u + wave, shares = p.parts * 4u;
-    const uint32_t begin = uint32_t(uint64_t(steps) * share / shares), end = uint32_t(uint64_t(steps) * (share + 1u) / shares);
-    __shared__ floatx4 sums[4][4][RANKS][64];
+    const uint32_t steps = (p.k + kAtOnce - 1u) / kAtOnce, begin = uint32_t(uint64_t(steps) * part / p.parts), end = uint32_t(uint64_t(steps) * (part + 1u) / p.parts);
     const float x_scale = p.x_scales ? p.x_scales[least(first + lane, p.rows - 1u)] : 1.0f;
-    Adapters adapters(id_of(p, first + lane, false));
-    const uint8_t* x[4];
-#pragma unroll
-    for (uint32_t r = 0; r < 4u; ++r) x[r] = p.x + least(first + r * 16u + c, p.rows - 1u) * p.x_stride;
-    for (uint32_t turn = 0;; ++turn) {
-        const int32_t one = adapters.next();
-        if (one < 0) break;
-        if (turn % p.slots != slot) continue;
-        const uint8_t* a[RANKS];
-#pragma unroll
-        for (uint32_t t = 0; t < RANKS; ++t) a[t] = reinterpret_cast<const uint8_t*>(p.a + uint64_t(one) * p.a_stride + least((group * RANKS + t) * 16u + c, p.rank - 1u) * p.a_row_stride);
+    const int32_t id = id_of(p, first + lane, false);
+    // This thread's pieces: of x's rows t / 8 and t / 8 + 32, of a's from t on every 256th.
+    const uint32_t x_row = threadIdx.x >> 3, x_piece = (threadIdx.x & 7u) * 16u;
+    // Few rows: a workgroup for each, which works at the row's adapter if no row before has it.  Else the adapters in turn.
+    uint64_t left = __ballot(id >= 0);
+    uint32_t wait = slot;
+    if (p.slots >= p.rows || p.slots == 64u) {
+        const int32_t one = __builtin_amdgcn_readlane(id, slot);
+        const uint64_t lanes = __ballot(id == one);
+        left = one >= 0 && uint32_t(__builtin_ctzll(lanes)) == slot ? lanes : 0u;
+        wait = 0u;
+    }
+    while (left) {
+        const int32_t one = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const uint64_t lanes = __ballot(id == one);
+        left &= ~lanes;
+        if (wait) {
+            --wait;
+            continue;
+        }
+        wait = p.slots - 1u;
         const float by = p.scales ? p.scales[one] : 1.0f;
-        bool has[4];
+        const uint8_t* x[2];
+        const uint8_t* a[kEachOfA];
+        bool has[2];
 #pragma unroll
-        for (uint32_t r = 0; r < 4u; ++r) has[r] = (adapters.lanes >> (16u * r) & 0xFFFFu) != 0u;
-        floatx4 sum[4][RANKS] = {};
+        for (uint32_t i = 0; i < 2u; ++i) {
+            has[i] = lanes >> (x_row + 32u * i) & 1u;               // (rows of other adapters stay what they were: nothing of theirs is kept)
+            x[i] = p.x + least(first + x_row + 32u * i, p.rows - 1u) * p.x_stride + x_piece;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kEachOfA; ++i) {
+            const uint32_t n = threadIdx.x + i * 256u;
+            a[i] = reinterpret_cast<const uint8_t*>(p.a + uint64_t(one) * p.a_stride + least(group * RANKS * 16u + n / (kRowOfA / 16u), p.rank - 1u) * p.a_row_stride) + n % (kRowOfA / 16u) * 16u;
+        }
         struct Step {
-            Sixteen<BYTES> x[4];
-            Sixteen<false> a[RANKS];
+            words4 x[2], a[kEachOfA];
         } now, then;
         const auto load = [&](Step& to, uint32_t s) __attribute__((always_inline)) {
-            const uint32_t at = s * 64u + g * 16u;
+            if (s * kAtOnce + kAtOnce <= p.k) {
 #pragma unroll
-            for (uint32_t t = 0; t < RANKS; ++t) to.a[t].load(a[t] + at * 2u);
+                for (uint32_t i = 0; i < kEachOfA; ++i) to.a[i] = *reinterpret_cast<const words4_any*>(a[i] + uint64_t(s) * kRowOfA);
 #pragma unroll
-            for (uint32_t r = 0; r < 4u; ++r)
-                if (has[r]) to.x[r].load(x[r] + at * (BYTES ? 1u : 2u));
-        };
-        const auto multiply = [&](const Step& with) __attribute__((always_inline)) {
+                for (uint32_t i = 0; i < 2u; ++i)
+                    if (has[i]) to.x[i] = *reinterpret_cast<const words4_any*>(x[i] + uint64_t(s) * 128u);
+            } else {
+                const int32_t left = int32_t(p.k - s * kAtOnce);
 #pragma unroll
-            for (uint32_t r = 0; r < 4u; ++r) {
-                if (!has[r]) continue;
+                for (uint32_t i = 0; i < kEachOfA; ++i)
+                    to.a[i] = careful(a[i] + uint64_t(s) * kRowOfA, left * 2 - int32_t((threadIdx.x + i * 256u) % (kRowOfA / 16u) * 16u), p.a_last);
 #pragma unroll
-                for (uint32_t half = 0; half < 2u; ++half) {
-                    const bf16x8 xs = with.x[r].operand(half);
-#pragma unroll
-                    for (uint32_t t = 0; t < RANKS; ++t) sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs, with.a[t].operand(half), sum[r][t], 0, 0, 0);
-                }
+                for (uint32_t i = 0; i < 2u; ++i)
+                    if (has[i]) to.x[i] = careful(x[i] + uint64_t(s) * 128u, left * (BYTES ? 1 : 2) - int32_t(x_piece), p.x_last);
             }
         };
-        // (the step in which k ends is one of its own, behind the others)
-        const uint32_t last = end * 64u > p.k ? end - 1u : end;
-        if (begin < last) load(now, begin);
-        for (uint32_t s = begin; s < last; s += 2u) {
-            if (s + 1u < last) load(then, s + 1u);
-            multiply(now);
-            if (s + 2u < last) load(now, s + 2u);
-            if (s + 1u < last) multiply(then);
+        floatx4 sum[RANKS] = {};
+        const bool works = (lanes >> (16u * wave) & 0xFFFFu) != 0u;
+        const auto step = [&](const Step& with, uint32_t s, Step& next) __attribute__((always_inline)) {
+            const uint32_t buffer = (s - begin) & 1u;
+#pragma unroll
+            for (uint32_t i = 0; i < kEachOfA; ++i) {
+                const uint32_t n = threadIdx.x + i * 256u;
+                if (kPiecesOfA % 256u == 0u || n < kPiecesOfA) *reinterpret_cast<words4*>(&as[buffer][n / (kRowOfA / 16u)][n % (kRowOfA / 16u) * 16u]) = with.a[i];
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 2u; ++i)
+                if (has[i]) *reinterpret_cast<words4*>(&xs[buffer][x_row + 32u * i][x_piece]) = with.x[i];
+            __syncthreads();
+            if (s + 2u < end) load(next, s + 2u);
+            if (!works) return;
+#pragma unroll
+            for (uint32_t k = 0; k < kAtOnce; k += 32u) {
+                bf16x8 of_x;
+                if constexpr (BYTES) of_x = bf16_of_bytes(*reinterpret_cast<const words2*>(&xs[buffer][wave * 16u + c][k + g * 8u]));
+                else of_x = as_bf16(*reinterpret_cast<const words4*>(&xs[buffer][wave * 16u + c][(k + g * 8u) * 2u]));
+#pragma unroll
+                for (uint32_t t = 0; t < RANKS; ++t)
+                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(of_x, as_bf16(*reinterpret_cast<const words4*>(&as[buffer][t * 16u + c][(k + g * 8u) * 2u])), sum[t], 0, 0, 0);
+            }
+        };
+        if (begin < end) load(now, begin);
+        if (begin + 1u < end) load(then, begin + 1u);
+        for (uint32_t s = begin; s < end; s += 2u) {
+            step(now, s, now);
+            if (s + 1u < end) step(then, s + 1u, then);
         }
-        if (begin < end && last < end) {
-            const uint32_t at = last * 64u + g * 16u;
-            const int32_t there = int32_t(p.k) - int32_t(at);
-#pragma unroll
-            for (uint32_t t = 0; t < RANKS; ++t) now.a[t].load(a[t] + at * 2u, there, p.a_last);
-#pragma unroll
-            for (uint32_t r = 0; r < 4u; ++r)
-                if (has[r]) now.x[r].load(x[r] + at * (BYTES ? 1u : 2u), there, p.x_last);
-            multiply(now);
-        }
+        // (the next adapter's first step goes to the buffer that this one's last may still be read from)
         __syncthreads();
-#pragma unroll
-        for (uint32_t r = 0; r < 4u; ++r)
-#pragma unroll
-            for (uint32_t t = 0; t < RANKS; ++t)
-                if (has[r]) sums[wave][r][t][lane] = sum[r][t];
-        __syncthreads();
-        if (!(adapters.lanes >> (16u * wave) & 0xFFFFu)) continue;
+        if (!works) continue;
 #pragma unroll
         for (uint32_t i = 0; i < 4u; ++i) {
             const uint32_t n = wave * 16u + 4u * g + i;
             const float scale = by * __shfl(x_scale, n);
-            if (!(adapters.lanes >> n & 1u)) continue;
+            if (!(lanes >> n & 1u)) continue;
 #pragma unroll
             for (uint32_t t = 0; t < RANKS; ++t) {
                 const uint32_t rank = (group * RANKS + t) * 16u + c;
-                const float all = (sums[0][wave][t][lane][i] + sums[1][wave][t][lane][i]) + (sums[2][wave][t][lane][i] + sums[3][wave][t][lane][i]);
-                if (rank < p.rank) p.h[(part * p.rows + first + n) * p.rank_room + rank] = scale * all;
+                if (rank < p.rank) p.h[(part * p.rows + first + n) * p.rank_room + rank] = scale * sum[t][i];
             }
         }
     }
@@ -578,7 +583,7 @@ __global__ __launch_bounds__(256) void adapt_up_any_kernel(AdaptParams p) {
 }
 
 struct Plan {
-    uint32_t ranks;                     // 16s of ranks a workgroup has
+    uint32_t ranks;                     // 16s of ranks a workgroup of the first product has
     uint32_t slots, groups, parts, blocks, terms, width;
     bool few, any_down, any_up;         // few rows; operands too short for the kernels of tiles
     uint64_t sums, workspace;           // bytes of the sums of k's parts, of all
@@ -606,16 +611,16 @@ Plan plan_of(const anszp_adapt_args_t& a) {
         q.width = 32u;
         return q;
     }
-    const uint32_t tiles = static_cast<uint32_t>((a.rows + 63u) / 64u), steps = (a.k + 63u) / 64u, sixteens = (a.rank + 15u) / 16u;
+    const uint32_t tiles = static_cast<uint32_t>((a.rows + 63u) / 64u), steps = a.x_dtype == ANSZP_I8 ? (a.k + 127u) / 128u : (a.k + 63u) / 64u, sixteens = (a.rank + 15u) / 16u;
     q.ranks = sixteens <= 1u ? 1u : sixteens <= 2u ? 2u : 4u;
     q.groups = (sixteens + q.ranks - 1u) / q.ranks;
-    // (a step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose turn does not come leave at once)
-    const uint32_t likely = a.rows < 512u ? static_cast<uint32_t>(a.rows < 64u ? a.rows : 64u) : 1u;
-    q.slots = a.rows < 512u ? likely : a.rows < 4096u ? 8u : 2u;
-    if (q.slots > a.adapters) q.slots = a.adapters;
-    const uint32_t groups = tiles * (likely < q.slots ? likely : q.slots) * q.groups, most = (steps + 7u) / 8u;
+    // A step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose rows are not the first of an adapter leave at once.  k in parts
+    // until there are two workgroups a CU, though h's parts are read again by every workgroup of the second product where rows are few.
+    const uint32_t rows = static_cast<uint32_t>(a.rows < 64u ? a.rows : 64u), likely = a.rows < 512u ? (rows < a.adapters ? rows : a.adapters) : 1u;
+    q.slots = a.rows < 512u ? rows : a.rows < 4096u ? (a.adapters < 8u ? a.adapters : 8u) : a.adapters < 2u ? 1u : 2u;
+    const uint32_t groups = tiles * likely * q.groups, most = (steps + 1u) / 2u, read_again = a.rows <= 4u ? 16u : a.rows <= 16u ? 8u : a.rows <= 256u ? 4u : 16u;
     q.parts = (2u * device_cus() + groups - 1u) / groups;
-    if (q.parts > 16u) q.parts = 16u;
+    if (q.parts > read_again) q.parts = read_again;
     if (q.parts > most) q.parts = most;
     q.any_down = bytes_of_x(a) < 16u || bytes_of(a, a.a_stride, a.rank, a.a_row_stride, a.k) < 16u;
     q.any_up = a.cols < 8u || bytes_of(a, a.b_stride, a.cols, a.b_row_stride, a.rank) < 16u;
