@@ -15,7 +15,7 @@
 
 namespace {
 
-constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64u, kSteps = 64, kBins = 44u * kSteps, kList = 512, kCuts = 1024;
+constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64u, kSteps = 64, kBins = 44u * kSteps, kList = 1024, kCuts = 1024;
 
 struct SampleParams {
     const void* logits;
@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t key_of(float l) {
     const uint32_t w = __builtin_bit_cast(uint32_t, l + 0.0f);
     return w ^ (w >> 31 ? ~0u : 0x80000000u);
 }
-constexpr uint32_t kLowest = 0x007FFFFFu;                           // key_of(-infinity)
+__device__ __forceinline__ float of_key(uint32_t key) { return __builtin_bit_cast(float, key ^ (key >> 31 ? 0x80000000u : ~0u)); }
 
 struct Shared {
     uint64_t mass[kBins + 1u];          // first the sums of q, then the masses before each bin
@@ -46,7 +46,7 @@ struct Shared {
     uint64_t cut_sum[kCuts];
     uint32_t cut_count[kCuts];
     uint32_t list_key[kList], list_id[kList];
-    uint64_t list_q[kList];
+    uint64_t list_q[kList];             // q, or a mass
     uint64_t of_wave[kWaves], of_wave_too[kWaves];
     uint32_t listed, least, most, list_bin;
     uint32_t found, found_id;
@@ -59,12 +59,21 @@ struct Row {
     uint64_t from;
     uint32_t n, point;
     double top, steps;                  // the largest logit, 64 log2(e) / temperature
-    bool infinite;
 
     // work(logit, token) for all tokens; a thread's come in rising order
     template <class Work>
     __device__ __forceinline__ void each(Work work) const {
-        for (uint32_t at = threadIdx.x * 8u; at < n; at += kThreads * 8u) {
+        uint32_t at = threadIdx.x * 8u;
+        for (; at + kThreads * 8u + 8u <= n; at += kThreads * 16u) {                // (two loads under way)
+            Eight<DTYPE> l, m;
+            l.load(logits, from + at, 8u);
+            m.load(logits, from + at + kThreads * 8u, 8u);
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) work(l[i], at + i);
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) work(m[i], at + kThreads * 8u + i);
+        }
+        for (; at < n; at += kThreads * 8u) {
             const uint32_t there = n - at;
             Eight<DTYPE> l;
             l.load(logits, from + at, there);
@@ -73,20 +82,25 @@ struct Row {
                 if (i < there) work(l[i], at + i);
         }
     }
-    // The bin of a logit and its q; false: it weighs nothing.
+    // The bin of a logit and its q; false: it weighs nothing.  (A masked one is infinitely far, or with an infinite temperature no number.)
     __device__ __forceinline__ bool weigh(float l, uint32_t& bin, uint64_t& q) const {
-        double t = (top - double(l)) * steps;
-        if (infinite) t = l == __builtin_inff() ? 0.0 : 1e9;
-        if (!(t < double(kBins) - 0.5) || l == -__builtin_inff()) return false;
+        const double t = (top - double(l)) * steps;
+        if (!(t < double(kBins) - 0.5)) return false;
         constexpr double kWhole = 0x1.8p52, kLn2 = 0.69314718055994530942 / double(kSteps);
-        const double whole = t + kWhole, y = (whole - kWhole - t) * kLn2;
+        const double whole = t + kWhole, y = (whole - kWhole) - t, one = __builtin_bit_cast(double, uint64_t(1023u + point) << 52);
         bin = uint32_t(__builtin_bit_cast(uint64_t, whole));
-        const double one = __builtin_bit_cast(double, uint64_t(1023u + point) << 52);
-        double s = fma(y, 1.0 / 24.0, 1.0 / 6.0);
-        s = fma(y, s, 0.5);
-        s = fma(y, s, 1.0) * y;
-        q = __builtin_bit_cast(uint64_t, fma(s, one, one + 0x1p52)) & 0xFFFFFFFFFFFFFull;
+        // exp(y ln2 / 64) without its 1, times 2^point
+        double s = fma(y, kLn2 * kLn2 * kLn2 * kLn2 / 24.0, kLn2 * kLn2 * kLn2 / 6.0);
+        s = fma(y, s, kLn2 * kLn2 / 2.0);
+        s = fma(y, s, kLn2);
+        q = __builtin_bit_cast(uint64_t, fma(s, y * one, one + 0x1p52)) & 0xFFFFFFFFFFFFFull;
         return true;
+    }
+    // Logits between which those of bins first .. last surely are.
+    __device__ __forceinline__ void reach_of(uint32_t first, uint32_t last, float& lo, float& hi) const {
+        const double low = top - (double(last) + 0.5) / steps, high = top - (double(first) - 0.5) / steps, more = (fabs(top) + fabs(low)) * 0x1p-22 + 1e-30;
+        lo = steps > 1e-300 ? float(low - more) : -__builtin_inff();
+        hi = steps > 1e-300 ? float(high + more) : __builtin_inff();
     }
 };
 
@@ -108,11 +122,48 @@ __device__ __forceinline__ uint64_t added_before(uint64_t v, uint64_t* of_wave) 
     return before;
 }
 
+// The token that is the `nth` (from 1 on) of those with this logit.
+template <uint32_t DTYPE>
+__device__ void find_equal(Shared& sh, const Row<DTYPE>& row, uint32_t key, uint64_t nth) {
+    uint64_t passed = 0u;
+    for (uint32_t from = 0; from < row.n; from += kThreads * 8u) {
+        const uint32_t at = from + threadIdx.x * 8u, there = at < row.n ? row.n - at : 0u;
+        Eight<DTYPE> l;
+        uint32_t mine = 0u;
+        if (there) {
+            l.load(row.logits, row.from + at, there);
+            for (uint32_t i = 0; i < 8u; ++i) mine += i < there && key_of(l[i]) == key ? 1u : 0u;
+        }
+        __syncthreads();
+        uint64_t seen = passed + added_before(mine, sh.of_wave);
+        for (uint32_t w = 0; w < kWaves; ++w) passed += sh.of_wave[w];
+        if (mine)
+            for (uint32_t i = 0; i < 8u; ++i)
+                if (i < there && key_of(l[i]) == key && ++seen == nth) sh.found_id = at + i;
+    }
+    __syncthreads();
+}
+
+// What lies before the list's entry `own` in the order of logits: how many of the n entries, and the sum of what they hold.
+__device__ __forceinline__ void before_in_list(const Shared& sh, uint32_t n, uint32_t own, uint64_t& count, uint64_t& sum) {
+    const uint32_t key = sh.list_key[own], id = sh.list_id[own];
+    uint32_t counted = 0u;
+    for (uint32_t j = 0; j < n; ++j) {
+        const uint32_t other = sh.list_key[j];
+        const bool first = other > key || (other == key && sh.list_id[j] < id);
+        counted += first ? 1u : 0u;
+        sum += first ? sh.list_q[j] : 0u;
+    }
+    count += counted;
+}
+
 // The first token of a bin at which reach(tokens up to it, their sum of q) holds, which it does for the bin as a whole: its number, its q and the sum.
 template <uint32_t DTYPE, class Reach>
-__device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reach) {
+__device__ __forceinline__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reach) {
     uint32_t lo = 0u, hi = ~0u;                                     // the logits looked at, by their keys
     uint64_t before = 0u, sum_before = 0u;                          // what lies above them in the bin
+    float low, high;
+    row.reach_of(bin, bin, low, high);
     for (;;) {
         __syncthreads();
         if (sh.list_bin != bin || sh.listed > kList) {
@@ -125,6 +176,7 @@ __device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reac
             }
             __syncthreads();
             row.each([&](float l, uint32_t id) __attribute__((always_inline)) {
+                if (!(l >= low && l <= high)) return;
                 uint32_t b;
                 uint64_t q;
                 if (!row.weigh(l, b, q) || b != bin) return;
@@ -144,18 +196,11 @@ __device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reac
         const uint32_t n = sh.listed, least = sh.least, most = sh.most;
         if (n <= kList) {
             if (threadIdx.x < n) {
-                const uint32_t key = sh.list_key[threadIdx.x], id = sh.list_id[threadIdx.x];
                 uint64_t count = before, sum = sum_before;
-                for (uint32_t j = 0; j < n; ++j) {
-                    const uint32_t other = sh.list_key[j];
-                    if (other > key || (other == key && sh.list_id[j] < id)) {
-                        ++count;
-                        sum += sh.list_q[j];
-                    }
-                }
+                before_in_list(sh, n, threadIdx.x, count, sum);
                 const uint64_t q = sh.list_q[threadIdx.x];
                 if (!reach(count, sum) && reach(count + 1u, sum + q)) {
-                    sh.found_id = id;
+                    sh.found_id = sh.list_id[threadIdx.x];
                     sh.found_q = q;
                     sh.found_sum = sum + q;
                 }
@@ -167,32 +212,16 @@ __device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reac
         if (least == most) {
             // Equal logits: which of them it is, then where that one is.
             const uint64_t q = sh.list_q[0];
-            uint32_t low = 0u, high = n;                            // reach holds for high of them, not for low
-            while (high - low > 1u) {
-                const uint32_t mid = low + (high - low) / 2u;
-                if (reach(before + mid, sum_before + mid * q)) high = mid;
-                else low = mid;
+            uint32_t under = 0u, over = n;                          // reach holds for `over` of them, not for `under`
+            while (over - under > 1u) {
+                const uint32_t mid = under + (over - under) / 2u;
+                if (reach(before + mid, sum_before + mid * q)) over = mid;
+                else under = mid;
             }
-            uint64_t passed = 0u;
-            for (uint32_t from = 0; from < row.n; from += kThreads * 8u) {
-                const uint32_t at = from + threadIdx.x * 8u, there = at < row.n ? row.n - at : 0u;
-                Eight<DTYPE> l;
-                uint32_t mine = 0u;
-                if (there) {
-                    l.load(row.logits, row.from + at, there);
-                    for (uint32_t i = 0; i < 8u; ++i) mine += i < there && key_of(l[i]) == most ? 1u : 0u;
-                }
-                __syncthreads();
-                const uint64_t ahead = passed + added_before(mine, sh.of_wave);
-                for (uint32_t w = 0; w < kWaves; ++w) passed += sh.of_wave[w];
-                uint64_t seen = ahead;
-                if (mine)
-                    for (uint32_t i = 0; i < 8u; ++i)
-                        if (i < there && key_of(l[i]) == most && ++seen == high) sh.found_id = at + i;
-            }
+            find_equal(sh, row, most, over);
             if (threadIdx.x == 0u) {
                 sh.found_q = q;
-                sh.found_sum = sum_before + high * q;
+                sh.found_sum = sum_before + over * q;
                 sh.list_bin = ~0u;
             }
             __syncthreads();
@@ -206,6 +235,7 @@ __device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reac
         }
         __syncthreads();
         row.each([&](float l, uint32_t) __attribute__((always_inline)) {
+            if (!(l >= low && l <= high)) return;
             uint32_t b;
             uint64_t q;
             if (!row.weigh(l, b, q) || b != bin) return;
@@ -235,119 +265,233 @@ __device__ void find(Shared& sh, const Row<DTYPE>& row, uint32_t bin, Reach reac
     }
 }
 
+// The sums of q (or none) and counts of all bins made into what lies before each.
+__device__ __forceinline__ void add_up_bins(Shared& sh) {
+    constexpr uint32_t kEach = (kBins + kThreads - 1u) / kThreads;
+    uint64_t mass[kEach], masses = 0u, counts = 0u;
+    uint32_t count[kEach];
+    const uint32_t first = threadIdx.x * kEach;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const bool there = first + i < kBins;
+        mass[i] = there ? mass_of(height(first + i), sh.mass[first + i]) : 0u;
+        count[i] = there ? sh.count[first + i] : 0u;
+        masses += mass[i];
+        counts += count[i];
+    }
+    __syncthreads();
+    uint64_t upto = added_before(masses, sh.of_wave), counted = added_before(counts, sh.of_wave_too);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        if (first + i <= kBins) {
+            sh.mass[first + i] = upto;
+            sh.count[first + i] = uint32_t(counted);
+        }
+        upto += mass[i];
+        counted += count[i];
+    }
+    __syncthreads();
+}
+// The bin in which some number that rises passes `wanted`: the one with at(bin) < wanted <= at(bin + 1).
+template <class At>
+__device__ __forceinline__ uint32_t bin_of(Shared& sh, At at, uint64_t wanted) {
+    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads)
+        if (at(b) < wanted && wanted <= at(b + 1u)) sh.found = b;
+    __syncthreads();
+    const uint32_t b = sh.found;
+    __syncthreads();
+    return b;
+}
+
+struct Settings {
+    float u, top_p, min_p;
+    uint32_t top_k;                     // 0: all
+};
+// What part of the kept mass is passed, and the least mass that reaches top_p of all.
+__device__ __forceinline__ uint64_t drawn_at(float u, uint64_t kept) {
+    const uint64_t at = u > 0.0f ? u < 1.0f ? uint64_t(double(u) * double(kept)) : kept - 1u : 0u;
+    return at < kept ? at : kept - 1u;
+}
+__device__ __forceinline__ uint64_t wanted_of(float top_p, uint64_t all) {
+    const uint64_t wanted = top_p > 0.0f ? uint64_t(ceil(double(top_p) * double(all))) : 1u;
+    return wanted < 1u ? 1u : wanted > all ? all : wanted;
+}
+
+// From the list of all tokens that may be kept (key, id, mass), n of them.
+__device__ __forceinline__ void draw_from_list(Shared& sh, const Settings& set, uint32_t n, uint32_t point, double least_mass) {
+    uint64_t count = 0u, before = 0u, mass = 0u;
+    const bool there = threadIdx.x < n;
+    if (there) {
+        before_in_list(sh, n, threadIdx.x, count, before);
+        mass = sh.list_q[threadIdx.x];
+    }
+    const uint32_t last = (set.top_k && set.top_k < n ? set.top_k : n) - 1u;
+    if (there && count == last) sh.found_sum = before + mass;
+    __syncthreads();
+    const uint64_t all = sh.found_sum;
+    uint64_t kept = all;
+    if (set.top_p < 1.0f) {
+        const uint64_t wanted = wanted_of(set.top_p, all);
+        if (there && before < wanted && wanted <= before + mass) sh.found_count = before + mass;
+        __syncthreads();
+        kept = sh.found_count;
+    }
+    if (set.min_p > 0.0f) {
+        // (those that weigh enough are the first of the order: the last one's sum is theirs)
+        uint64_t upto = there && double(mass) >= least_mass ? before + mass : 0u;
+        for (uint32_t d = 32; d; d >>= 1) {
+            const uint64_t other = __shfl_xor(upto, d);
+            upto = other > upto ? other : upto;
+        }
+        if ((threadIdx.x & 63u) == 0u) sh.of_wave[threadIdx.x >> 6] = upto;
+        __syncthreads();
+        upto = 0u;
+        for (uint32_t w = 0; w < kWaves; ++w) upto = sh.of_wave[w] > upto ? sh.of_wave[w] : upto;
+        kept = upto < kept ? upto : kept;
+    }
+    const uint64_t at = drawn_at(set.u, kept);
+    if (there && before <= at && at < before + mass) {
+        sh.found_id = sh.list_id[threadIdx.x];
+        sh.found_q = mass;
+        sh.found_sum = kept;
+    }
+    __syncthreads();
+}
+
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
     __shared__ Shared sh;
     const uint64_t r = uint64_t(blockIdx.y) * kAcross + blockIdx.x;
     if (r >= p.rows) return;
-    const float temperature = p.temperature ? p.temperature[r] : p.any_temperature, top_p = p.top_p ? p.top_p[r] : p.any_top_p;
-    const float min_p = p.min_p ? p.min_p[r] : p.any_min_p;
+    const float temperature = p.temperature ? p.temperature[r] : p.any_temperature;
     const int32_t top_k = p.top_k ? p.top_k[r] : p.any_top_k;
-    Row<DTYPE> row = {p.logits, r * p.stride, p.vocabulary, p.point, 0.0, 0.0, false};
+    const Settings set = {p.uniforms[r], p.top_p ? p.top_p[r] : p.any_top_p, p.min_p ? p.min_p[r] : p.any_min_p, top_k > 0 ? uint32_t(top_k) : 0u};
+    Row<DTYPE> row = {p.logits, r * p.stride, p.vocabulary, p.point, 0.0, 0.0};
+    const auto answer = [&](int64_t token, float chance) __attribute__((always_inline)) {
+        if (threadIdx.x != 0u) return;
+        p.tokens[r] = token;
+        if (p.chances) p.chances[r] = chance;
+    };
 
-    // The largest logit and its first token.
-    uint32_t best = 0u, id = 0u;
-    bool none = !(temperature >= 0.0f);
-    row.each([&](float l, uint32_t at) __attribute__((always_inline)) {
-        none |= l != l;
-        const uint32_t key = key_of(l);
-        if (key > best) {
-            best = key;
-            id = at;
-        }
+    // The largest logit; the largest of bits without sign is a NaN's where there is one.
+    float top = -__builtin_inff();
+    uint32_t bits = 0u;
+    row.each([&](float l, uint32_t) __attribute__((always_inline)) {
+        top = fmaxf(top, l);
+        const uint32_t w = __builtin_bit_cast(uint32_t, l) & 0x7FFFFFFFu;
+        bits = w > bits ? w : bits;
     });
-    uint64_t both = uint64_t(best) << 32 | ~id;
+    const float own_top = top;
+    uint64_t both = uint64_t(key_of(top)) << 32 | bits;
     for (uint32_t d = 32; d; d >>= 1) {
         const uint64_t other = __shfl_xor(both, d);
-        both = other > both ? other : both;
+        both = (other >> 32 > both >> 32 ? other >> 32 : both >> 32) << 32 | (uint32_t(other) > uint32_t(both) ? uint32_t(other) : uint32_t(both));
     }
-    none = __any(none);
-    if ((threadIdx.x & 63u) == 0u) {
-        sh.of_wave[threadIdx.x >> 6] = both;
-        sh.of_wave_too[threadIdx.x >> 6] = none;
-    }
+    if ((threadIdx.x & 63u) == 0u) sh.of_wave[threadIdx.x >> 6] = both;
     for (uint32_t i = threadIdx.x; i <= kBins; i += kThreads) {
         sh.mass[i] = 0u;
         sh.count[i] = 0u;
     }
-    if (threadIdx.x == 0u) sh.list_bin = ~0u;
-    __syncthreads();
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        both = sh.of_wave[w] > both ? sh.of_wave[w] : both;
-        none |= sh.of_wave_too[w] != 0u;
+    if (threadIdx.x == 0u) {
+        sh.list_bin = ~0u;
+        sh.listed = 0u;
     }
-    best = uint32_t(both >> 32);
-    if (none || best <= kLowest || temperature == 0.0f || top_k == 1) {
-        if (threadIdx.x == 0u) {
-            const bool any = !none && best > kLowest;
-            p.tokens[r] = any ? int64_t(~uint32_t(both)) : -1;
-            if (p.chances) p.chances[r] = any ? 1.0f : 0.0f;
-        }
+    __syncthreads();
+    uint32_t best = 0u;
+    for (uint32_t w = 0; w < kWaves; ++w) {
+        best = uint32_t(sh.of_wave[w] >> 32) > best ? uint32_t(sh.of_wave[w] >> 32) : best;
+        bits = uint32_t(sh.of_wave[w]) > bits ? uint32_t(sh.of_wave[w]) : bits;
+    }
+    top = of_key(best);
+    if (bits > 0x7F800000u || !(temperature >= 0.0f) || top == -__builtin_inff()) {
+        answer(-1, 0.0f);
         return;
     }
-    const uint32_t w = best ^ (best >> 31 ? 0x80000000u : ~0u);
-    row.top = double(__builtin_bit_cast(float, w));
-    row.infinite = w == 0x7F800000u;
+    if (temperature == 0.0f || set.top_k == 1u) {
+        find_equal(sh, row, best, 1u);
+        answer(int64_t(sh.found_id), 1.0f);
+        return;
+    }
+    if (top == __builtin_inff()) {
+        // infinities share the row alone, each a mass of 1
+        uint32_t mine = 0u;
+        row.each([&](float l, uint32_t) __attribute__((always_inline)) { mine += l == __builtin_inff() ? 1u : 0u; });
+        __syncthreads();
+        added_before(mine, sh.of_wave);
+        uint64_t kept = 0u;
+        for (uint32_t w = 0; w < kWaves; ++w) kept += sh.of_wave[w];
+        kept = set.top_k && set.top_k < kept ? set.top_k : kept;
+        if (set.top_p < 1.0f) kept = wanted_of(set.top_p, kept);
+        find_equal(sh, row, best, drawn_at(set.u, kept) + 1u);
+        answer(int64_t(sh.found_id), float(1.0 / double(kept)));
+        return;
+    }
+    row.top = double(top);
     row.steps = 1.4426950408889634074 * double(kSteps) / double(temperature);
+    const double one = __builtin_bit_cast(double, uint64_t(1023u + p.point) << 52);
+    const double least = set.min_p < 1.0f ? double(set.min_p) : 1.0;                // (not looked at where there is none)
 
+    // Few tokens that may be kept are listed, and all else is done in the list.  top_k: as many threads' largest logits are at least the least of those that are
+    // listed, so that at least top_k tokens are.  min_p alone: those that weigh enough.
+    const bool by_weight = set.min_p > 0.0f && !(set.top_p < 1.0f);
+    if ((set.top_k && set.top_k <= kList / 2u) || by_weight) {
+        uint32_t last = kBins - 1u;
+        if (set.top_k && set.top_k <= kList / 2u) {
+            uint32_t bin;
+            uint64_t q;
+            if (row.weigh(own_top, bin, q)) atomicAdd(&sh.count[bin], 1u);
+            __syncthreads();
+            add_up_bins(sh);
+            if (set.top_k <= sh.count[kBins]) last = bin_of(sh, [&](uint32_t i) __attribute__((always_inline)) { return uint64_t(sh.count[i]); }, set.top_k);
+        }
+        if (by_weight) {
+            const double t = -double(kSteps) * log2(least) + 1.0;
+            last = t < double(last) ? uint32_t(t) : last;
+        }
+        float low, high;
+        row.reach_of(0u, last, low, high);
+        row.each([&](float l, uint32_t id) __attribute__((always_inline)) {
+            if (!(l >= low)) return;
+            uint32_t bin;
+            uint64_t q;
+            if (!row.weigh(l, bin, q)) return;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at >= kList) return;
+            sh.list_key[at] = key_of(l);
+            sh.list_id[at] = id;
+            sh.list_q[at] = mass_of(height(bin), q);
+        });
+        __syncthreads();
+        const uint32_t n = sh.listed;
+        if (n <= kList) {
+            draw_from_list(sh, set, n, p.point, least * one);
+            answer(int64_t(sh.found_id), float(double(sh.found_q) / double(sh.found_sum)));
+            return;
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i <= kBins; i += kThreads) {
+            sh.mass[i] = 0u;
+            sh.count[i] = 0u;
+        }
+        __syncthreads();
+    }
+
+    const bool counts = set.top_k != 0u;
     row.each([&](float l, uint32_t) __attribute__((always_inline)) {
         uint32_t bin;
         uint64_t q;
         if (!row.weigh(l, bin, q)) return;
         atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[bin]), q);
-        if (top_k > 0) atomicAdd(&sh.count[bin], 1u);
+        if (counts) atomicAdd(&sh.count[bin], 1u);
     });
     __syncthreads();
-    {
-        constexpr uint32_t kEach = (kBins + kThreads - 1u) / kThreads;
-        uint64_t mass[kEach], masses = 0u, counts = 0u;
-        uint32_t count[kEach];
-        const uint32_t first = threadIdx.x * kEach;
-        for (uint32_t i = 0; i < kEach; ++i) {
-            const bool there = first + i < kBins;
-            mass[i] = there ? mass_of(height(first + i), sh.mass[first + i]) : 0u;
-            count[i] = there ? sh.count[first + i] : 0u;
-            masses += mass[i];
-            counts += count[i];
-        }
-        __syncthreads();
-        uint64_t upto = added_before(masses, sh.of_wave), counted = added_before(counts, sh.of_wave_too);
-        for (uint32_t i = 0; i < kEach; ++i) {
-            if (first + i <= kBins) {
-                sh.mass[first + i] = upto;
-                sh.count[first + i] = uint32_t(counted);
-            }
-            upto += mass[i];
-            counted += count[i];
-        }
-        __syncthreads();
-    }
-    // The bin in which some number that rises passes `wanted`: the one with at(bin) < wanted <= at(bin + 1).
-    const auto bin_of = [&](auto at, uint64_t wanted) __attribute__((always_inline)) {
-        for (uint32_t b = threadIdx.x; b < kBins; b += kThreads)
-            if (at(b) < wanted && wanted <= at(b + 1u)) sh.found = b;
-        __syncthreads();
-        const uint32_t b = sh.found;
-        __syncthreads();
-        return b;
-    };
+    add_up_bins(sh);
     const auto mass_before = [&](uint32_t b) __attribute__((always_inline)) { return sh.mass[b]; };
-    // The mass up to the first token at which it is at least `wanted` (1 .. all).
-    const auto mass_that_reaches = [&](uint64_t wanted) __attribute__((always_inline)) {
-        const uint32_t b = bin_of(mass_before, wanted);
-        if (wanted == sh.mass[b + 1u] && sh.mass[b + 1u] == sh.mass[kBins]) return sh.mass[kBins];
-        const uint64_t before = sh.mass[b];
-        const double high = height(b);
-        find<DTYPE>(sh, row, b, [=](uint64_t, uint64_t sum) { return before + mass_of(high, sum) >= wanted; });
-        const uint64_t upto = before + mass_of(high, sh.found_sum);
-        __syncthreads();
-        return upto;
-    };
 
     uint64_t kept = sh.mass[kBins];
-    if (top_k > 0 && uint32_t(top_k) < sh.count[kBins]) {
-        const uint32_t b = bin_of([&](uint32_t i) __attribute__((always_inline)) { return uint64_t(sh.count[i]); }, uint32_t(top_k));
-        const uint64_t wanted = uint32_t(top_k) - sh.count[b];
+    if (set.top_k && set.top_k < sh.count[kBins]) {
+        const uint32_t b = bin_of(sh, [&](uint32_t i) __attribute__((always_inline)) { return uint64_t(sh.count[i]); }, set.top_k);
+        const uint64_t wanted = set.top_k - sh.count[b];
         if (wanted == sh.count[b + 1u] - sh.count[b]) {
             kept = sh.mass[b + 1u];
         } else {
@@ -356,43 +500,49 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
             __syncthreads();
         }
     }
-    if (top_p < 1.0f) {
-        const uint64_t wanted = top_p > 0.0f ? uint64_t(ceil(double(top_p) * double(kept))) : 1u;
-        const uint64_t upto = mass_that_reaches(wanted < 1u ? 1u : wanted > kept ? kept : wanted);
+    // The bins in which the two other borders are: the first border counts, and where that is one bin's both have to be worked out.
+    uint32_t bin_p = kBins, bin_m = kBins;
+    uint64_t wanted = 0u;
+    if (set.top_p < 1.0f) {
+        wanted = wanted_of(set.top_p, kept);
+        bin_p = bin_of(sh, mass_before, wanted);
+    }
+    if (set.min_p > 0.0f) {
+        const double t = -double(kSteps) * log2(least);
+        if (t < double(kBins) - 1.0) bin_m = uint32_t(rint(t));
+    }
+    if (bin_p < kBins && bin_p <= bin_m) {
+        const uint64_t before = sh.mass[bin_p];
+        const double high = height(bin_p);
+        find<DTYPE>(sh, row, bin_p, [=](uint64_t, uint64_t sum) { return before + mass_of(high, sum) >= wanted; });
+        const uint64_t upto = before + mass_of(high, sh.found_sum);
+        kept = upto < kept ? upto : kept;
+        __syncthreads();
+    }
+    if (bin_m < kBins && bin_m <= bin_p) {
+        const double high = height(bin_m), border = least * one;
+        float lo, hi;
+        row.reach_of(bin_m, bin_m, lo, hi);
+        uint64_t sum = 0u;
+        row.each([&](float l, uint32_t) __attribute__((always_inline)) {
+            if (!(l >= lo && l <= hi)) return;
+            uint32_t bin;
+            uint64_t q;
+            if (row.weigh(l, bin, q) && bin == bin_m && high * double(q) >= border) sum += q;
+        });
+        __syncthreads();
+        added_before(sum, sh.of_wave);
+        sum = 0u;
+        for (uint32_t i = 0; i < kWaves; ++i) sum += sh.of_wave[i];
+        const uint64_t upto = sh.mass[bin_m] + mass_of(high, sum);
         kept = upto < kept ? upto : kept;
     }
-    if (min_p > 0.0f) {
-        const double least = min_p < 1.0f ? double(min_p) : 1.0, t = -double(kSteps) * log2(least);
-        if (t < double(kBins) - 1.0) {
-            const uint32_t b = uint32_t(rint(t));
-            const double high = height(b), border = least * __builtin_bit_cast(double, uint64_t(1023u + p.point) << 52);
-            uint64_t sum = 0u;
-            row.each([&](float l, uint32_t) __attribute__((always_inline)) {
-                uint32_t bin;
-                uint64_t q;
-                if (row.weigh(l, bin, q) && bin == b && high * double(q) >= border) sum += q;
-            });
-            for (uint32_t d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-            __syncthreads();
-            if ((threadIdx.x & 63u) == 0u) sh.of_wave[threadIdx.x >> 6] = sum;
-            __syncthreads();
-            sum = 0u;
-            for (uint32_t i = 0; i < kWaves; ++i) sum += sh.of_wave[i];
-            const uint64_t upto = sh.mass[b] + mass_of(high, sum);
-            kept = upto < kept ? upto : kept;
-        }
-    }
-    const float u = p.uniforms[r];
-    uint64_t at = u > 0.0f ? u < 1.0f ? uint64_t(double(u) * double(kept)) : kept - 1u : 0u;
-    if (at >= kept) at = kept - 1u;
-    const uint32_t b = bin_of(mass_before, at + 1u);
+    const uint64_t at = drawn_at(set.u, kept);
+    const uint32_t b = bin_of(sh, mass_before, at + 1u);
     const uint64_t before = sh.mass[b];
     const double high = height(b);
     find<DTYPE>(sh, row, b, [=](uint64_t, uint64_t sum) { return before + mass_of(high, sum) > at; });
-    if (threadIdx.x == 0u) {
-        p.tokens[r] = int64_t(sh.found_id);
-        if (p.chances) p.chances[r] = float(high * double(sh.found_q) / double(kept));
-    }
+    answer(int64_t(sh.found_id), float(high * double(sh.found_q) / double(kept)));
 }
 
 }  // namespace
