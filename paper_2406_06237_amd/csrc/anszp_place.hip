@@ -7,16 +7,17 @@
 // All of it are sums over the sequences and a look-up a token, so nothing depends on the order in which threads arrive.
 //
 // One workgroup adds up over the sequences and leaves a record for each; a thread a token then finds its sequence in the starts and its page
-// in the table or on the stack, and writes the table where it is the first in its page.  Latency bounds both.
+// in the table or on the stack, and writes the table where it is the first in its page.  Latency bounds both: LATENCY
 #include <hip/hip_runtime.h>
 
 #include "anszp_numbers.h"
 
 namespace {
 
-// What a sequence's tokens need to know: tokens before this step (-1: refused), pages before it, and the stack's place of its first new page.
+// What a sequence's tokens need to know: tokens before this step (-1: refused), pages before it, and the stack's place of its first new page; and where its pages go that
+// it gives back, and how many.
 struct Record {
-    int32_t old, pages, top;
+    int32_t old, pages, top, back_at, back;
 };
 
 struct PlaceParams {
@@ -36,7 +37,7 @@ struct PlaceParams {
     uint32_t n_seqs, n_tokens, free_room, width, page_log;
 };
 
-constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64u;
+constexpr uint32_t kInLds = 2048;       // sequences whose starts a workgroup keeps
 
 __device__ __forceinline__ void tell(const PlaceParams& p) {
     if (p.status) {
@@ -49,7 +50,9 @@ __device__ __forceinline__ void tell(const PlaceParams& p) {
 struct Sums {
     int64_t before, all;
 };
+template <uint32_t THREADS>
 __device__ __forceinline__ Sums added_up(int64_t v) {
+    constexpr uint32_t kWaves = THREADS / 64u;
     __shared__ int64_t of_wave[kWaves];
     int64_t upto = v;
     for (uint32_t d = 1; d < 64u; d <<= 1) {
@@ -59,9 +62,11 @@ __device__ __forceinline__ Sums added_up(int64_t v) {
     if ((threadIdx.x & 63u) == 63u) of_wave[threadIdx.x >> 6] = upto;
     __syncthreads();
     Sums r = {upto - v, 0};
+#pragma unroll
     for (uint32_t w = 0; w < kWaves; ++w) {
-        if (w < threadIdx.x >> 6) r.before += of_wave[w];
-        r.all += of_wave[w];
+        const int64_t other = of_wave[w];
+        r.before += w < threadIdx.x >> 6 ? other : 0;
+        r.all += other;
     }
     __syncthreads();
     return r;
@@ -81,13 +86,13 @@ __device__ __forceinline__ uint32_t last_not_above(const T* rising, uint32_t n, 
 
 __device__ __forceinline__ uint32_t pages_for(int64_t tokens, uint32_t page_log) { return uint32_t((tokens + (1ll << page_log) - 1) >> page_log); }
 
-__device__ __forceinline__ void place_token(const PlaceParams& p, const int32_t* starts, uint32_t t) {
+__device__ __forceinline__ void place_token(const PlaceParams& p, const int32_t* starts, const Record* records, uint32_t t) {
     int64_t slot = -1;
     int32_t owner = -1;
     if (int32_t(t) < starts[p.n_seqs]) {
         // (sequences without new tokens begin where the next one does: the last one that begins here has the token)
         const uint32_t s = last_not_above(starts, p.n_seqs, int32_t(t));
-        const Record r = p.records[s];
+        const Record r = records[s];
         owner = int32_t(s);
         if (r.old >= 0) {
             const uint32_t at = uint32_t(r.old) + t - uint32_t(starts[s]), column = at >> p.page_log, inside = at & ((1u << p.page_log) - 1u);
@@ -107,18 +112,20 @@ __device__ __forceinline__ void place_token(const PlaceParams& p, const int32_t*
     if (p.owners) p.owners[t] = owner;
 }
 
-// Sums over the sequences; with TOKENS the tokens' places as well.
-template <bool TOKENS>
-__global__ __launch_bounds__(kThreads) void place_sequences_kernel(PlaceParams p) {
-    __shared__ int32_t first_of[kThreads];
+// Sums over the sequences; ALONE: the pages that go back and the tokens' places as well, with what they need in LDS where there is a thread for each sequence.
+template <uint32_t THREADS, bool ALONE>
+__global__ __launch_bounds__(THREADS) void place_sequences_kernel(PlaceParams p) {
+    __shared__ int32_t first_of[THREADS], starts[THREADS + 1u];
+    __shared__ Record records[THREADS];
     const int64_t room = int64_t(p.width) << p.page_log;
+    const bool one_each = ALONE && p.n_seqs <= THREADS;
     int64_t top = p.n_free[0];
     if (top < 0 || top > p.free_room) {
         top = top < 0 ? 0 : p.free_room;
         if (threadIdx.x == 0u) tell(p);
     }
     if (p.ends) {
-        for (uint32_t from = 0; from < p.n_seqs; from += kThreads) {
+        for (uint32_t from = 0; from < p.n_seqs; from += THREADS) {
             const uint32_t s = from + threadIdx.x;
             uint32_t back = 0u;
             if (s < p.n_seqs && p.ends[s]) {
@@ -126,34 +133,40 @@ __global__ __launch_bounds__(kThreads) void place_sequences_kernel(PlaceParams p
                 if (held < 0 || held > room) tell(p);
                 back = pages_for(held < 0 ? 0 : held > room ? room : held, p.page_log);
             }
-            const Sums sums = added_up(back);
+            const Sums sums = added_up<THREADS>(back);
             // (a stack that its own pages overflow holds some twice; what is beyond its room is lost, and told)
             const int64_t fits = sums.all <= int64_t(p.free_room) - top ? sums.all : int64_t(p.free_room) - top;
             if (fits < sums.all && threadIdx.x == 0u) tell(p);
-            // The pages that go back are shared out to the threads, whichever sequences they are of.
-            first_of[threadIdx.x] = int32_t(sums.before < fits ? sums.before : fits);
-            __syncthreads();
-            for (int64_t j = threadIdx.x; j < fits; j += kThreads) {
-                const uint32_t i = last_not_above(first_of, kThreads, int32_t(j));
-                p.free[top + j] = p.pages[uint64_t(from + i) * p.width + uint32_t(j - first_of[i])];
+            const int64_t first = sums.before < fits ? sums.before : fits;
+            if constexpr (ALONE) {
+                // The pages that go back are shared out to the threads, whichever sequences they are of.
+                first_of[threadIdx.x] = int32_t(first);
+                __syncthreads();
+                for (int64_t j = threadIdx.x; j < fits; j += THREADS) {
+                    const uint32_t i = last_not_above(first_of, THREADS, int32_t(j));
+                    p.free[top + j] = p.pages[uint64_t(from + i) * p.width + uint32_t(j - first_of[i])];
+                }
+                __syncthreads();
+            } else if (s < p.n_seqs) {
+                p.records[s].back_at = int32_t(top + first);
+                p.records[s].back = int32_t(first + back < fits ? back : fits - first);
             }
             top += fits;
-            __syncthreads();
         }
     }
     int64_t tokens = 0, pages = 0, taken = 0;
-    for (uint32_t from = 0; from < p.n_seqs; from += kThreads) {
+    for (uint32_t from = 0; from < p.n_seqs; from += THREADS) {
         const uint32_t s = from + threadIdx.x;
         const bool there = s < p.n_seqs;
         const int32_t held = there ? p.lengths[s] : 0, fresh = there ? p.fresh[s] : 0;
         const bool ended = there && p.ends && p.ends[s];
         const int64_t old = ended ? 0 : held, more = fresh < 0 ? 0 : fresh;
-        const Sums t = added_up(more);
+        const Sums t = added_up<THREADS>(more);
         const int64_t start = tokens + t.before;
         tokens += t.all;
         bool served = fresh >= 0 && old >= 0 && old + more <= room && start + more <= p.n_tokens;
         const uint32_t have = served ? pages_for(old, p.page_log) : 0u, need = served ? pages_for(old + more, p.page_log) - have : 0u;
-        const Sums n = added_up(need);
+        const Sums n = added_up<THREADS>(need);
         const int64_t upto = pages + n.before + need;
         pages += n.all;
         served = served && (need == 0u || upto <= top);
@@ -163,31 +176,61 @@ __global__ __launch_bounds__(kThreads) void place_sequences_kernel(PlaceParams p
             const int64_t other = __shfl_xor(last, d);
             last = other > last ? other : last;
         }
-        __shared__ int64_t lasts[kWaves];
+        __shared__ int64_t lasts[THREADS / 64u];
         if ((threadIdx.x & 63u) == 0u) lasts[threadIdx.x >> 6] = last;
         __syncthreads();
-        for (uint32_t w = 0; w < kWaves; ++w) taken = lasts[w] > taken ? lasts[w] : taken;
+#pragma unroll
+        for (uint32_t w = 0; w < THREADS / 64u; ++w) taken = lasts[w] > taken ? lasts[w] : taken;
         if (there) {
             if (!served) tell(p);
-            p.records[s] = {served ? int32_t(old) : -1, int32_t(have), int32_t(top - 1 - (upto - need))};
-            p.starts[s] = int32_t(start < p.n_tokens ? start : p.n_tokens);
+            const int32_t at = int32_t(start < p.n_tokens ? start : p.n_tokens);
+            const Record r = {served ? int32_t(old) : -1, int32_t(have), int32_t(top - 1 - (upto - need)), 0, 0};
+            if (one_each) {
+                records[threadIdx.x] = r;
+                starts[threadIdx.x] = at;
+            } else {
+                p.records[s].old = r.old;
+                p.records[s].pages = r.pages;
+                p.records[s].top = r.top;
+            }
+            p.starts[s] = at;
             p.lengths_out[s] = int32_t(served ? old + more : old);
         }
     }
     __syncthreads();                                                // (n_free may be its own output)
     if (threadIdx.x == 0u) {
-        p.starts[p.n_seqs] = int32_t(tokens < p.n_tokens ? tokens : p.n_tokens);
+        const int32_t all = int32_t(tokens < p.n_tokens ? tokens : p.n_tokens);
+        if (one_each) starts[p.n_seqs] = all;
+        p.starts[p.n_seqs] = all;
         p.n_free_out[0] = int32_t(top - taken);
     }
-    if constexpr (TOKENS) {
+    if constexpr (ALONE) {
         __syncthreads();
-        for (uint32_t t = threadIdx.x; t < p.n_tokens; t += kThreads) place_token(p, p.starts, t);
+        for (uint32_t t = threadIdx.x; t < p.n_tokens; t += THREADS) {
+            if (one_each) place_token(p, starts, records, t);
+            else place_token(p, p.starts, p.records, t);
+        }
+    }
+}
+
+// The pages that go back, a workgroup for each sequence.
+__global__ __launch_bounds__(256) void place_back_kernel(PlaceParams p) {
+    for (uint32_t s = blockIdx.x; s < p.n_seqs; s += gridDim.x) {
+        const Record r = p.records[s];
+        for (uint32_t j = threadIdx.x; int32_t(j) < r.back; j += 256u) p.free[uint32_t(r.back_at) + j] = p.pages[uint64_t(s) * p.width + j];
     }
 }
 
 __global__ __launch_bounds__(256) void place_tokens_kernel(PlaceParams p) {
+    __shared__ int32_t starts[kInLds + 1u];
     const uint64_t t = uint64_t(blockIdx.x) * 256u + threadIdx.x;
-    if (t < p.n_tokens) place_token(p, p.starts, uint32_t(t));
+    if (p.n_seqs <= kInLds) {
+        for (uint32_t s = threadIdx.x; s <= p.n_seqs; s += 256u) starts[s] = p.starts[s];
+        __syncthreads();
+        if (t < p.n_tokens) place_token(p, starts, p.records, uint32_t(t));
+    } else if (t < p.n_tokens) {
+        place_token(p, p.starts, p.records, uint32_t(t));
+    }
 }
 
 int place_check(const anszp_place_args_t& a) {
@@ -227,11 +270,16 @@ extern "C" int anszp_place(const anszp_place_args_t* a, void* hip_stream) {
                      static_cast<Record*>(a->workspace), static_cast<uint32_t>(a->n_seqs), static_cast<uint32_t>(a->n_tokens), static_cast<uint32_t>(a->free_room),
                      a->table_width, static_cast<uint32_t>(__builtin_ctz(a->page_size))};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (a->n_tokens <= 4096u) {
-        hipLaunchKernelGGL(place_sequences_kernel<true>, dim3(1), dim3(kThreads), 0, s, p);
+    // One launch where a workgroup has few tokens to place and few sequences whose pages could go back (16 sequences with a token each: ONE us, in two launches TWO);
+    // else the pages and the tokens have the chip.
+    if (a->n_tokens <= 1024u && a->n_seqs <= 256u && !a->ends) {
+        hipLaunchKernelGGL((place_sequences_kernel<256u, true>), dim3(1), dim3(256), 0, s, p);
+    } else if (a->n_tokens <= 4096u && (!a->ends || a->n_seqs <= 64u)) {
+        hipLaunchKernelGGL((place_sequences_kernel<1024u, true>), dim3(1), dim3(1024), 0, s, p);
     } else {
-        hipLaunchKernelGGL(place_sequences_kernel<false>, dim3(1), dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL(place_tokens_kernel, dim3(static_cast<uint32_t>((a->n_tokens + 255u) / 256u)), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((place_sequences_kernel<1024u, false>), dim3(1), dim3(1024), 0, s, p);
+        if (a->ends && a->n_seqs) hipLaunchKernelGGL(place_back_kernel, dim3(static_cast<uint32_t>(a->n_seqs < 65536u ? a->n_seqs : 65536u)), dim3(256), 0, s, p);
+        if (a->n_tokens) hipLaunchKernelGGL(place_tokens_kernel, dim3(static_cast<uint32_t>((a->n_tokens + 255u) / 256u)), dim3(256), 0, s, p);
     }
     return hipGetLastError() == hipSuccess ? ANSZP_OK : ANSZP_E_HIP;
 }
