@@ -557,13 +557,13 @@ typedef struct {
     int32_t*       starts;        /* [device] n_seqs + 1: as anszp_attend takes them                 */
     uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for a sequence that gets nothing though it asks, numbers out of
                                      range, a page below 0, pages that overflow the stack; [1] grows */
-    void*          workspace;     /* [device] anszp_place_workspace_bytes, 16-byte aligned, in use until the call is done */
+    void*          workspace;     /* [device] anszp_place_workspace_bytes, 16-byte aligned, in use until the call is done; NULL if none */
     uint64_t       workspace_bytes;
     uint64_t       n_seqs, n_tokens, free_room;           /* < 2^24, < 2^31, < 2^31; may be 0        */
     uint32_t       table_width;   /* >= 1; table_width * page_size <= 2^30                           */
     uint32_t       page_size;     /* a power of two from 16 to 65536                                 */
 } anszp_place_args_t;
-/* [host only] Bytes of workspace a call takes; reads sizes only, no pointers. */
+/* [host only] Bytes of workspace a call takes (0: none); reads sizes, and whether there are `ends`. */
 uint64_t anszp_place_workspace_bytes(const anszp_place_args_t* args);
 /* Errors: E_NULL, E_RANGE (also for a workspace that is too small, and for an output that meets another operand), E_HIP. */
 int anszp_place(const anszp_place_args_t* args, void* hip_stream);

@@ -102,21 +102,24 @@ struct Adapters {
     }
 };
 
-// h of 64 rows and up to 16 * RANKS ranks, 16 rows a wavefront.  128 bytes of each row of x and as much of k of a's rows go to LDS at a time, in pieces of 16 bytes end to
+// h of 64 rows and up to 16 * RANKS ranks, 16 rows a wavefront.  128 or 256 bytes of each row of x and as much of k of a's rows go to LDS at a time, in pieces of 16 bytes end to
 // end (operands taken from memory as the instructions want them are 16 bytes of 16 rows for every 16 lanes, and a CU looks up four times the lines: 33 us for
 // 8192 rows of 4096 bytes and rank 64, this 20); two times of them are under way beside the one in LDS.
+constexpr uint32_t at_once(bool bytes, uint32_t ranks) { return bytes || ranks <= 2u ? 128u : 64u; }
 template <bool BYTES, uint32_t RANKS>
 __global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
-    constexpr uint32_t kAtOnce = BYTES ? 128u : 64u, kRowOfA = kAtOnce * 2u, kPiecesOfA = RANKS * 16u * kRowOfA / 16u, kEachOfA = (kPiecesOfA + 255u) / 256u;
-    __shared__ __attribute__((aligned(16))) uint8_t xs[2][64][128u + 16u], as[2][16u * RANKS][kRowOfA + 16u];
+    constexpr uint32_t kAtOnce = at_once(BYTES, RANKS), kRowOfX = kAtOnce * (BYTES ? 1u : 2u), kRowOfA = kAtOnce * 2u, kInX = kRowOfX / 16u, kInA = kRowOfA / 16u;
+    constexpr uint32_t kPiecesOfA = RANKS * 16u * kInA, kEachOfA = (kPiecesOfA + 255u) / 256u, kEachOfX = 64u * kInX / 256u;
+    __shared__ __attribute__((aligned(16))) uint8_t xs[2][64][kRowOfX + 16u], as[2][16u * RANKS][kRowOfA + 16u];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint32_t slot = blockIdx.y / p.groups, group = blockIdx.y - slot * p.groups, part = blockIdx.z;
     const uint64_t first = uint64_t(blockIdx.x) * 64u;
     const uint32_t steps = (p.k + kAtOnce - 1u) / kAtOnce, begin = uint32_t(uint64_t(steps) * part / p.parts), end = uint32_t(uint64_t(steps) * (part + 1u) / p.parts);
     const float x_scale = p.x_scales ? p.x_scales[least(first + lane, p.rows - 1u)] : 1.0f;
     const int32_t id = id_of(p, first + lane, false);
-    // This thread's pieces: of x's rows t / 8 and t / 8 + 32, of a's from t on every 256th.
-    const uint32_t x_row = threadIdx.x >> 3, x_piece = (threadIdx.x & 7u) * 16u;
+    // This thread's pieces are every 256th of x's and of a's.
+    const uint32_t x_row = threadIdx.x / kInX, x_piece = threadIdx.x % kInX * 16u;
+    constexpr uint32_t kRowsApart = 256u / kInX;
     // Few rows: a workgroup for each, which works at the row's adapter if no row before has it.  Else the adapters in turn.
     uint64_t left = __ballot(id >= 0);
     uint32_t wait = slot;
@@ -136,37 +139,37 @@ __global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
         }
         wait = p.slots - 1u;
         const float by = p.scales ? p.scales[one] : 1.0f;
-        const uint8_t* x[2];
+        const uint8_t* x[kEachOfX];
         const uint8_t* a[kEachOfA];
-        bool has[2];
+        bool has[kEachOfX];
 #pragma unroll
-        for (uint32_t i = 0; i < 2u; ++i) {
-            has[i] = lanes >> (x_row + 32u * i) & 1u;               // (rows of other adapters stay what they were: nothing of theirs is kept)
-            x[i] = p.x + least(first + x_row + 32u * i, p.rows - 1u) * p.x_stride + x_piece;
+        for (uint32_t i = 0; i < kEachOfX; ++i) {
+            has[i] = lanes >> (x_row + kRowsApart * i) & 1u;               // (rows of other adapters stay what they were: nothing of theirs is kept)
+            x[i] = p.x + least(first + x_row + kRowsApart * i, p.rows - 1u) * p.x_stride + x_piece;
         }
 #pragma unroll
         for (uint32_t i = 0; i < kEachOfA; ++i) {
             const uint32_t n = threadIdx.x + i * 256u;
-            a[i] = reinterpret_cast<const uint8_t*>(p.a + uint64_t(one) * p.a_stride + least(group * RANKS * 16u + n / (kRowOfA / 16u), p.rank - 1u) * p.a_row_stride) + n % (kRowOfA / 16u) * 16u;
+            a[i] = reinterpret_cast<const uint8_t*>(p.a + uint64_t(one) * p.a_stride + least(group * RANKS * 16u + n / kInA, p.rank - 1u) * p.a_row_stride) + n % kInA * 16u;
         }
         struct Step {
-            words4 x[2], a[kEachOfA];
+            words4 x[kEachOfX], a[kEachOfA];
         } now, then;
         const auto load = [&](Step& to, uint32_t s) __attribute__((always_inline)) {
             if (s * kAtOnce + kAtOnce <= p.k) {
 #pragma unroll
                 for (uint32_t i = 0; i < kEachOfA; ++i) to.a[i] = *reinterpret_cast<const words4_any*>(a[i] + uint64_t(s) * kRowOfA);
 #pragma unroll
-                for (uint32_t i = 0; i < 2u; ++i)
-                    if (has[i]) to.x[i] = *reinterpret_cast<const words4_any*>(x[i] + uint64_t(s) * 128u);
+                for (uint32_t i = 0; i < kEachOfX; ++i)
+                    if (has[i]) to.x[i] = *reinterpret_cast<const words4_any*>(x[i] + uint64_t(s) * kRowOfX);
             } else {
                 const int32_t left = int32_t(p.k - s * kAtOnce);
 #pragma unroll
                 for (uint32_t i = 0; i < kEachOfA; ++i)
-                    to.a[i] = careful(a[i] + uint64_t(s) * kRowOfA, left * 2 - int32_t((threadIdx.x + i * 256u) % (kRowOfA / 16u) * 16u), p.a_last);
+                    to.a[i] = careful(a[i] + uint64_t(s) * kRowOfA, left * 2 - int32_t((threadIdx.x + i * 256u) % kInA * 16u), p.a_last);
 #pragma unroll
-                for (uint32_t i = 0; i < 2u; ++i)
-                    if (has[i]) to.x[i] = careful(x[i] + uint64_t(s) * 128u, left * (BYTES ? 1 : 2) - int32_t(x_piece), p.x_last);
+                for (uint32_t i = 0; i < kEachOfX; ++i)
+                    if (has[i]) to.x[i] = careful(x[i] + uint64_t(s) * kRowOfX, left * (BYTES ? 1 : 2) - int32_t(x_piece), p.x_last);
             }
         };
         floatx4 sum[RANKS] = {};
@@ -176,11 +179,11 @@ __global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
 #pragma unroll
             for (uint32_t i = 0; i < kEachOfA; ++i) {
                 const uint32_t n = threadIdx.x + i * 256u;
-                if (kPiecesOfA % 256u == 0u || n < kPiecesOfA) *reinterpret_cast<words4*>(&as[buffer][n / (kRowOfA / 16u)][n % (kRowOfA / 16u) * 16u]) = with.a[i];
+                if (kPiecesOfA % 256u == 0u || n < kPiecesOfA) *reinterpret_cast<words4*>(&as[buffer][n / kInA][n % kInA * 16u]) = with.a[i];
             }
 #pragma unroll
-            for (uint32_t i = 0; i < 2u; ++i)
-                if (has[i]) *reinterpret_cast<words4*>(&xs[buffer][x_row + 32u * i][x_piece]) = with.x[i];
+            for (uint32_t i = 0; i < kEachOfX; ++i)
+                if (has[i]) *reinterpret_cast<words4*>(&xs[buffer][x_row + kRowsApart * i][x_piece]) = with.x[i];
             __syncthreads();
             if (s + 2u < end) load(next, s + 2u);
             if (!works) return;
@@ -222,33 +225,34 @@ __device__ __forceinline__ uint16_t part_of(float h) {
     return !(__builtin_fabsf(h) < 0x1p127f) ? uint16_t(__builtin_bit_cast(uint32_t, h) >> 16) | (h != h ? 0x40u : 0u) : to_bf16(h);
 }
 
-// Block `block` of a row's terms, [term][block][8] behind `to`: the parts of k added up, in all terms; the blocks behind all of them are zeros.
-__device__ __forceinline__ void write_terms(const AdaptParams& p, uint64_t row, uint32_t block, uint16_t* to) {
-    if (block >= p.blocks && block < p.blocks * p.terms) return;
-    float h[8] = {};
-    if (block < p.blocks && block * 8u < p.rank && row < p.rows && uint32_t(p.ids[row]) < p.adapters) {
-        const float* const from = p.h + row * p.rank_room + block * 8u;
-        const uint64_t apart = p.rows * p.rank_room;
-        // (four under way together; behind the last one it is read again, and not added)
-        for (uint32_t s = 0; s < p.parts; s += 4u) {
-            floatx4 lo[4], hi[4];
+// Eight ranks of h of a row, the parts of k added up; what a row without an adapter has there is not looked at.
+__device__ __forceinline__ void load_h(const AdaptParams& p, uint64_t row, uint32_t block, float (&h)[8]) {
+    const float* const from = p.h + row * p.rank_room + block * 8u;
+    const uint64_t apart = p.rows * p.rank_room;
 #pragma unroll
-            for (uint32_t i = 0; i < 4u; ++i) {
-                const float* at = from + (s + i < p.parts ? s + i : p.parts - 1u) * apart;
-                lo[i] = reinterpret_cast<const floatx4*>(at)[0];
-                hi[i] = reinterpret_cast<const floatx4*>(at)[1];
-            }
+    for (uint32_t i = 0; i < 8u; ++i) h[i] = 0.0f;
+    // (four under way together; behind the last one it is read again, and not added)
+    for (uint32_t s = 0; s < p.parts; s += 4u) {
+        floatx4 lo[4], hi[4];
 #pragma unroll
-            for (uint32_t i = 0; i < 4u; ++i)
-#pragma unroll
-                for (uint32_t n = 0; n < 4u; ++n) {
-                    h[n] += s + i < p.parts ? lo[i][n] : 0.0f;
-                    h[n + 4u] += s + i < p.parts ? hi[i][n] : 0.0f;
-                }
+        for (uint32_t i = 0; i < 4u; ++i) {
+            const float* at = from + (s + i < p.parts ? s + i : p.parts - 1u) * apart;
+            lo[i] = reinterpret_cast<const floatx4*>(at)[0];
+            hi[i] = reinterpret_cast<const floatx4*>(at)[1];
         }
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i) h[i] = block * 8u + i < p.rank ? h[i] : 0.0f;
+        for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+            for (uint32_t n = 0; n < 4u; ++n) {
+                h[n] += s + i < p.parts ? lo[i][n] : 0.0f;
+                h[n + 4u] += s + i < p.parts ? hi[i][n] : 0.0f;
+            }
     }
+}
+// Block `block` of a row's terms, [term][block][8] behind `to`, from these ranks; `adapted`: the row has an adapter.
+__device__ __forceinline__ void write_terms(const AdaptParams& p, bool adapted, uint32_t block, float (&h)[8], uint16_t* to) {
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) h[i] = adapted && block < p.blocks && block * 8u + i < p.rank ? h[i] : 0.0f;
     for (uint32_t term = 0; term < (block < p.blocks ? p.terms : 1u); ++term) {
         words4 w;
 #pragma unroll
@@ -260,11 +264,8 @@ __device__ __forceinline__ void write_terms(const AdaptParams& p, uint64_t row, 
         *reinterpret_cast<words4*>(to + (term * p.blocks + block) * 8u) = w;
     }
 }
-
-// ... of 64 rows to LDS, 16 bytes more a row.
-__device__ __forceinline__ void terms_to_lds(const AdaptParams& p, uint64_t first, uint16_t* to) {
-    for (uint32_t n = threadIdx.x; n < 64u * (p.width / 8u); n += 256u) write_terms(p, first + (n & 63u), n >> 6, to + (n & 63u) * (p.width + 8u));
-}
+// Which blocks there are to write: each of the first term, which writes the others too, and those behind all terms, which are zeros.
+__device__ __forceinline__ bool writes(const AdaptParams& p, uint32_t block) { return block < p.blocks || block >= p.blocks * p.terms; }
 
 // 8 consecutive elements of an operand that has as many in a row.
 template <uint32_t DTYPE>
@@ -351,7 +352,10 @@ __global__ __launch_bounds__(256) void adapt_terms_kernel(AdaptParams p) {
     const uint32_t room = p.width / 8u;
     const uint64_t n = uint64_t(blockIdx.x) * 256u + threadIdx.x, row = n / room;
     const uint32_t block = uint32_t(n - row * room);
-    if (row < p.rows) write_terms(p, row, block, p.terms_of_h + row * p.width);
+    if (row >= p.rows || !writes(p, block)) return;
+    float h[8] = {};
+    if (block * 8u < p.rank && block < p.blocks) load_h(p, row, block, h);
+    write_terms(p, uint32_t(p.ids[row]) < p.adapters, block, h, p.terms_of_h + row * p.width);
 }
 
 // Many rows: 16 of them and 128 columns a wavefront, 64 of them a workgroup, which has b's rows of its columns in LDS.  In the instructions' terms h's rows are the rows and
@@ -440,30 +444,34 @@ __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 || OUT == ANSZP_OUT_BF1
 // waits for memory once, not for each.
 template <uint32_t BASE, uint32_t OUT, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
-    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u;
+    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u, kRing = 4u;
     extern __shared__ __attribute__((aligned(16))) uint16_t terms_of_h[];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
     const uint64_t first = uint64_t(tile) * 64u;
-    const int32_t id = tile_ids(p, first, piece == 0u && wave == 0u);
-    uint32_t of_wave = lane & 3u;                                   // (rows without an adapter are anyone's)
-    {
-        uint32_t turn = 0u;
-        Adapters adapters(id);
-        while (adapters.next() >= 0) {
-            if (adapters.lanes >> lane & 1u) of_wave = turn & 3u;
-            ++turn;
-        }
+    const Eighth cols(uint64_t(piece) * 32u + g * 8u, p.cols), cols_of_b(uint64_t(piece) * 32u + (c >> 2) * 8u, p.cols);
+    // All that does not wait for the rows' ids is asked for first: their operands, and the first piece of h that this thread writes to LDS.
+    Eight<BASE> base[4];
+    Eight<OUT> beside[4];
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r) {
+        const uint64_t row = least(first + r * 16u + c, p.rows - 1u);
+        base[r] = eight<BASE>(p.base, row * p.base_stride + cols.at);
+        if (p.mul) beside[r] = eight<OUT>(p.mul, row * p.mul_stride + cols.at);
+        else if (p.residual) beside[r] = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
     }
+    float h[8] = {};
+    if (wave < p.blocks && wave * 8u < p.rank) load_h(p, least(first + lane, p.rows - 1u), wave, h);
+    const int32_t id = tile_ids(p, first, piece == 0u && wave == 0u);
+    const uint32_t of_wave = (id < 0 ? lane : uint32_t(id) ^ uint32_t(id) >> 2 ^ uint32_t(id) >> 4) & 3u;          // (rows without an adapter are anyone's)
     // A piece of an adapter: four blocks of its ranks.
     struct Piece {
         words4 b[2];
         int32_t one;
         uint32_t s;
         uint64_t lanes;
-    } ring[4];
+    } ring[kRing];
     const uint32_t steps = steps_of<OUT>(p);
-    const Eighth cols(uint64_t(piece) * 32u + g * 8u, p.cols), cols_of_b(uint64_t(piece) * 32u + (c >> 2) * 8u, p.cols);
     const uint16_t* const b_at = p.b + (cols_of_b.at + (c & 3u)) * p.b_row_stride;
     Adapters adapters(of_wave == wave ? id : -1);
     int32_t asked = -1;
@@ -481,28 +489,26 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
         for (uint32_t t = 0; t < 2u; ++t) to.b[t] = ranks_of<WHOLE>(p, b_at + uint64_t(asked) * p.b_stride + t * 4u * p.b_row_stride, block_of(p, asked_at, g));
     };
 #pragma unroll
-    for (uint32_t i = 0; i < 4u; ++i) ask(ring[i]);
+    for (uint32_t i = 0; i < kRing; ++i) ask(ring[i]);
     int32_t own[4];
     bool mine[4];
-    Eight<BASE> base[4];
-    Eight<OUT> beside[4];
 #pragma unroll
     for (uint32_t r = 0; r < 4u; ++r) {
-        const uint64_t row = least(first + r * 16u + c, p.rows - 1u);
         own[r] = __shfl(id, r * 16u + c);
         mine[r] = __shfl(of_wave, r * 16u + c) == wave && first + r * 16u + c < p.rows;
-        base[r] = eight<BASE>(p.base, row * p.base_stride + cols.at);
-        if (p.mul) beside[r] = eight<OUT>(p.mul, row * p.mul_stride + cols.at);
-        else if (p.residual) beside[r] = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
     }
-    terms_to_lds(p, first, terms_of_h);
+    for (uint32_t block = wave; block < p.width / 8u; block += 4u) {
+        if (!writes(p, block)) continue;
+        if (block != wave && block < p.blocks && block * 8u < p.rank) load_h(p, least(first + lane, p.rows - 1u), block, h);
+        write_terms(p, id >= 0, block, h, terms_of_h + lane * (p.width + 8u));
+    }
     // (out may be one of the operands: what another wavefront stores has been read by all behind this, too)
     __syncthreads();
     const uint16_t* const h_at = terms_of_h + c * (p.width + 8u) + g * 8u;
     floatx4 sum[4][2] = {}, part[4][2] = {};
     for (bool more = true; more;) {
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i) {
+        for (uint32_t i = 0; i < kRing; ++i) {
             Piece& now = ring[i];
             if (now.one < 0) {
                 more = false;
@@ -524,12 +530,14 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
             }
             if (now.s + 1u == steps) {
 #pragma unroll
-                for (uint32_t r = 0; r < 4u; ++r)
+                for (uint32_t r = 0; r < 4u; ++r) {
+                    if (!(now.lanes >> (16u * r) & 0xFFFFu)) continue;
 #pragma unroll
                     for (uint32_t t = 0; t < 2u; ++t) {
                         sum[r][t] = own[r] == now.one ? part[r][t] : sum[r][t];
                         part[r][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
                     }
+                }
             }
             ask(now);
         }
@@ -611,8 +619,9 @@ Plan plan_of(const anszp_adapt_args_t& a) {
         q.width = 32u;
         return q;
     }
-    const uint32_t tiles = static_cast<uint32_t>((a.rows + 63u) / 64u), steps = a.x_dtype == ANSZP_I8 ? (a.k + 127u) / 128u : (a.k + 63u) / 64u, sixteens = (a.rank + 15u) / 16u;
+    const uint32_t tiles = static_cast<uint32_t>((a.rows + 63u) / 64u), sixteens = (a.rank + 15u) / 16u;
     q.ranks = sixteens <= 1u ? 1u : sixteens <= 2u ? 2u : 4u;
+    const uint32_t once = at_once(a.x_dtype == ANSZP_I8, q.ranks), steps = (a.k + once - 1u) / once;
     q.groups = (sixteens + q.ranks - 1u) / q.ranks;
     // A step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose rows are not the first of an adapter leave at once.  k in parts
     // until there are two workgroups a CU, though h's parts are read again by every workgroup of the second product where rows are few.

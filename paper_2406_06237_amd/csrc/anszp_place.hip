@@ -233,6 +233,12 @@ __global__ __launch_bounds__(256) void place_tokens_kernel(PlaceParams p) {
     }
 }
 
+// The threads of the one workgroup that does all of a call, or 0: it has few tokens to place and few sequences whose pages could go back.  (16 sequences with a token
+// each: ONE us in one launch, TWO in two.)  256 keep what the tokens need in LDS.
+uint32_t alone(const anszp_place_args_t& a) {
+    return a.n_tokens <= 1024u && a.n_seqs <= 256u && !a.ends ? 256u : a.n_tokens <= 4096u && (!a.ends || a.n_seqs <= 64u) ? 1024u : 0u;
+}
+
 int place_check(const anszp_place_args_t& a) {
     if (a.page_size < 16u || a.page_size > 65536u || (a.page_size & (a.page_size - 1u)) || a.table_width == 0u || a.n_seqs >= 1ull << 24 || a.n_tokens >= 1ull << 31 ||
         a.free_room >= 1ull << 31 || uint64_t(a.table_width) * a.page_size > 1ull << 30)
@@ -242,18 +248,21 @@ int place_check(const anszp_place_args_t& a) {
 
 }  // namespace
 
-extern "C" uint64_t anszp_place_workspace_bytes(const anszp_place_args_t* a) { return !a || place_check(*a) ? 0u : (a->n_seqs * sizeof(Record) + 15u) & ~15ull; }
+extern "C" uint64_t anszp_place_workspace_bytes(const anszp_place_args_t* a) {
+    return !a || place_check(*a) || alone(*a) == 256u ? 0u : (a->n_seqs * sizeof(Record) + 15u) & ~15ull;
+}
 
 extern "C" int anszp_place(const anszp_place_args_t* a, void* hip_stream) {
     if (!a) return ANSZP_E_NULL;
     const int rc = place_check(*a);
     if (rc) return rc;
     if (!a->n_free || !a->n_free_out || !a->starts || (a->n_tokens && !a->slots) || (a->free_room && !a->free_pages)) return ANSZP_E_NULL;
-    if (a->n_seqs && (!a->pages || !a->lengths || !a->lengths_out || !a->new_tokens || !a->workspace)) return ANSZP_E_NULL;
-    if (a->workspace_bytes < anszp_place_workspace_bytes(a) || (reinterpret_cast<uintptr_t>(a->workspace) & 15u)) return ANSZP_E_RANGE;
+    const uint64_t need = anszp_place_workspace_bytes(a);
+    if ((a->n_seqs && (!a->pages || !a->lengths || !a->lengths_out || !a->new_tokens)) || (need && !a->workspace)) return ANSZP_E_NULL;
+    if (a->workspace_bytes < need || (reinterpret_cast<uintptr_t>(a->workspace) & 15u)) return ANSZP_E_RANGE;
     // What is written may meet nothing that other threads still read or write: lengths and n_free may be their own outputs.
     const Rows written[] = {{a->pages, 1, 0, a->n_seqs * a->table_width * 4u}, {a->free_pages, 1, 0, a->free_room * 4u}, {a->slots, 1, 0, a->n_tokens * 8u},
-                            {a->owners, 1, 0, a->n_tokens * 4u}, {a->starts, 1, 0, (a->n_seqs + 1u) * 4u}, {a->workspace, 1, 0, a->n_seqs * sizeof(Record)},
+                            {a->owners, 1, 0, a->n_tokens * 4u}, {a->starts, 1, 0, (a->n_seqs + 1u) * 4u}, {a->workspace, 1, 0, need},
                             {a->lengths_out, 1, 0, a->n_seqs * 4u}, {a->n_free_out, 1, 0, 4}};
     const Rows lengths = {a->lengths, 1, 0, a->n_seqs * 4u}, n_free = {a->n_free, 1, 0, 4};
     const Rows read[] = {{a->new_tokens, 1, 0, a->n_seqs * 4u}, {a->ends, 1, 0, a->n_seqs * 4u}};
@@ -270,11 +279,9 @@ extern "C" int anszp_place(const anszp_place_args_t* a, void* hip_stream) {
                      static_cast<Record*>(a->workspace), static_cast<uint32_t>(a->n_seqs), static_cast<uint32_t>(a->n_tokens), static_cast<uint32_t>(a->free_room),
                      a->table_width, static_cast<uint32_t>(__builtin_ctz(a->page_size))};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    // One launch where a workgroup has few tokens to place and few sequences whose pages could go back (16 sequences with a token each: ONE us, in two launches TWO);
-    // else the pages and the tokens have the chip.
-    if (a->n_tokens <= 1024u && a->n_seqs <= 256u && !a->ends) {
+    if (alone(*a) == 256u) {
         hipLaunchKernelGGL((place_sequences_kernel<256u, true>), dim3(1), dim3(256), 0, s, p);
-    } else if (a->n_tokens <= 4096u && (!a->ends || a->n_seqs <= 64u)) {
+    } else if (alone(*a) == 1024u) {
         hipLaunchKernelGGL((place_sequences_kernel<1024u, true>), dim3(1), dim3(1024), 0, s, p);
     } else {
         hipLaunchKernelGGL((place_sequences_kernel<1024u, false>), dim3(1), dim3(1024), 0, s, p);
