@@ -1,0 +1,181 @@
+"""GPU: the serving step's operators together, as linear_block's Serving runs them: tokens placed, looked up, through the block with an adapter for each sequence, and drawn."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import serving_plain as P
+from paper_2406_06237_amd import binding as B
+from paper_2406_06237_amd import linear_block as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+D_MODEL, D_FF, KV_HEADS, VOCABULARY, SEQUENCES, RANK = 256, 704, 1, 1000, 3, 12
+SETTINGS = dict(temperature=0.9, top_k=40, top_p=0.9, min_p=0.01)
+
+
+def _serving(adapted, most=200, seed=3):
+    workload = L.block_workload(D_MODEL, D_FF, KV_HEADS, seed=seed)
+    block = L.Block(workload, SEQUENCES * -(-most // L.PAGE_SIZE))
+    block.decode()
+    adapters = L.new_adapters(workload, 2, RANK, seed=5) if adapted else None
+    serving = L.Serving(block, L.vocabulary_workload(D_MODEL, VOCABULARY, seed=seed), SEQUENCES, most, adapters, seed=1)
+    serving.adapter_of.copy_(torch.tensor([1, -1, 0], dtype=torch.int32))
+    return workload, serving
+
+
+def _ints(a):
+    return torch.tensor(a, dtype=torch.int32, device=DEV)
+
+
+def _plain_logits(workload, serving, tokens, adapter):
+    """The last token's logits of one sequence in 64 bits, nothing quantised but the weights."""
+    w = {l.name: torch.from_numpy((s.astype(np.float64).reshape(l.shape) - l.zero_point) * l.channel_scales.astype(np.float64)[:, None])
+         for l, s in zip(workload.layers, workload.symbols())}
+    if adapter >= 0 and serving.adapters:
+        for name, its in serving.adapters.items():
+            w[name] = w[name] + float(its.scales[adapter]) * its.b[adapter].cpu().double() @ its.a[adapter].cpu().double()
+    we, wl = ((m.symbols.cpu().double() - m.zero_point) * m.scales.cpu().double()[:, None] for m in (serving.words, serving.logits))
+    norm = lambda t: t / torch.sqrt((t * t).mean(-1, keepdim=True) + 1e-6)
+    x = we[tokens] * math.sqrt(D_MODEL)
+    n = norm(x)
+    q, k, v = ((n @ w[m].T).view(len(x), -1, L.HEAD_DIM) for m in ("wq", "wk", "wv"))
+    group = q.shape[1] // k.shape[1]
+    scores = torch.einsum("thd,shd->hts", q, k.repeat_interleave(group, 1)) / math.sqrt(L.HEAD_DIM)
+    scores = scores.masked_fill(torch.ones(len(x), len(x), dtype=torch.bool).triu(1), -math.inf)
+    x = x + torch.einsum("hts,shd->thd", torch.softmax(scores, -1), v.repeat_interleave(group, 1)).reshape(len(x), -1) @ w["wo"].T
+    n = norm(x)
+    gate = n @ w["wg"].T
+    x = x + (gate * torch.sigmoid(gate) * (n @ w["wu"].T)) @ w["wd"].T
+    return norm(x[-1]) @ wl.T
+
+
+# Rows of 8 bits are off by at most 13 % of the block's result, if nothing averages out (rows of normal numbers: half a step of largest / 127 is 2 % of their root mean square, three kinds
+# of rows and the cache's vectors 2 % each, the last 5 %), and the last norm's row by 2 % more; the logits are a product of that.
+@pytest.mark.parametrize("adapted", [False, True])
+def test_a_prompt_and_steps(adapted):
+    workload, serving = _serving(adapted)
+    g = torch.Generator().manual_seed(8)
+    history = [torch.randint(0, VOCABULARY, (n,), generator=g).tolist() for n in (70, 1, 129)]
+    new = [len(t) for t in history]
+    tokens = torch.tensor(sum(history, []), device=DEV)
+    for step in range(3):
+        u = torch.rand(SEQUENCES, generator=g).to(DEV)
+        drawn, chances, logits = serving.step(tokens, _ints(new), u, **SETTINGS)
+        assert serving.lengths.tolist() == [len(t) for t in history]
+        for s, its in enumerate(history):
+            want = _plain_logits(workload, serving, its, int(serving.adapter_of[s]))
+            off = (logits[s].cpu().double() - want).norm() / want.norm()
+            assert off < 0.15, (step, s, float(off))
+            f = lambda v: float(np.float32(v))
+            token, chance = P.drawn(*P.kept(logits[s].cpu().numpy(), f(0.9), 40, f(0.9), f(0.01)), float(u[s]))
+            assert int(drawn[s]) == token and abs(float(chances[s]) - chance) <= chance * 2.0 ** -23
+            its.append(token)
+        new, tokens = [1] * SEQUENCES, drawn
+    assert serving.block.cache.status.tolist() == [0, 0]
+    if adapted:
+        assert next(iter(serving.adapters.values())).status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("adapted", [False, True])
+def test_captured_steps_are_the_eager_ones(adapted):
+    """Replayed several times, with eager work between: the same tokens, chances and logits as without a graph."""
+    results = []
+    for captured in (False, True):
+        _, serving = _serving(adapted)
+        g = torch.Generator().manual_seed(9)
+        tokens = torch.randint(0, VOCABULARY, (33 + 2 + 60,), generator=g).to(DEV)
+        u = torch.rand(7, SEQUENCES, generator=g).to(DEV)
+        tokens, _, _ = serving.step(tokens, _ints([33, 2, 60]), u[0], **SETTINGS)
+        one, own, seen = _ints([1] * SEQUENCES), u[1].clone(), []
+        if captured:
+            graph, out = serving.captured_step(tokens, one, own, **SETTINGS)
+        for i in range(1, 7):
+            own.copy_(u[i])
+            if captured:
+                graph.replay()
+            else:
+                out = serving.step(tokens, one, own, **SETTINGS)
+            seen += [t.clone() for t in out]
+            tokens.copy_(out[0])
+            torch.cuda.synchronize()
+            torch.randn(1000, device=DEV).sum()                          # (the program's own work between replays)
+        results.append([*seen, serving.lengths, serving.n_free, serving.pages])
+    for eager, replayed in zip(*results):
+        assert torch.equal(eager, replayed)
+
+
+def test_sequences_end_and_begin_anew():
+    """Places are refilled in a step: the others go on, pages come back, and the results are those of sequences that had the place for themselves."""
+    _, serving = _serving(True)
+    _, alone = _serving(True)
+    g = torch.Generator().manual_seed(4)
+    first, second = (torch.randint(0, VOCABULARY, (n,), generator=g).to(DEV) for n in (100 + 50 + 150, 1 + 80 + 1))
+    u = torch.rand(2, SEQUENCES, generator=g).to(DEV)
+    serving.step(first, _ints([100, 50, 150]), u[0], **SETTINGS)
+    _, _, got = serving.step(second, _ints([1, 80, 1]), u[1], ends=_ints([0, 1, 0]), **SETTINGS)
+    _, _, want = alone.step(second[1:81], _ints([0, 80, 0]), u[1], **SETTINGS)
+    assert torch.equal(got[1], want[1]) and serving.lengths.tolist() == [101, 80, 151]
+    held = [-(-n // L.PAGE_SIZE) for n in serving.lengths.tolist()]
+    assert int(serving.n_free) == serving.block.cache.k.shape[0] - sum(held)
+    pages = sum((serving.pages[s, :n].tolist() for s, n in enumerate(held)), []) + serving.free[:int(serving.n_free)].tolist()
+    assert sorted(pages) == list(range(serving.block.cache.k.shape[0])) and serving.block.cache.status.tolist() == [0, 0]
+
+
+def test_two_graphs_and_an_eager_call_do_not_share_memory():
+    """Captured calls keep workspaces of their own: replayed in turn, with eager calls of other sizes between, each gives what it gave."""
+    g = torch.Generator(device=DEV).manual_seed(6)
+    rnd = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    graphs = []
+    for rows in (5, 700):
+        o = dict(base=rnd(rows, 300), x=rnd(rows, 500).to(torch.bfloat16), a=rnd(6, 20, 500).to(torch.bfloat16), b=rnd(6, 300, 20).to(torch.bfloat16),
+                 ids=torch.randint(-1, 6, (rows,), dtype=torch.int32, device=DEV, generator=g))
+        logits, u = rnd(rows, 3000) * 3, torch.rand(rows, device=DEV, generator=g)
+        table, free = torch.zeros(rows, 3, dtype=torch.int32, device=DEV), torch.arange(3 * rows, dtype=torch.int32, device=DEV)
+        held, n_free, new = torch.zeros(rows, dtype=torch.int32, device=DEV), _ints([3 * rows]), torch.full((rows,), 20, dtype=torch.int32, device=DEV)
+        work = lambda o=o, l=logits, u=u, t=table, f=free, h=held, n=n_free, k=new, r=rows: [B.adapt(**o), *B.sample(l, u, top_p=0.8), *B.place_tokens(t, 16, h, k, f, n, 20 * r)]  # noqa: E731
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            work()
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = work()
+        graphs.append((graph, out, [t.clone() for t in work()], work))
+    for _ in range(3):
+        for graph, out, want, work in graphs:
+            for t in out:
+                t.zero_()
+            graph.replay()
+            eager = work()
+            torch.cuda.synchronize()
+            for a, b, c in zip(out, want, eager):
+                assert torch.equal(a, b) and torch.equal(c, b)
+
+
+def test_both_of_the_bindings_paths_give_the_same(monkeypatch):
+    def everything():
+        g = torch.Generator(device=DEV).manual_seed(3)
+        rnd = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+        table, status = torch.full((2, 4), -1, dtype=torch.int32, device=DEV), _ints([0, 0])
+        out = [*B.place_tokens(table, 16, _ints([0, 0]), _ints([20, 3]), _ints(list(range(9))), _ints([9]), 30, ends=_ints([0, 1]), status=status), table, status]
+        tokens = torch.tensor([3, -1, 7, 20], device=DEV)
+        symbols = torch.randint(0, 16, (9, 70), device=DEV, generator=g).to(torch.uint8)
+        out += [B.embed(tokens, symbols, 7, rnd(9), 2.0, status=status), B.embed(tokens, rnd(9, 70).to(torch.bfloat16), out_dtype="f32"), status]
+        into = torch.zeros(4, 100, dtype=torch.bfloat16, device=DEV)
+        B.embed(tokens, symbols, out=into[:, 5:75])
+        x = torch.randint(-100, 100, (4, 64), device=DEV, generator=g).to(torch.int8)
+        o = dict(a=rnd(3, 10, 64).to(torch.bfloat16), b=rnd(3, 70, 10).to(torch.bfloat16), ids=_ints([2, -1, 0, 9]), x_scales=rnd(4), scales=rnd(3), status=status)
+        out += [into, B.adapt(out[-3], x, **o, activation="gelu", residual=rnd(4, 70).to(torch.bfloat16)), B.adapt(rnd(4, 70), x, **o, mul=rnd(4, 70), out_dtype="f32"), status]
+        logits = rnd(4, 500) * 3
+        out += [*B.sample(logits, torch.rand(4, device=DEV, generator=g), 0.7, 20, 0.9, 0.01), *B.sample(logits.to(torch.bfloat16), torch.rand(4, device=DEV, generator=g), top_p=rnd(4).abs(),
+                                                                                                         temperature=rnd(4).abs(), min_p=rnd(4).abs() / 9, top_k=_ints([0, 3, 400, 1]))]
+        return [t.clone() for t in out]
+
+    assert B._operator_calls()
+    native = everything()
+    monkeypatch.setattr(B, "_host", False)
+    for a, b in zip(native, everything()):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)

@@ -105,7 +105,8 @@ def test_embed_over_its_operands(other):
     (dict(rows=1 << 28), E_RANGE), (dict(cols=1 << 31), E_RANGE), (dict(k=0), E_RANGE), (dict(k=(1 << 30) + 1), E_RANGE), (dict(rank=0), E_RANGE), (dict(rank=129), E_RANGE),
     (dict(adapters=1 << 24), E_RANGE), (dict(x_dtype=B.OUT_F32), E_RANGE), (dict(x_dtype=B.OUT_U8), E_RANGE), (dict(base_dtype=B.I8), E_RANGE), (dict(out_dtype=B.OUT_U8), E_RANGE),
     (dict(activation=4), E_RANGE), (dict(out_stride=63), E_RANGE), (dict(workspace_bytes=16), E_RANGE), (dict(workspace=(1 << 32) + 8), E_RANGE),
-    (dict(rows=1 << 27, cols=1 << 10, out_stride=1 << 10, x=1 << 60, base=1 << 59, mul=None, residual=None), E_RANGE), (dict(rows=0, x=None), 0), (dict(cols=0, b=None), 0)])
+    (dict(rows=1 << 27, cols=1 << 10, out_stride=1 << 10, x=1 << 60, base=1 << 59, mul=None, residual=None), E_RANGE), (dict(rows=(1 << 28) - 1, cols=8, rank=128, x=1 << 60, base=1 << 59, ids=1 << 58, mul=None, residual=None, x_scales=None), E_RANGE),
+    (dict(rows=0, x=None), 0), (dict(cols=0, b=None), 0)])
 def test_adapt(change, code):
     assert _adapt(**change) == code
     assert B.lib().anszp_adapt(None, None) == E_NULL and B.lib().anszp_adapt_workspace_bytes(None) == 0
