@@ -627,8 +627,8 @@ int anszp_adapt(const anszp_adapt_args_t* args, void* hip_stream);
  * first token at which the sum of the kept weights, in the same order, passes uniform * (all of it); uniforms are in [0, 1), others
  * count as the nearest.  A temperature of 0 draws the first token.  Each setting is one number for all rows, or one for each.  A row that holds a NaN, or
  * nothing above -infinity, or has a temperature below 0 or NaN, has token -1 and a chance of 0; +infinities share a row alone.
- * Weights are exact to 2^-43, sums of them too (for vocabularies above 2^18, to 2^-61 of the vocabulary's size); a token below 2^-44 of the first weighs nothing.  No result depends on the
- * order of additions. */
+ * Weights are good to 5e-12 of each and 2^-44 of the largest (2^-62 times the vocabulary where that is more), their sums exact; a token below
+ * 2^-44 of the first weighs nothing.  No result depends on the order of additions. */
 typedef struct {
     const void*    logits;        /* [device] rows x vocabulary of dtype                             */
     const float*   uniforms;      /* [device] rows                                                   */

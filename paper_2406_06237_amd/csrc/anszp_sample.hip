@@ -5,10 +5,16 @@
 //
 // Sums decide which token it is, so they are whole numbers and no order of additions changes them.  With t = 64 log2(e) (max l - l) / temperature, in 64
 // bits, and b = round(t):
-//   w = 2^(-b / 64) * q,    q = 2^((b - t) / 64) in 1 +- 0.0054, which four terms of its series give to 4e-14,
-// the q are held in fixed point with 2^-44 (less only for more than 2^18 tokens) and added up for each b in LDS; a bin's mass is its sum times 2^(-b / 64), rounded down, and
-// masses are added up over the bins.  What is further down than 44 octaves weighs nothing.  A border that lies in a bin is found among the bin's own
-// tokens, every one compared with all others; where a bin has more than the list holds, it is cut by its tokens' own logits first, as often as that takes.
+//   w = 2^(-b / 64) * q,    q = 2^((b - t) / 64) in 1 +- 0.0054, which a polynomial of three powers gives to 5e-12,
+// the q are held in fixed point with 2^-44 (less only for more than 2^18 tokens) and added up for each b in LDS; a bin's mass is its sum times
+// 2^(-b / 64), rounded down, and masses are added up over the bins.  What is further down than 44 octaves weighs nothing.  Weights of 32 bits would not do: of 10000
+// tokens that are kept, one in 100000 draws would be another token than the formula's.  The bins say in which of them the border and the token are; the tokens of these are
+// listed, a few hundred, and each is compared with all others.  Where they are more than the list holds, each bin is cut by its tokens' own logits, as often
+// as that takes.  A small top_k needs no bins: a list of all tokens that may be kept is found by the threads' own largest.
+//
+// Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with the unit busy 70 % of the
+// time and LDS 27 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000 takes 16 us: each of three
+// passes waits for its first loads, and the sums between them for each other.
 #include <hip/hip_runtime.h>
 
 #include "anszp_cus.h"
@@ -81,9 +87,9 @@ __device__ __forceinline__ uint32_t most_of_wave(uint32_t v) {
     return v;
 }
 
-// A row and the workgroup of THREADS threads that has it.  HELD: so many times 8 logits a thread has in registers, which are all of the row; 0: the row is read for each
-// pass.
-template <uint32_t DTYPE, uint32_t THREADS, uint32_t HELD>
+// A row and the workgroup of THREADS threads that has it, which reads it for each pass.  (Rows up to 32768 held in registers, 64 of them a thread, took as long where rows are few and half as long again
+// where they are many, 512 of 20000 30 us instead of 20: one workgroup a CU has the registers.)
+template <uint32_t DTYPE, uint32_t THREADS>
 struct Row {
     static constexpr uint32_t kWaves = THREADS / 64u;
     Shared& sh;
@@ -93,7 +99,6 @@ struct Row {
     double top, steps, shift;           // the largest logit, 64 log2(e) / temperature, their product
     double c0, c1, c2, c3, one;         // of q
     bool far;
-    Eight<DTYPE> held[HELD ? HELD : 1u];
 
     // Eight logits; behind the row's end there is nothing that weighs.
     __device__ __forceinline__ Eight<DTYPE> eight(uint32_t at) const {
@@ -113,29 +118,16 @@ struct Row {
     // work(eight logits, the first one's token) for all tokens; a thread's come in rising order.  Several loads are under way together, and none of these looks for the row's end.
     template <class Work>
     __device__ __forceinline__ void each(Work work) const {
-        if constexpr (HELD != 0u) {
+        constexpr uint32_t kAtOnce = DTYPE == ANSZP_OUT_BF16 ? 4u : 2u;
+        uint32_t at = threadIdx.x * 8u;
+        for (; at + (kAtOnce - 1u) * THREADS * 8u + 8u <= n; at += kAtOnce * THREADS * 8u) {
+            Eight<DTYPE> l[kAtOnce];
 #pragma unroll
-            for (uint32_t j = 0; j < HELD; ++j)
-                if (j * THREADS * 8u < n) work(held[j], (j * THREADS + threadIdx.x) * 8u);
-        } else {
-            constexpr uint32_t kAtOnce = DTYPE == ANSZP_OUT_BF16 ? 4u : 2u;
-            uint32_t at = threadIdx.x * 8u;
-            for (; at + (kAtOnce - 1u) * THREADS * 8u + 8u <= n; at += kAtOnce * THREADS * 8u) {
-                Eight<DTYPE> l[kAtOnce];
+            for (uint32_t j = 0; j < kAtOnce; ++j) l[j].load(logits, from + at + j * THREADS * 8u, 8u);
 #pragma unroll
-                for (uint32_t j = 0; j < kAtOnce; ++j) l[j].load(logits, from + at + j * THREADS * 8u, 8u);
-#pragma unroll
-                for (uint32_t j = 0; j < kAtOnce; ++j) work(l[j], at + j * THREADS * 8u);
-            }
-            for (; at < n; at += THREADS * 8u) work(eight(at), at);
+            for (uint32_t j = 0; j < kAtOnce; ++j) work(l[j], at + j * THREADS * 8u);
         }
-    }
-    __device__ __forceinline__ void hold() {
-        if constexpr (HELD != 0u) {
-#pragma unroll
-            for (uint32_t j = 0; j < HELD; ++j)
-                if (j * THREADS * 8u < n) held[j] = eight((j * THREADS + threadIdx.x) * 8u);
-        }
+        for (; at < n; at += THREADS * 8u) work(eight(at), at);
     }
     __device__ __forceinline__ float logit(uint32_t id) const {
         return DTYPE == ANSZP_OUT_BF16 ? bf16_low(static_cast<const uint16_t*>(logits)[from + id]) : static_cast<const float*>(logits)[from + id];
@@ -464,16 +456,15 @@ __device__ __forceinline__ uint64_t wanted_of(float top_p, uint64_t all) {
     return wanted < 1u ? 1u : wanted > all ? all : wanted;
 }
 
-template <uint32_t DTYPE, uint32_t THREADS, uint32_t HELD>
-__global__ __launch_bounds__(THREADS, HELD ? 2 : 4) void sample_kernel(SampleParams p) {
+template <uint32_t DTYPE, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
     __shared__ Shared sh;
     const uint64_t r = uint64_t(blockIdx.y) * kAcross + blockIdx.x;
     if (r >= p.rows) return;
     const float temperature = p.temperature ? p.temperature[r] : p.any_temperature;
     const int32_t top_k = p.top_k ? p.top_k[r] : p.any_top_k;
     const Settings set = {p.uniforms[r], p.top_p ? p.top_p[r] : p.any_top_p, p.min_p ? p.min_p[r] : p.any_min_p, top_k > 0 ? uint32_t(top_k) : 0u};
-    Row<DTYPE, THREADS, HELD> row = {sh, p.logits, r * p.stride, p.vocabulary, p.point};
-    row.hold();
+    Row<DTYPE, THREADS> row = {sh, p.logits, r * p.stride, p.vocabulary, p.point};
     const auto answer = [&](int64_t token, float chance) __attribute__((always_inline)) {
         if (threadIdx.x != 0u) return;
         p.tokens[r] = token;
@@ -746,9 +737,10 @@ __global__ __launch_bounds__(THREADS, HELD ? 2 : 4) void sample_kernel(SamplePar
 template <uint32_t DTYPE>
 void launch(const SampleParams& p, hipStream_t s) {
     const dim3 grid(groups_across(p.rows), groups_down(p.rows));
-    if (p.vocabulary <= 32768u) hipLaunchKernelGGL((sample_kernel<DTYPE, 512u, 8u>), grid, dim3(512), 0, s, p);
-    else if (p.rows > device_cus()) hipLaunchKernelGGL((sample_kernel<DTYPE, 512u, 0u>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((sample_kernel<DTYPE, 1024u, 0u>), grid, dim3(1024), 0, s, p);
+    // More rows than compute units: half the threads, so that a CU has two rows at a time and goes on with one where the other waits.  (512 rows of 131072 in bf16 88 us, with 1024
+    // threads 103; 32 rows of 131072 52 us with 1024 threads, 68 with 512; short rows take the same.)
+    if (p.rows > device_cus()) hipLaunchKernelGGL((sample_kernel<DTYPE, 512u>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((sample_kernel<DTYPE, 1024u>), grid, dim3(1024), 0, s, p);
 }
 
 }  // namespace

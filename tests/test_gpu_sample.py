@@ -26,8 +26,8 @@ def _check(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     for r, (row, x, t, k, p, m) in enumerate(zip(logits.float().cpu().numpy(), uniforms.tolist(), each(temperature), each(top_k), each(top_p), each(min_p))):
         token, chance = P.drawn(*P.kept(row, t, k, p, m), x)
         assert int(tokens[r]) == token, (r, int(tokens[r]), token, t, k, p, m, x)
-        # one rounding to 32 bits, and weights that are off by 4e-14
-        assert abs(float(chances[r]) - chance) <= chance * (2.0 ** -24 + 1e-12), (r, float(chances[r]), chance)
+        # one rounding to 32 bits, and weights whose polynomial leaves (ln2 / 128)^4 / 192 = 4.5e-12, in the token's and in the sum
+        assert abs(float(chances[r]) - chance) <= chance * (2.0 ** -24 + 1e-11), (r, float(chances[r]), chance)
     return tokens
 
 
