@@ -226,22 +226,23 @@ __device__ __forceinline__ uint16_t part_of(float h) {
 }
 
 // Eight ranks of h of a row, the parts of k added up; what a row without an adapter has there is not looked at.
+template <uint32_t AT_ONCE>
 __device__ __forceinline__ void load_h(const AdaptParams& p, uint64_t row, uint32_t block, float (&h)[8]) {
     const float* const from = p.h + row * p.rank_room + block * 8u;
     const uint64_t apart = p.rows * p.rank_room;
 #pragma unroll
     for (uint32_t i = 0; i < 8u; ++i) h[i] = 0.0f;
-    // (four under way together; behind the last one it is read again, and not added)
-    for (uint32_t s = 0; s < p.parts; s += 4u) {
-        floatx4 lo[4], hi[4];
+    // (several under way together; behind the last one it is read again, and not added)
+    for (uint32_t s = 0; s < p.parts; s += AT_ONCE) {
+        floatx4 lo[AT_ONCE], hi[AT_ONCE];
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i) {
+        for (uint32_t i = 0; i < AT_ONCE; ++i) {
             const float* at = from + (s + i < p.parts ? s + i : p.parts - 1u) * apart;
             lo[i] = reinterpret_cast<const floatx4*>(at)[0];
             hi[i] = reinterpret_cast<const floatx4*>(at)[1];
         }
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i)
+        for (uint32_t i = 0; i < AT_ONCE; ++i)
 #pragma unroll
             for (uint32_t n = 0; n < 4u; ++n) {
                 h[n] += s + i < p.parts ? lo[i][n] : 0.0f;
@@ -354,7 +355,10 @@ __global__ __launch_bounds__(256) void adapt_terms_kernel(AdaptParams p) {
     const uint32_t block = uint32_t(n - row * room);
     if (row >= p.rows || !writes(p, block)) return;
     float h[8] = {};
-    if (block * 8u < p.rank && block < p.blocks) load_h(p, row, block, h);
+    if (block * 8u < p.rank && block < p.blocks) {
+        if (p.parts > 4u) load_h<16u>(p, row, block, h);
+        else load_h<4u>(p, row, block, h);
+    }
     write_terms(p, uint32_t(p.ids[row]) < p.adapters, block, h, p.terms_of_h + row * p.width);
 }
 
@@ -461,7 +465,7 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
         else if (p.residual) beside[r] = eight<OUT>(p.residual, row * p.residual_stride + cols.at);
     }
     float h[8] = {};
-    if (wave < p.blocks && wave * 8u < p.rank) load_h(p, least(first + lane, p.rows - 1u), wave, h);
+    if (wave < p.blocks && wave * 8u < p.rank) load_h<4u>(p, least(first + lane, p.rows - 1u), wave, h);
     const int32_t id = tile_ids(p, first, piece == 0u && wave == 0u);
     const uint32_t of_wave = (id < 0 ? lane : uint32_t(id) ^ uint32_t(id) >> 2 ^ uint32_t(id) >> 4) & 3u;          // (rows without an adapter are anyone's)
     // A piece of an adapter: four blocks of its ranks.
@@ -499,7 +503,7 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
     }
     for (uint32_t block = wave; block < p.width / 8u; block += 4u) {
         if (!writes(p, block)) continue;
-        if (block != wave && block < p.blocks && block * 8u < p.rank) load_h(p, least(first + lane, p.rows - 1u), block, h);
+        if (block != wave && block < p.blocks && block * 8u < p.rank) load_h<4u>(p, least(first + lane, p.rows - 1u), block, h);
         write_terms(p, id >= 0, block, h, terms_of_h + lane * (p.width + 8u));
     }
     // (out may be one of the operands: what another wavefront stores has been read by all behind this, too)
@@ -626,7 +630,7 @@ Plan plan_of(const anszp_adapt_args_t& a) {
     // A step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose rows are not the first of an adapter leave at once.  k in parts
     // until there are two workgroups a CU, though h's parts are read again by every workgroup of the second product where rows are few.
     const uint32_t rows = static_cast<uint32_t>(a.rows < 64u ? a.rows : 64u), likely = a.rows < 512u ? (rows < a.adapters ? rows : a.adapters) : 1u;
-    q.slots = a.rows < 512u ? rows : a.rows < 4096u ? (a.adapters < 8u ? a.adapters : 8u) : a.adapters < 2u ? 1u : 2u;
+    q.slots = a.rows < 512u ? rows : a.adapters < 2u ? 1u : a.adapters <= 8u || a.rows >= 4096u ? 2u : 8u;
     const uint32_t groups = tiles * likely * q.groups, most = (steps + 1u) / 2u, read_again = a.rows <= 4u ? 16u : a.rows <= 16u ? 8u : a.rows <= 256u ? 4u : 16u;
     q.parts = (2u * device_cus() + groups - 1u) / groups;
     if (q.parts > read_again) q.parts = read_again;
