@@ -697,7 +697,7 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
         return ANSZP_E_RANGE;
     if ((a->rows + 63u) / 64u * ((a->cols + 31u) / 32u) >= 1ull << 24) return ANSZP_E_RANGE;          // (threads that one launch has not)
     const Plan q = plan_of(*a);
-    if (a->rows * (q.width / 8u) >= 1ull << 32) return ANSZP_E_RANGE;
+    if (a->rows * (q.width / 8u) >= 1ull << 32 || (q.any_down && a->rows * a->rank >= 1ull << 32) || (q.any_up && a->rows * a->cols >= 1ull << 32)) return ANSZP_E_RANGE;
     if (q.workspace && !a->workspace) return ANSZP_E_NULL;
     if (q.workspace && (a->workspace_bytes < q.workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u))) return ANSZP_E_RANGE;
     AdaptParams p = {};

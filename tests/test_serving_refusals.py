@@ -119,6 +119,13 @@ def test_adapt_over_its_operands(other, by):
     assert B.lib().anszp_adapt(C.addressof(a), None) == E_RANGE
 
 
+@pytest.mark.parametrize("change", [dict(rows=1 << 26, rank=128, k=4, a_row_stride=0), dict(rows=1 << 15, cols=1 << 17, rank=4, b_row_stride=0, base_stride=1 << 17, out_stride=1 << 17)])
+def test_adapt_of_operands_of_a_few_bytes_by_more_threads_than_one_launch_has(change):
+    """A thread an element: 2^33 of h, 2^32 of the output."""
+    apart = dict(adapters=1, workspace_bytes=1 << 50, x=1 << 60, base=1 << 59, ids=1 << 58, out=1 << 57, mul=None, residual=None, x_scales=None, scales=None)
+    assert _adapt(**{**apart, **change}) == E_RANGE
+
+
 def test_adapt_over_a_base_of_another_type_or_stride():
     for change in (dict(base_dtype=B.OUT_F32), dict(base_stride=80)):
         a = _args(B.AdaptArgs, ADAPT, change)
