@@ -7,15 +7,17 @@
 // All of it are sums over the sequences and a look-up a token, so nothing depends on the order in which threads arrive.
 //
 // One workgroup adds up over the sequences and leaves a record for each; a thread a token then finds its sequence in the starts and its page
-// in the table or on the stack, and writes the table where it is the first in its page.  Latency bounds both: LATENCY
+// in the table or on the stack, and writes the table where it is the first in its page.  Latency bounds it, of loads and of the sums' barriers: 16 sequences with a
+// token each take 3.6 us, 512 sequences with 151000 tokens and some of them ended 7.0 for the sums, 2.5 for the pages that go back and 4.6 for the tokens, whose
+// starts, looked up eight or nine times each, are in LDS (from memory 7).
 #include <hip/hip_runtime.h>
 
 #include "anszp_numbers.h"
 
 namespace {
 
-// What a sequence's tokens need to know: tokens before this step (-1: refused), pages before it, and the stack's place of its first new page; and where its pages go that
-// it gives back, and how many.
+// What a sequence's tokens need to know: tokens before this step (-1: refused), pages before it, and the stack's place of its first new page; and
+// where its pages go that it gives back, and how many.
 struct Record {
     int32_t old, pages, top, back_at, back;
 };
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(256) void place_tokens_kernel(PlaceParams p) {
 }
 
 // The threads of the one workgroup that does all of a call, or 0: it has few tokens to place and few sequences whose pages could go back.  (16 sequences with a token
-// each: ONE us in one launch, TWO in two.)  256 keep what the tokens need in LDS.
+// each: 3.6 us in one launch, 5.3 and 1.8 in two.)  256 keep what the tokens need in LDS.
 uint32_t alone(const anszp_place_args_t& a) {
     return a.n_tokens <= 1024u && a.n_seqs <= 256u && !a.ends ? 256u : a.n_tokens <= 4096u && (!a.ends || a.n_seqs <= 64u) ? 1024u : 0u;
 }
