@@ -454,7 +454,7 @@ typedef struct {
     const void*  mul;             /* [device] rows x cols of out_dtype, or NULL                      */
     const void*  residual;        /* [device] rows x cols of out_dtype, or NULL                      */
     void*        out;             /* [device] rows x cols of out_dtype; may be mul or residual (same stride), apart from x and weight */
-    uint64_t     rows, cols;      /* each < 2^31, may be 0; fewer than 2^24 tiles of 64 x 32 together, rows * (rank up to a multiple of 32) < 2^33, and < 2^32 rows * rank with x or a of fewer than 16 bytes, rows * cols with b */
+    uint64_t     rows, cols;      /* each < 2^31, may be 0; fewer than 2^24 tiles of 64 x 64 together */
     uint64_t     x_stride, weight_stride, mul_stride, residual_stride, out_stride;
     uint32_t     k;               /* 1 .. 2^30 (x in 8 bits: 65536, so that sums fit 32 bits)        */
     uint32_t     x_dtype;         /* ANSZP_OUT_BF16 or ANSZP_I8                                      */
@@ -606,7 +606,8 @@ typedef struct {
     uint32_t*      status;        /* [device] 2 words, or NULL: ANSZP_ST_BAD_DESC for an id beyond the adapters, whose row has none then, counted */
     void*          workspace;     /* [device] anszp_adapt_workspace_bytes, 16-byte aligned, in use until the call is done */
     uint64_t       workspace_bytes;
-    uint64_t       rows, cols;    /* < 2^28, < 2^31, may be 0; fewer than 2^24 tiles of 64 x 32 together, rows * (rank up to a multiple of 32) < 2^33, and < 2^32 rows * rank with x or a of fewer than 16 bytes, rows * cols with b */
+    uint64_t       rows, cols;    /* < 2^28, < 2^31, may be 0; fewer than 2^24 tiles of 64 x 32 together, rows * (rank up to a multiple of 32) < 2^33; with x or a
+                                   * of fewer than 16 bytes rows * rank < 2^32, with such a b rows * cols */
     uint64_t       x_stride, a_stride, a_row_stride, b_stride, b_row_stride, base_stride, mul_stride, residual_stride, out_stride;
     uint32_t       adapters;      /* < 2^24, may be 0                                                */
     uint32_t       k;             /* 1 .. 2^30                                                       */

@@ -3,12 +3,12 @@
 // and no adapter's part for ids below 0.  Two launches: h from all of k, then the output's columns.
 //
 // Rows come in tiles of 64, and a tile is worked through once for each adapter that its rows have: one for a prompt, up to 64 for a step of as
-// many requests.  What a row has from other rows' adapters is never selected, so that nothing in them, an infinity or a NaN, reaches it.  x and a are bf16 (8-bit rows are exact in
-// it), their sums in 32 bits.  h goes into the second product as two bf16 numbers, to 2^-18 of it, for bf16 outputs, and as three, all of it, for fp32 ones: a number rounded
-// to bf16 leaves a rest that is exact.
+// many requests.  What a row has from other rows' adapters is never selected, so that nothing in them, an infinity or a NaN, reaches it.  x and a are bf16
+// (8-bit rows are exact in it), their sums in 32 bits.  h goes into the second product as two bf16 numbers, to 2^-18 of it, for bf16 outputs, and as three,
+// all of it, for fp32 ones: a number rounded to bf16 leaves a rest that is exact.
 //
-// Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h 25 us (1.4 TB/s of x, 175
-// TFLOP/s), its terms 5, the columns 140 (3.9 TB/s; what streams three such matrices and does nothing else reaches 5.9).  1531 rows from 11008 bf16
+// Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h
+// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 140 (3.9 TB/s; what streams three such matrices and does nothing else reaches 5.9).  1531 rows from 11008 bf16
 // to 4096 fp32 with a residual, rank 24: 15, 5 and 21 (3.7 TB/s).  64 requests with 48 adapters of rank 16: 8 and 12.5 us, most of them waiting for loads.
 #include <hip/hip_runtime.h>
 
@@ -104,9 +104,9 @@ struct Adapters {
     }
 };
 
-// h of 64 rows and up to 16 * RANKS ranks, 16 rows a wavefront.  128 or 256 bytes of each row of x and as much of k of a's rows go to LDS at a time, in pieces of 16 bytes end to
-// end (operands taken from memory as the instructions want them are 16 bytes of 16 rows for every 16 lanes, and a CU looks up four times the lines: 33 us for
-// 8192 rows of 4096 bytes and rank 64, this 25); two times of them are under way beside the one in LDS.
+// h of 64 rows and up to 16 * RANKS ranks, 16 rows a wavefront.  128 or 256 bytes of each row of x and as much of k of a's rows go to LDS at a time, in
+// pieces of 16 bytes end to end (operands taken from memory as the instructions want them are 16 bytes of 16 rows for every 16 lanes, and a CU looks up four
+// times the lines: 33 us for 8192 rows of 4096 bytes and rank 64, this 25); two times of them are under way beside the one in LDS.
 constexpr uint32_t at_once(bool bytes, uint32_t ranks) { return bytes || ranks <= 2u ? 128u : 64u; }
 template <bool BYTES, uint32_t RANKS>
 __global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
@@ -629,8 +629,8 @@ Plan plan_of(const anszp_adapt_args_t& a) {
     q.ranks = sixteens <= 1u ? 1u : sixteens <= 2u ? 2u : 4u;
     const uint32_t once = at_once(a.x_dtype == ANSZP_I8, q.ranks), steps = (a.k + once - 1u) / once;
     q.groups = (sixteens + q.ranks - 1u) / q.ranks;
-    // A step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose rows are not the first of an adapter leave at once.  (1531 rows with five adapters
-    // 15.3 us with two workgroups that share a tile's adapters, 18.8 with five: each asks for its tile's ids before it can leave.)
+    // A step's rows may have an adapter each, a prompt's tiles have one or two: workgroups whose rows are not the first of an adapter leave at once.  (1531
+    // rows with five adapters 15.3 us with two workgroups that share a tile's adapters, 18.8 with five: each asks for its tile's ids before it can leave.)
     // k in parts until there are two workgroups a CU.  Where a workgroup of the second product adds them up for 64 rows itself, with hundreds of such workgroups, parts have
     // eight steps at least (256 rows to 11008 with four adapters, k of 4096: four parts 26.6 us, sixteen 28.7; k of 11008 to 4096: four 26.7, ten 19.4).
     const uint32_t rows = static_cast<uint32_t>(a.rows < 64u ? a.rows : 64u), likely = a.rows < 512u ? (rows < a.adapters ? rows : a.adapters) : 1u;
@@ -643,8 +643,9 @@ Plan plan_of(const anszp_adapt_args_t& a) {
     q.any_up = a.cols < 8u || bytes_of(a, a.b_stride, a.cols, a.b_row_stride, a.rank) < 16u;
     if (q.any_down) q.parts = 1u;
     const uint32_t blocks = (a.rank + 7u) / 8u;
-    // Few rows: adapters at the same time, in a kernel that reads all of h for 32 columns and has no terms' kernel before it.  (64 rows to 11008: one adapter 13.7 us, else 14.7; four, mixed, 14.1 to 21.5;
-    // 256 rows: 16, mixed, 34 to 46; two, 128 rows each, 26.7 to 18; four, 64 each, 26.6 to 18.  512: eight, 64 each, 43 to 16; 48, mixed, 88 to 100.)
+    // Few rows: adapters at the same time, in a kernel that reads all of h for 32 columns and has no terms' kernel before it.  (64 rows to 11008: one
+    // adapter 13.7 us, else 14.7; four, mixed, 14.1 to 21.5; 256 rows: 16, mixed, 34 to 46; two, 128 rows each, 26.7 to 18; four, 64 each, 26.6 to 18.  512:
+    // eight, 64 each, 43 to 16; 48, mixed, 88 to 100.)
     q.few = q.any_up || a.rows <= 64u || (a.rows <= 256u && a.adapters >= 4u);
     q.terms = a.out_dtype == ANSZP_OUT_BF16 ? 2u : 3u;
     q.blocks = blocks <= 2u ? blocks : (blocks + 3u) / 4u * 4u;     // (a step of the second product has four blocks: of one term, or of several short ones)
@@ -695,7 +696,8 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
     const bool bytes = a->x_dtype == ANSZP_I8;
     const uint64_t size = a->out_dtype == ANSZP_OUT_BF16 ? 2u : 4u, base_size = a->base_dtype == ANSZP_OUT_BF16 ? 2u : 4u, x_size = bytes ? 1u : 2u, width = a->cols * size;
     const Rows out = {a->out, a->rows, a->out_stride * size, width}, base = {a->base, a->rows, a->base_stride * base_size, a->cols * base_size};
-    if (meet(out, {a->x_scales, 1, 0, a->rows * 4u}) || meet(out, {a->scales, 1, 0, a->adapters * 4u}) || meet(out, {a->x, a->rows, a->x_stride * x_size, a->k * x_size}) || meet(out, {a->ids, 1, 0, a->rows * 4u}) ||
+    if (meet(out, {a->x_scales, 1, 0, a->rows * 4u}) || meet(out, {a->scales, 1, 0, a->adapters * 4u}) || meet(out, {a->x, a->rows, a->x_stride * x_size, a->k * x_size}) ||
+        meet(out, {a->ids, 1, 0, a->rows * 4u}) ||
         (base_size == size ? meet_elsewhere(out, base) : meet(out, base)) || meet_elsewhere(out, {a->mul, a->rows, a->mul_stride * size, width}) ||
         meet_elsewhere(out, {a->residual, a->rows, a->residual_stride * size, width}) ||
         meet(out, {a->a, 1, 0, ((a->adapters - 1ull) * a->a_stride + (a->rank - 1ull) * a->a_row_stride + a->k) * (a->adapters ? 2u : 0u)}) ||

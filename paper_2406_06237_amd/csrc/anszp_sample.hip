@@ -12,9 +12,9 @@
 // listed, a few hundred, and each is compared with all others.  Where they are more than the list holds, each bin is cut by its tokens' own logits, as often
 // as that takes.  A small top_k needs no bins: a list of all tokens that may be kept is found by the threads' own largest.
 //
-// Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with the unit busy 70 % of the
-// time and LDS 27 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000 takes 16 us: each of three
-// passes waits for its first loads, and the sums between them for each other.
+// Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with
+// the unit busy 70 % of the time and LDS 27 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000
+// takes 16 us: each of three passes waits for its first loads, and the sums between them for each other.
 #include <hip/hip_runtime.h>
 
 #include "anszp_cus.h"
@@ -87,8 +87,8 @@ __device__ __forceinline__ uint32_t most_of_wave(uint32_t v) {
     return v;
 }
 
-// A row and the workgroup of THREADS threads that has it, which reads it for each pass.  (Rows up to 32768 held in registers, 64 of them a thread, took as long where rows are few and half as long again
-// where they are many, 512 of 20000 30 us instead of 20: one workgroup a CU has the registers.)
+// A row and the workgroup of THREADS threads that has it, which reads it for each pass.  (Rows up to 32768 held in registers, 64 of them a thread, took as
+// long where rows are few and half as long again where they are many, 512 of 20000 30 us instead of 20: one workgroup a CU has the registers.)
 template <uint32_t DTYPE, uint32_t THREADS>
 struct Row {
     static constexpr uint32_t kWaves = THREADS / 64u;
@@ -115,7 +115,8 @@ struct Row {
         }
         return l;
     }
-    // work(eight logits, the first one's token) for all tokens; a thread's come in rising order.  Several loads are under way together, and none of these looks for the row's end.
+    // work(eight logits, the first one's token) for all tokens; a thread's come in rising order.  Several loads are under way together, and none of these
+    // looks for the row's end.
     template <class Work>
     __device__ __forceinline__ void each(Work work) const {
         constexpr uint32_t kAtOnce = DTYPE == ANSZP_OUT_BF16 ? 4u : 2u;
@@ -132,9 +133,9 @@ struct Row {
     __device__ __forceinline__ float logit(uint32_t id) const {
         return DTYPE == ANSZP_OUT_BF16 ? bf16_low(static_cast<const uint16_t*>(logits)[from + id]) : static_cast<const float*>(logits)[from + id];
     }
-    // Tokens with logits near `mid` or `mid_b`, by less than `half` and `half_b`, into the list, as many as it holds, by their numbers; sh.listed counts them all.  (What they weigh is
-    // worked out behind the pass, by a thread each: here the registers of eight logits would be looked up by number, which is done in memory.  Which lanes have
-    // one is known to the whole wavefront: groups that have none, most, are through behind four instructions a logit.)
+    // Tokens with logits near `mid` or `mid_b`, by less than `half` and `half_b`, into the list, as many as it holds, by their numbers; sh.listed counts
+    // them all.  (What they weigh is worked out behind the pass, by a thread each: here the registers of eight logits would be looked up by number, which is
+    // done in memory.  Which lanes have one is known to the whole wavefront: groups that have none, most, are through behind four instructions a logit.)
     __device__ __forceinline__ void list_those(float mid, float half, float mid_b, float half_b) const {
         each([&](const Eight<DTYPE>& l, uint32_t at) __attribute__((always_inline)) {
             uint64_t those[8], any = 0u;
@@ -737,8 +738,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
 template <uint32_t DTYPE>
 void launch(const SampleParams& p, hipStream_t s) {
     const dim3 grid(groups_across(p.rows), groups_down(p.rows));
-    // More rows than compute units: half the threads, so that a CU has two rows at a time and goes on with one where the other waits.  (512 rows of 131072 in bf16 88 us, with 1024
-    // threads 103; 32 rows of 131072 52 us with 1024 threads, 68 with 512; short rows take the same.)
+    // More rows than compute units: half the threads, so that a CU has two rows at a time and goes on with one where the other waits.  (512 rows of 131072
+    // in bf16 88 us, with 1024 threads 103; 32 rows of 131072 52 us with 1024 threads, 68 with 512; short rows take the same.)
     if (p.rows > device_cus()) hipLaunchKernelGGL((sample_kernel<DTYPE, 512u>), grid, dim3(512), 0, s, p);
     else hipLaunchKernelGGL((sample_kernel<DTYPE, 1024u>), grid, dim3(1024), 0, s, p);
 }
