@@ -8,8 +8,9 @@
 // all of it, for fp32 ones: a number rounded to bf16 leaves a rest that is exact.
 //
 // Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h
-// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 140 (3.9 TB/s; what streams three such matrices and does nothing else reaches 5.9).  1531 rows from 11008 bf16
-// to 4096 fp32 with a residual, rank 24: 15, 5 and 21 (3.7 TB/s).  64 requests with 48 adapters of rank 16: 8 and 12.5 us, most of them waiting for loads.
+// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 134 (4.1 TB/s, the vector unit busy 54 % of the time; torch's product of two such matrices,
+// which streams as many bytes, 92).  1531 rows from 11008 bf16 to 4096 fp32 with a residual, rank 24: 15, 5 and 19 (4 TB/s).  64 requests with 48 adapters
+// of rank 16: 6.4 and 13 us, most of them waiting for loads.
 #include <hip/hip_runtime.h>
 
 #include "anszp_cus.h"
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(256) void adapt_terms_kernel(AdaptParams p) {
 // every eighth of b's a column, so that a lane ends up with 8 consecutive columns of four rows and 16 lanes with a row's 128: operands and results move 256
 // bytes of a row (of bf16) at a time.
 template <uint32_t BASE, uint32_t OUT, bool WHOLE>
-__global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 || OUT == ANSZP_OUT_BF16 ? 3 : 2) void adapt_up_kernel(AdaptParams p) {
+__global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 && OUT == ANSZP_OUT_BF16 ? 4 : 3) void adapt_up_kernel(AdaptParams p) {
     constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u;
     extern __shared__ __attribute__((aligned(16))) uint16_t b_rows[];                              // [column / 8 in steps of 8][block][8], 8 more behind a row
     const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4, wave = threadIdx.x >> 6;
@@ -378,6 +379,7 @@ __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 || OUT == ANSZP_OUT_BF1
     const Eighth cols(uint64_t(piece) * 128u + c * 8u, p.cols);
     const uint32_t rows = uint32_t(least(p.rows - top, 64u)), steps = steps_of<OUT>(p), width = p.blocks * 8u + 8u;
     const uint16_t* const h_at = p.terms_of_h + least(first + c, p.rows - 1u) * p.width + g * 8u;
+    const uint32_t terms = p.blocks < 4u ? 1u : kTerms, pieces = steps * terms;                     // of h: a step's terms are one each, short ones share one
     uint64_t left = ~0ull >> (64u - rows);
     bool staged = false;
     while (left) {
@@ -420,18 +422,15 @@ __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 || OUT == ANSZP_OUT_BF1
             }
             __syncthreads();
             if (mine) {
-                for (uint32_t s = 0; s < steps; ++s) {
+                // (not unrolled: 135 registers instead of 119, and three wavefronts a SIMD instead of four, 140 us instead of 134)
+#pragma unroll 1
+                for (uint32_t n = 0; n < pieces; ++n) {
+                    const uint32_t s = n / terms, term = n - s * terms;
+                    const bf16x8 h = as_bf16(*reinterpret_cast<const words4*>(h_at + s * 32u + term * p.blocks * 8u));
                     const uint16_t* const b_at = b_rows + c * width + block_of(p, s, g) * 8u;
-                    const auto multiply = [&](uint32_t behind) __attribute__((always_inline)) {
-                        const bf16x8 h = as_bf16(*reinterpret_cast<const words4*>(h_at + s * 32u + behind));
 #pragma unroll
-                        for (uint32_t t = 0; t < 8u; ++t)
-                            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, *reinterpret_cast<const bf16x8*>(b_at + t * 16u * width), sum[t], 0, 0, 0);
-                    };
-                    multiply(0u);
-                    if (p.blocks < 4u) continue;
-#pragma unroll
-                    for (uint32_t u = 1; u < kTerms; ++u) multiply(u * p.blocks * 8u);
+                    for (uint32_t t = 0; t < 8u; ++t)
+                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, *reinterpret_cast<const bf16x8*>(b_at + t * 16u * width), sum[t], 0, 0, 0);
                 }
             }
         }
