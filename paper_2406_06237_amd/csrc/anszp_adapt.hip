@@ -8,7 +8,7 @@
 // all of it, for fp32 ones: a number rounded to bf16 leaves a rest that is exact.
 //
 // Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h
-// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 134 (4.1 TB/s, the vector unit busy 54 % of the time; torch's product of two such matrices,
+// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 134 (4.1 TB/s, the vector unit busy 56 % of the time; torch's product of two such matrices,
 // which streams as many bytes, 92).  1531 rows from 11008 bf16 to 4096 fp32 with a residual, rank 24: 15, 5 and 19 (4 TB/s).  64 requests with 48 adapters
 // of rank 16: 6.4 and 13 us, most of them waiting for loads.
 #include <hip/hip_runtime.h>

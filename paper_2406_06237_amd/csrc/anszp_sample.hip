@@ -13,7 +13,7 @@
 // as that takes.  A small top_k needs no bins: a list of all tokens that may be kept is found by the threads' own largest.
 //
 // Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with
-// the unit busy 70 % of the time and LDS 27 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000
+// the unit busy 58 % of the time and LDS 28 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000
 // takes 16 us: each of three passes waits for its first loads, and the sums between them for each other.
 #include <hip/hip_runtime.h>
 
