@@ -14,7 +14,7 @@
 //
 // Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with
 // the unit busy 58 % of the time and LDS 28 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000
-// takes 16 us: each of three passes waits for its first loads, and the sums between them for each other.
+// takes 15 us: each of three passes waits for its first loads, and the sums between them for each other.
 #include <hip/hip_runtime.h>
 
 #include "anszp_cus.h"
@@ -100,35 +100,47 @@ struct Row {
     double c0, c1, c2, c3, one;         // of q
     bool far;
 
-    // Eight logits; behind the row's end there is nothing that weighs.
+    // Eight logits, in pieces of 16 bytes so that the lanes of a load lie next to each other: of fp32 four, and four a workgroup's load further.
+    // Behind the row's end there is nothing that weighs.
+    static constexpr uint32_t kPiece = DTYPE == ANSZP_OUT_BF16 ? 8u : 4u, kApart = THREADS * kPiece;
+    static __device__ __forceinline__ uint32_t token_of(uint32_t at, uint32_t i) { return at + i / kPiece * kApart + i % kPiece; }
     __device__ __forceinline__ Eight<DTYPE> eight(uint32_t at) const {
         Eight<DTYPE> l;
-        const uint32_t there = at < n ? n - at : 0u;
-        l.load(logits, from + at, there);
-        if (there < 8u) {
+        if constexpr (DTYPE == ANSZP_OUT_BF16) {
+            l.w = *reinterpret_cast<const words4_any*>(static_cast<const uint16_t*>(logits) + from + at);
+        } else {
 #pragma unroll
-            for (uint32_t i = 0; i < 8u; ++i) {
-                if (i < there) continue;
-                if constexpr (DTYPE == ANSZP_OUT_BF16) l.w[i >> 1] = i & 1u ? (l.w[i >> 1] & 0xFFFFu) | 0xFF800000u : (l.w[i >> 1] & 0xFFFF0000u) | 0xFF80u;
-                else l.w[i >> 2][i & 3u] = 0xFF800000u;
+            for (uint32_t j = 0; j < 2u; ++j) l.w[j] = *reinterpret_cast<const words4_any*>(static_cast<const float*>(logits) + from + at + j * kApart);
+        }
+        return l;
+    }
+    __device__ __forceinline__ Eight<DTYPE> last_eight(uint32_t at) const {
+        Eight<DTYPE> l;
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            const uint32_t id = token_of(at, i);
+            if constexpr (DTYPE == ANSZP_OUT_BF16) {
+                const uint32_t w = id < n ? static_cast<const uint16_t*>(logits)[from + id] : 0xFF80u;
+                l.w[i >> 1] = i & 1u ? l.w[i >> 1] | w << 16 : w;
+            } else {
+                l.w[i >> 2][i & 3u] = id < n ? static_cast<const uint32_t*>(logits)[from + id] : 0xFF800000u;
             }
         }
         return l;
     }
-    // work(eight logits, the first one's token) for all tokens; a thread's come in rising order.  Several loads are under way together, and none of these
-    // looks for the row's end.
+    // work(eight logits, the first one's token) for all tokens.  Several loads are under way together, and none of these looks for the row's end.
     template <class Work>
     __device__ __forceinline__ void each(Work work) const {
-        constexpr uint32_t kAtOnce = DTYPE == ANSZP_OUT_BF16 ? 4u : 2u;
-        uint32_t at = threadIdx.x * 8u;
-        for (; at + (kAtOnce - 1u) * THREADS * 8u + 8u <= n; at += kAtOnce * THREADS * 8u) {
+        constexpr uint32_t kAtOnce = DTYPE == ANSZP_OUT_BF16 ? 4u : 2u, kLast = 8u / kPiece * kApart - kApart + kPiece;
+        uint32_t at = threadIdx.x * kPiece;
+        for (; at + (kAtOnce - 1u) * THREADS * 8u + kLast <= n; at += kAtOnce * THREADS * 8u) {
             Eight<DTYPE> l[kAtOnce];
 #pragma unroll
-            for (uint32_t j = 0; j < kAtOnce; ++j) l[j].load(logits, from + at + j * THREADS * 8u, 8u);
+            for (uint32_t j = 0; j < kAtOnce; ++j) l[j] = eight(at + j * THREADS * 8u);
 #pragma unroll
             for (uint32_t j = 0; j < kAtOnce; ++j) work(l[j], at + j * THREADS * 8u);
         }
-        for (; at < n; at += THREADS * 8u) work(eight(at), at);
+        for (; at < n; at += THREADS * 8u) work(at + kLast <= n ? eight(at) : last_eight(at), at);
     }
     __device__ __forceinline__ float logit(uint32_t id) const {
         return DTYPE == ANSZP_OUT_BF16 ? bf16_low(static_cast<const uint16_t*>(logits)[from + id]) : static_cast<const float*>(logits)[from + id];
@@ -155,7 +167,7 @@ struct Row {
             for (uint32_t i = 0; i < 8u; ++i) {
                 if (!those[i]) continue;
                 const uint32_t own = place + __builtin_amdgcn_mbcnt_hi(uint32_t(those[i] >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(those[i]), 0u));
-                if (those[i] >> (threadIdx.x & 63u) & 1u && own < kList) sh.list[own].order = at + i;
+                if (those[i] >> (threadIdx.x & 63u) & 1u && own < kList) sh.list[own].order = token_of(at, i);
                 place += uint32_t(__builtin_popcountll(those[i]));
             }
         });
