@@ -269,6 +269,18 @@ struct Row {
         return v;
     }
 
+    // The first token with this logit.
+    __device__ __forceinline__ uint32_t first_equal(float logit) const {
+        uint32_t first = ~0u;
+        each([&](const Eight<DTYPE>& l, uint32_t at) __attribute__((always_inline)) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8u; ++i) {
+                const uint32_t id = l[i] == logit ? token_of(at, i) : ~0u;
+                first = id < first ? id : first;
+            }
+        });
+        return ~uint32_t(most_of_all(~first));
+    }
     // The token that is the `nth` (from 1 on) of those with this logit.
     __device__ __forceinline__ void find_equal(uint32_t key, uint64_t nth) const {
         uint64_t passed = 0u;
@@ -523,8 +535,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
         return;
     }
     if (temperature == 0.0f || set.top_k == 1u) {
-        row.find_equal(best, 1u);
-        answer(int64_t(sh.found_id), 1.0f);
+        answer(int64_t(row.first_equal(top)), 1.0f);
         return;
     }
     if (top == __builtin_inff()) {
