@@ -269,7 +269,7 @@ struct Row {
         return v;
     }
 
-    // The first token with this logit.
+    // The first token with this logit.  (A pass that counts as it goes, as the next one, takes a sum over the workgroup for every 8192 tokens: 32 us for 131072, this 11.)
     __device__ __forceinline__ uint32_t first_equal(float logit) const {
         uint32_t first = ~0u;
         each([&](const Eight<DTYPE>& l, uint32_t at) __attribute__((always_inline)) {
