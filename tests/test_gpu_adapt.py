@@ -122,3 +122,31 @@ def test_the_same_again(rows):
     want = B.adapt(**o)
     for _ in range(5):
         assert torch.equal(B.adapt(**o), want)
+
+
+@pytest.mark.parametrize("adapters", [1, 3, 4])
+@pytest.mark.parametrize("rows", [63, 64, 65, 256, 257, 511, 512, 4097])
+def test_where_another_kernel_begins(rows, adapters):
+    for k in (100, 4200) if rows < 4000 else (100,):
+        _check(_operands(rows, k, 136, 20, adapters, "i8"), "f32" if rows % 2 else "bf16")
+
+
+@pytest.mark.parametrize("rows", [60, 200, 700])
+def test_operands_of_one_row_for_all(rows):
+    """Rows that lie on each other are read, each row's own as any."""
+    o = _operands(rows, 256, 200, 16, 5, base=torch.float32)
+    one = lambda dt, n: torch.randn(1, n, device=DEV).to(dt).expand(rows, n)  # noqa: E731
+    o.update(base=one(torch.float32, 200), x=one(BF16, 256))
+    _check(o, "bf16", mul=one(BF16, 200), residual=one(BF16, 200), activation="silu")
+
+
+@pytest.mark.parametrize("rows", [60, 200, 700])
+@pytest.mark.parametrize("cols", [75, 4100])
+def test_into_each_operand_it_may(rows, cols):
+    o = _operands(rows, 128, cols, 40, 11, "i8")
+    mul, residual = (torch.randn(rows, cols, device=DEV).to(BF16) for _ in range(2))
+    want = B.adapt(**o, mul=mul, residual=residual, activation="gelu")
+    for which in ("base", "mul", "residual"):
+        into = dict(o, mul=mul, residual=residual)
+        into[which] = into[which].clone()
+        assert torch.equal(B.adapt(**into, activation="gelu", out=into[which]), want)

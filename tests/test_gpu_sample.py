@@ -124,6 +124,22 @@ def test_borders():
     assert got.tolist()[:3] == [-1, -1, 1] and chances.tolist()[:3] == [0, 0, 1] and got[3] == got[5] == got[6] == got[7] and int(got[4]) == 1
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocabulary", [1, 9, 4099, 8205, 33001])
+def test_first_of_the_largest(vocabulary, dtype):
+    """Without a temperature and with a top_k of 1, wherever the largest are: in the row's last elements, in two threads' or in two of a thread's."""
+    g = torch.Generator(device=DEV).manual_seed(vocabulary)
+    places = sorted({min(p, vocabulary - 1) for p in (0, 3, 4, 7, 8, 4095, 4096, 4100, 8191, 8192, vocabulary - 6, vocabulary - 2, vocabulary - 1) if p >= 0})
+    logits = torch.randn(len(places), vocabulary, device=DEV, generator=g).to(dtype)
+    for r, p in enumerate(places):
+        logits[r, p:] = torch.where(torch.rand(vocabulary - p, device=DEV, generator=g) < 0.3, 9.0, logits[r, p:].float()).to(dtype)
+        logits[r, p] = 9.0
+    u = torch.rand(len(places), device=DEV, generator=g)
+    for more in (dict(temperature=0.0), dict(top_k=1), dict(temperature=0.0, top_k=5, top_p=0.1, min_p=0.5)):
+        tokens, chances = B.sample(logits, u, **more)
+        assert tokens.tolist() == places and chances.tolist() == [1.0] * len(places)
+
+
 def test_frequencies():
     """Uniforms that are spread evenly draw each token as often as its chance says, to one draw."""
     n = 4096
