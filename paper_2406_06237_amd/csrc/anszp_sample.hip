@@ -65,6 +65,7 @@ struct Shared {
     uint32_t list_bin[kList];
     uint32_t listed, least, most;
     uint32_t found, found_too, found_id;
+    uint32_t found_top_p;               // (a word of its own: what marks the next bin waits for no one who still reads this one)
     uint64_t found_sum, found_q, found_count;
 };
 
@@ -664,9 +665,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
     uint64_t wanted = 0u, fewest = kept, most = kept;
     if (set.top_p < 1.0f) {
         wanted = wanted_of(set.top_p, kept);
-        row.mark_bin(mass_before, wanted, sh.found);
+        row.mark_bin(mass_before, wanted, sh.found_top_p);
         __syncthreads();
-        bin_p = sh.found;
+        bin_p = sh.found_top_p;
     }
     if (set.min_p > 0.0f) {
         const double t = -double(kSteps) * log2(least);

@@ -169,3 +169,18 @@ def test_into_an_output_on_another_stream():
     side.synchronize()
     assert got is into and torch.equal(into, want) and torch.equal(again, chances)
     assert B.sample(logits[:0], u[:0])[0].shape == (0,)
+
+
+@pytest.mark.parametrize("rows,dtype", [(40, torch.float32), (700, torch.bfloat16)])
+def test_top_p_by_the_bins_again_and_again(rows, dtype):
+    """Rows whose top_p border and drawn token are found in the bins, by workgroups of each size: the same ones each time, and the formula's."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    logits = (torch.randn(rows, 6001, device=DEV, generator=g) * 2.5).to(dtype)
+    u = torch.rand(rows, device=DEV, generator=g)
+    for more in (dict(top_p=0.9), dict(top_p=0.6, min_p=0.001), dict(top_p=0.97, top_k=900)):
+        want = _check(logits[:40], u[:40].tolist(), **more)
+        first = B.sample(logits, u, **more)
+        assert torch.equal(first[0][:40], want)
+        for _ in range(20):
+            again = B.sample(logits, u, **more)
+            assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
