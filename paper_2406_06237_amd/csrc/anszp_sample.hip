@@ -677,7 +677,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
     if (bin_m > bin_p) bin_m = kBins;
     const uint32_t bin_b = bin_p < bin_m ? bin_p : bin_m;
     if (bin_b < kBins) {
-        fewest = sh.mass[bin_b] < kept ? sh.mass[bin_b] + 1u : kept;
+        // (top_p's border leaves at least a token of its bin, the weight's perhaps none: then what lies before the bin is all that is kept)
+        const uint64_t before = sh.mass[bin_b], some = bin_m == kBins || before == 0u ? before + 1u : before;
+        fewest = some < kept ? some : kept;
         most = sh.mass[bin_b + 1u] < kept ? sh.mass[bin_b + 1u] : kept;
     }
     // What is drawn lies in bins first .. last.  Their tokens and those of the border's bin are listed in one go, if they are few.

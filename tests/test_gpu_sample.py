@@ -184,3 +184,19 @@ def test_top_p_by_the_bins_again_and_again(rows, dtype):
         for _ in range(20):
             again = B.sample(logits, u, **more)
             assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocabulary", [3, 6, 60, 3000])
+def test_uniforms_of_one_and_beyond_beside_both_borders(vocabulary, dtype):
+    """The last token that is kept, where the weight's border lies in a bin that has no token, in one whose tokens weigh too little, and in one of which some are kept."""
+    g = torch.Generator(device=DEV).manual_seed(vocabulary)
+    uniforms = [1.0, 2.0, float("inf"), 1 - 2.0 ** -24, 0.0, 0.5]
+    steps = torch.arange(vocabulary, device=DEV, dtype=torch.float32)
+    logits = torch.stack([-steps, -6.0 * steps, -steps / 512, *(torch.randn(5, vocabulary, device=DEV, generator=g) * 2.5)]).to(dtype)
+    logits = logits.repeat_interleave(len(uniforms), 0)
+    # (no min_p is within the weights' error of a token's weight: logits of the first rows are whole numbers or 512ths)
+    for top_p in (0.5, 0.99, 0.999):
+        for min_p in (0.9995, 0.9, 0.3, 0.2, 0.05, 0.001):
+            for more in (dict(), dict(top_k=vocabulary), dict(top_k=700)):
+                _check(logits, uniforms * 8, top_p=top_p, min_p=min_p, **more)
