@@ -595,7 +595,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
             Entry e = {0u, 0u};
             uint32_t bin = 0u;
             const bool there = row.listed_one(n, e, bin);
-            e.q = there ? mass_of(height(sh, bin), e.q) : 0u;
+            // (its weight as the way over the bins has it: of a light token the mass, a whole number, has few digits)
+            const double weight = there ? height(sh, bin) * double(e.q) : 0.0;
+            e.q = uint64_t(weight);
             __syncthreads();
             if (threadIdx.x < n) sh.list[threadIdx.x] = e;
             const uint32_t those = uint32_t(__syncthreads_count(there));
@@ -612,13 +614,13 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p) {
             }
             if (set.min_p > 0.0f) {
                 // (those that weigh enough are the first of the order: the last one's sum is theirs)
-                const uint64_t upto = row.most_of_all(there && double(e.q) >= border ? before + e.q : 0u);
+                const uint64_t upto = row.most_of_all(there && weight >= border ? before + e.q : 0u);
                 kept = upto < kept ? upto : kept;
             }
             const uint64_t at = drawn_at(set.u, kept);
             if (there && before <= at && at < before + e.q) {
                 p.tokens[r] = int64_t(id_of(e));
-                if (p.chances) p.chances[r] = float(double(e.q) / double(kept));
+                if (p.chances) p.chances[r] = float(weight / double(kept));
             }
             return;
         }

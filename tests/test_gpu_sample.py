@@ -200,3 +200,11 @@ def test_uniforms_of_one_and_beyond_beside_both_borders(vocabulary, dtype):
         for min_p in (0.9995, 0.9, 0.3, 0.2, 0.05, 0.001):
             for more in (dict(), dict(top_k=vocabulary), dict(top_k=700)):
                 _check(logits, uniforms * 8, top_p=top_p, min_p=min_p, **more)
+
+
+def test_the_chance_of_a_light_token_is_the_same_by_the_list_and_by_the_bins():
+    """The last of two tokens, down to 2^-40 of the first: its chance to one rounding, whether top_k lists them or not."""
+    far = [1.0, 5.0, 10.0, 15.0, 19.4, 23.1, 27.7]
+    logits = torch.tensor([[0.0, -f] for f in far], device=DEV)
+    for more in (dict(), dict(top_k=2), dict(min_p=1e-13), dict(top_k=2, min_p=1e-13)):
+        assert _check(logits, [1.0] * len(far), **more).tolist() == [1] * len(far)
