@@ -541,8 +541,9 @@ int anszp_attend(const anszp_attend_args_t* args, void* hip_stream);
  *   need = ceil((old + new) / P) - ceil(old / P) pages are taken from the stack's end, in the sequences' order, and written to the table.
  * A sequence gets nothing (its length stays, its slots are -1) where the stack has not as many pages as it and those before it need, or
  * new_tokens[s] is negative or more than its row of the table or n_tokens has room for; lengths out of range are treated alike (those of a
- * sequence that ends are clamped).  Apart from lengths_out, n_free_out, the table's entries behind the pages that a sequence holds and the
- * stack's behind n_free nothing is changed, so a call may be made again. */
+ * sequence that ends are clamped).  Apart from lengths_out, n_free_out, the table's entries behind the pages that a sequence goes on with (of one
+ * that ends: from its first on) and the stack's behind n_free nothing is changed.  So a call with outputs of their own may be made again, and gives the same, unless
+ * a sequence both ends and gets tokens: its row then begins with other pages than those that it has to give back. */
 typedef struct {
     int32_t*       pages;         /* [device] n_seqs x table_width                                   */
     const int32_t* lengths;       /* [device] n_seqs, 0 .. table_width * page_size                   */

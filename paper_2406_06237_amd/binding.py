@@ -1142,9 +1142,10 @@ class Placed(NamedTuple):
 def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: int, ends=None, lengths_out=None, n_free_out=None, status=None) -> Placed:
     """anszp_place on torch's current stream: sequences that hold lengths[s] tokens get new[s] more, in pages from the end of the stack free[:n_free].  pages int32
     [sequences, width] (contiguous), lengths, new and ends int32 [sequences], free int32 [room for all pages], n_free int32 [1]; n_tokens: as many slots are made, at least
-    the sum of new.  A sequence with a number other than 0 in ends gives its pages back first and begins anew.  pages and free are written in place where
-    nothing was held; lengths_out and n_free_out may be lengths and n_free themselves.  A sequence for which there is no room gets nothing: its slots are -1, its
-    length stays, and the status (two int32 words) says so."""
+    the sum of new.  A sequence with a number other than 0 in ends gives its pages back first and begins anew.  pages and free are written in place, behind what goes on
+    being held; lengths_out and n_free_out may be lengths and n_free themselves, and where they are not, the same call gives the same again, unless a sequence both
+    ends and gets tokens, whose row is written from its first page on.  A sequence for which there is no room gets nothing: its slots are -1, its length (0, if it
+    ends) stays, and the status (two int32 words) says so."""
     torch = _torch()
     dev = pages.device
     result = _call("anszp_place", "place_tokens", dev, pages, page_size, lengths, new, free, n_free, n_tokens, ends, lengths_out, n_free_out, status, calls=_operator_calls)

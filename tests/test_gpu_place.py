@@ -99,3 +99,26 @@ def test_on_another_stream():
     with torch.cuda.stream(side):
         _check(pages, 16, lengths, [7] * 40, free, n_free, 280)
     side.synchronize()
+
+
+@pytest.mark.parametrize("n", [5, 60, 400])
+def test_a_call_made_again_gives_the_same(n):
+    """With outputs of their own, where no sequence that ends gets tokens (a refused one gets none); in one workgroup and in three launches."""
+    rng = random.Random(n)
+    pages, lengths, free, n_free = _state(rng, n, 16, 90, n)
+    ends = [int(s % 4 == 1) for s in range(n)]
+    new = [0 if e else rng.randint(0, 30) for e in ends]
+    ends[-1], new[-1] = 1, 10 ** 6
+    table, held, stack, count, status = torch.tensor(pages, dtype=torch.int32, device=DEV), ints(lengths), ints(free), ints([n_free]), ints([0, 0])
+    call = lambda: [t.clone() for t in (*B.place_tokens(table, 16, held, ints(new), stack, count, 40 * n, ends=ints(ends), status=status), table, stack)]  # noqa: E731
+    first = call()
+    assert first[2].tolist()[-1] == 0 and int(status[1]) >= 1 and (first[0] >= 0).any()
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(call(), first))
+
+
+def test_a_sequence_that_ends_and_gets_tokens_has_its_new_pages_at_once():
+    """Its row begins with what it was dealt, so what it gave back is in the stack alone, and the same call on this table would be another one."""
+    table, stack = ints([[3, 5, 1]]), ints([-1, -1, -1])
+    got = B.place_tokens(table, 16, ints([40]), ints([20]), stack, ints([0]), 20, ends=ints([1]))
+    assert table.tolist() == [[1, 5, 1]] and stack.tolist() == [3, 5, 1] and got.n_free.tolist() == [1] and got.slots.tolist() == [*range(16, 32), *range(80, 84)]
