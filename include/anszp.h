@@ -608,7 +608,7 @@ typedef struct {
     void*          workspace;     /* [device] anszp_adapt_workspace_bytes, 16-byte aligned, in use until the call is done */
     uint64_t       workspace_bytes;
     uint64_t       rows, cols;    /* < 2^28, < 2^31, may be 0; fewer than 2^24 tiles of 64 x 32 together, rows * (rank up to a multiple of 32) < 2^33; with x or a
-                                   * of fewer than 16 bytes rows * rank < 2^32, with such a b rows * cols */
+                                   * of fewer than 16 bytes rows * rank <= 2^32 - 256, with such a b rows * cols */
     uint64_t       x_stride, a_stride, a_row_stride, b_stride, b_row_stride, base_stride, mul_stride, residual_stride, out_stride;
     uint32_t       adapters;      /* < 2^24, may be 0                                                */
     uint32_t       k;             /* 1 .. 2^30                                                       */

@@ -704,7 +704,9 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
         return ANSZP_E_RANGE;
     if ((a->rows + 63u) / 64u * ((a->cols + 31u) / 32u) >= 1ull << 24) return ANSZP_E_RANGE;          // (threads that one launch has not)
     const Plan q = plan_of(*a);
-    if (a->rows * (q.width / 8u) >= 1ull << 32 || (q.any_down && a->rows * a->rank >= 1ull << 32) || (q.any_up && a->rows * a->cols >= 1ull << 32)) return ANSZP_E_RANGE;
+    constexpr uint64_t kMost = (1ull << 32) - 256u;                 // threads that launches an element a thread have, in workgroups of 256
+    const bool any = q.any_up || a->cols < 8u;                      // (also where there are no adapters)
+    if (a->rows * (q.width / 8u) > kMost || (q.any_down && a->rows * a->rank > kMost) || (any && a->rows * a->cols > kMost)) return ANSZP_E_RANGE;
     if (q.workspace && !a->workspace) return ANSZP_E_NULL;
     if (q.workspace && (a->workspace_bytes < q.workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u))) return ANSZP_E_RANGE;
     AdaptParams p = {};
@@ -727,7 +729,6 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
         else launch_down<false>(p, q, s);
         if (!q.few) hipLaunchKernelGGL(adapt_terms_kernel, dim3(static_cast<uint32_t>((a->rows * (q.width / 8u) + 255u) / 256u)), dim3(256), 0, s, p);
     }
-    const bool any = q.any_up || a->cols < 8u;                      // (also where there are no adapters)
     const bool base_short = a->base_dtype == ANSZP_OUT_BF16, out_short = a->out_dtype == ANSZP_OUT_BF16;
     if (base_short && out_short) launch_up<ANSZP_OUT_BF16, ANSZP_OUT_BF16>(p, any, q.few, s);
     else if (base_short) launch_up<ANSZP_OUT_BF16, ANSZP_OUT_F32>(p, any, q.few, s);

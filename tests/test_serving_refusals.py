@@ -126,6 +126,13 @@ def test_adapt_of_operands_of_a_few_bytes_by_more_threads_than_one_launch_has(ch
     assert _adapt(**{**apart, **change}) == E_RANGE
 
 
+@pytest.mark.parametrize("change", [dict(rows=65537, cols=65535, rank=4, b_row_stride=0, base_stride=65535, out_stride=65535), dict(rows=33818640, rank=127, k=4, a_row_stride=0)])
+def test_adapt_where_whole_workgroups_are_the_thread_too_many(change):
+    """2^32 - 1 elements of the output and 2^32 - 16 of h, a thread each, are 2^32 threads in workgroups of 256, which one launch has not."""
+    apart = dict(adapters=1, workspace_bytes=1 << 50, x=1 << 60, base=1 << 59, ids=1 << 58, out=1 << 57, mul=None, residual=None, x_scales=None, scales=None)
+    assert _adapt(**{**apart, **change}) == E_RANGE
+
+
 def test_adapt_over_a_base_of_another_type_or_stride():
     for change in (dict(base_dtype=B.OUT_F32), dict(base_stride=80)):
         a = _args(B.AdaptArgs, ADAPT, change)
