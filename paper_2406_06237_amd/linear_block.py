@@ -67,10 +67,11 @@ class Matrix:
     scales: object           # fp32 [out]
 
     def __call__(self, x, x_scales, adapters=None, ids=None, **epilogue):
-        """The product with its epilogue; with adapters, and ids of each row's, what they add to it comes before the epilogue."""
+        """The product with its epilogue; with adapters, and ids of each row's, what they add to it comes before the epilogue.  The product is in fp32 between the
+        two calls, so that a row is rounded once, and one without an adapter has what it has where there are none."""
         if adapters is None:
             return B.linear(x, self.symbols, x_scales=x_scales, zero_point=self.zero_point, channel_scales=self.scales, **epilogue)
-        base = B.linear(x, self.symbols, x_scales=x_scales, zero_point=self.zero_point, channel_scales=self.scales)
+        base = B.linear(x, self.symbols, x_scales=x_scales, zero_point=self.zero_point, channel_scales=self.scales, out_dtype="f32")
         return B.adapt(base, x, adapters.a, adapters.b, ids, x_scales=x_scales, scales=adapters.scales, status=adapters.status, **epilogue)
 
 

@@ -179,3 +179,33 @@ def test_both_of_the_bindings_paths_give_the_same(monkeypatch):
     monkeypatch.setattr(B, "_host", False)
     for a, b in zip(native, everything()):
         assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows", [5, 90, 600])
+def test_a_row_without_an_adapter_is_the_same_beside_adapters(rows):
+    """To the bit, with each epilogue that the block has."""
+    workload = L.block_workload(D_MODEL, D_FF, KV_HEADS)
+    block = L.Block(workload, 1)
+    block.decode()
+    adapters = L.new_adapters(workload, 3, RANK)
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    rnd = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    ids = torch.arange(rows, dtype=torch.int32, device=DEV) % 4 - 1
+    without = ids < 0
+    for name in ("wq", "wg", "wu", "wd"):
+        matrix = getattr(block, name)
+        out, k = matrix.symbols.shape
+        n, s = B.quantise_rows(rnd(rows, k))
+        beside = rnd(rows, out).to(torch.bfloat16)
+        epilogue = {"wq": {}, "wg": dict(activation="silu"), "wu": dict(mul=beside), "wd": dict(residual=beside)}[name]
+        want, got = matrix(n, s, **epilogue), matrix(n, s, adapters=adapters[name], ids=ids, **epilogue)
+        assert torch.equal(got[without], want[without]) and not torch.equal(got, want)
+
+
+def test_a_sequence_without_an_adapter_has_the_logits_it_has_alone():
+    _, adapted = _serving(True)
+    _, plain = _serving(False)
+    g = torch.Generator().manual_seed(2)
+    tokens, u = torch.randint(0, VOCABULARY, (20 + 90 + 3,), generator=g).to(DEV), torch.rand(SEQUENCES, generator=g).to(DEV)
+    got, want = (serving.step(tokens, _ints([20, 90, 3]), u, **SETTINGS)[2] for serving in (adapted, plain))
+    assert torch.equal(got[1], want[1]) and not torch.equal(got[0], want[0]) and not torch.equal(got[2], want[2])
