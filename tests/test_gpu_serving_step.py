@@ -209,3 +209,28 @@ def test_a_sequence_without_an_adapter_has_the_logits_it_has_alone():
     tokens, u = torch.randint(0, VOCABULARY, (20 + 90 + 3,), generator=g).to(DEV), torch.rand(SEQUENCES, generator=g).to(DEV)
     got, want = (serving.step(tokens, _ints([20, 90, 3]), u, **SETTINGS)[2] for serving in (adapted, plain))
     assert torch.equal(got[1], want[1]) and not torch.equal(got[0], want[0]) and not torch.equal(got[2], want[2])
+
+
+def test_a_sequence_for_which_no_page_is_left():
+    """It has no token, the others have theirs, and it goes on once there are pages."""
+    _, serving = _serving(False, most=300)
+    _, other = _serving(False, most=300)
+    g = torch.Generator().manual_seed(12)
+    tokens = torch.randint(0, VOCABULARY, (100 + 64 + 30,), generator=g).to(DEV)
+    u = torch.rand(3, SEQUENCES, generator=g).to(DEV)
+    for s in (serving, other):
+        s.step(tokens, _ints([100, 64, 30]), u[0], **SETTINGS)
+    kept = int(serving.n_free)
+    serving.n_free.zero_()
+    one = torch.tensor([7, 8, 9], device=DEV)
+    got, chances, logits = serving.step(one, _ints([1, 1, 1]), u[1], **SETTINGS)
+    want = other.step(one, _ints([1, 1, 1]), u[1], **SETTINGS)
+    # (64 tokens fill a page, so the second sequence needs another one)
+    assert got.tolist() == [int(want[0][0]), -1, int(want[0][2])] and chances.tolist() == [float(want[1][0]), 0.0, float(want[1][2])]
+    assert serving.lengths.tolist() == [101, 64, 31] and serving.block.cache.status.tolist() == [1, 1] and torch.equal(logits[0], want[2][0]) and torch.equal(logits[2], want[2][2])
+    serving.n_free.fill_(kept)
+    got, chances, logits = serving.step(one[1:2], _ints([0, 1, 0]), u[1], **SETTINGS)
+    assert got.tolist() == [-1, int(want[0][1]), -1] and chances.tolist() == [0.0, float(want[1][1]), 0.0] and serving.lengths.tolist() == [101, 65, 31]
+    # more tokens than the row of the table has room for, and more than are given
+    got, chances, _ = serving.step(tokens[:30], _ints([1000, 3, 5]), u[2], **SETTINGS)
+    assert got.tolist() == [-1, -1, -1] and chances.tolist() == [0.0] * 3 and serving.lengths.tolist() == [101, 65, 31]
