@@ -192,19 +192,22 @@ class Serving:
         none = (placed.slots[last] < 0) | (placed.owners[last] != self.places)
         return drawn.masked_fill_(none, -1), chances.masked_fill_(none, 0.0), logits
 
-    def captured_step(self, tokens, new, uniforms, **settings):
-        """The step as a graph that reads `tokens`, `new` and `uniforms` each time it is replayed: (graph, its results).  The state is what it was before."""
+    def captured_step(self, tokens, new, uniforms, ends=None, **settings):
+        """The step as a graph that reads `tokens`, `new` and `uniforms`, and `ends` and settings that are tensors, each time it is replayed: (graph, its results).  The state is what it
+        was before."""
         torch = B._torch()
-        state = [t.clone() for t in (self.pages, self.lengths, self.free, self.n_free)]
+        held = [self.pages, self.lengths, self.free, self.n_free, self.block.cache.status, *({id(a.status): a.status for a in self.adapters.values()}.values() if self.adapters else ())]
+        state = [t.clone() for t in held]
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
-            self.step(tokens, new, uniforms, **settings)
+            # (no sequence ends here: its pages would be dealt, and what the cache holds in them written over)
+            self.step(tokens, new, uniforms, ends=None if ends is None else torch.zeros_like(ends), **settings)
         torch.cuda.current_stream().wait_stream(side)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            results = self.step(tokens, new, uniforms, **settings)
-        for t, was in zip((self.pages, self.lengths, self.free, self.n_free), state):
+            results = self.step(tokens, new, uniforms, ends=ends, **settings)
+        for t, was in zip(held, state):
             t.copy_(was)
         return graph, results
 

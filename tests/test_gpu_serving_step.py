@@ -234,3 +234,36 @@ def test_a_sequence_for_which_no_page_is_left():
     # more tokens than the row of the table has room for, and more than are given
     got, chances, _ = serving.step(tokens[:30], _ints([1000, 3, 5]), u[2], **SETTINGS)
     assert got.tolist() == [-1, -1, -1] and chances.tolist() == [0.0] * 3 and serving.lengths.tolist() == [101, 65, 31]
+
+
+def test_a_captured_step_in_which_sequences_end():
+    """`ends` is read at each replay, and what is captured leaves the sequences that it names as they were."""
+    results = []
+    for captured in (False, True):
+        _, serving = _serving(True)
+        g = torch.Generator().manual_seed(21)
+        first, after = (torch.randint(0, VOCABULARY, (n,), generator=g).to(DEV) for n in (60 + 70 + 5, SEQUENCES))
+        u = torch.rand(6, SEQUENCES, generator=g).to(DEV)
+        serving.step(first, _ints([60, 70, 5]), u[0], **SETTINGS)
+        tokens, new, own, ends, seen = after.clone(), _ints([1, 1, 1]), u[1].clone(), _ints([1, 1, 0]), []
+        if captured:
+            # (no page is left but those of the sequences that would end)
+            kept = serving.n_free.clone()
+            serving.n_free.zero_()
+            graph, out = serving.captured_step(tokens, new, own, ends=ends, **SETTINGS)
+            assert serving.block.cache.status.tolist() == [0, 0] and serving.n_free.tolist() == [0] and serving.lengths.tolist() == [60, 70, 5]
+            serving.n_free.copy_(kept)
+        for i, which in enumerate(([0, 0, 0], [0, 1, 0], [0, 0, 0], [1, 0, 1], [0, 0, 0])):
+            own.copy_(u[1 + i])
+            ends.copy_(_ints(which))
+            if captured:
+                graph.replay()
+            else:
+                out = serving.step(tokens, new, own, ends=ends, **SETTINGS)
+            seen += [t.clone() for t in out]
+            tokens.copy_(out[0])
+            torch.cuda.synchronize()
+        results.append([*seen, serving.lengths, serving.n_free, serving.pages, serving.free[:int(serving.n_free)], serving.block.cache.status])
+    for eager, replayed in zip(*results):
+        assert torch.equal(eager, replayed)
+    assert results[0][-1].tolist() == [0, 0]
