@@ -180,6 +180,8 @@ class Serving:
         anew.  settings: sample's.  Returns (the next token of each sequence int64, its chance, logits fp32 [sequences, vocabulary]).  A sequence without new tokens, and one that place_tokens
         refuses, as for lack of pages (its length stays, and the cache's status says so), has token -1 and a chance of 0; its logits mean nothing, and no
         token of it is to be given to a later step before those that it was refused."""
+        if tokens.shape[0] == 0:
+            raise ValueError("a step has one token at least")
         placed = B.place_tokens(self.pages, PAGE_SIZE, self.lengths, new, self.free, self.n_free, tokens.shape[0], ends=ends, lengths_out=self.lengths, n_free_out=self.n_free,
                                 status=self.block.cache.status)
         x = B.embed(tokens, self.words.symbols, self.words.zero_point, self.words.scales, scale=math.sqrt(self.words.symbols.shape[1]), status=self.block.cache.status)

@@ -267,3 +267,14 @@ def test_a_captured_step_in_which_sequences_end():
     for eager, replayed in zip(*results):
         assert torch.equal(eager, replayed)
     assert results[0][-1].tolist() == [0, 0]
+
+
+def test_a_step_of_no_tokens_is_refused_before_it_changes_anything():
+    _, serving = _serving(False)
+    g = torch.Generator().manual_seed(1)
+    tokens, u = torch.randint(0, VOCABULARY, (9,), generator=g).to(DEV), torch.rand(SEQUENCES, generator=g).to(DEV)
+    serving.step(tokens, _ints([3, 3, 3]), u)
+    state = [t.clone() for t in (serving.pages, serving.lengths, serving.free, serving.n_free)]
+    with pytest.raises(ValueError, match="one token at least"):
+        serving.step(tokens[:0], _ints([0, 0, 0]), u, ends=_ints([1, 0, 0]))
+    assert all(torch.equal(a, b) for a, b in zip(state, (serving.pages, serving.lengths, serving.free, serving.n_free)))
