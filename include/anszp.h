@@ -590,9 +590,9 @@ int anszp_embed(const anszp_embed_args_t* args, void* hip_stream);
 
 /* Low-rank adapters beside a product: with i = ids[r] the adapter of row r,
  *   out = act(base + scales[i] * x_scales[r] * (x[r] a[i]^T) b[i]^T) * mul + residual
- * and without the middle term for a row that has none.  base is what anszp_linear gives without its epilogue.  Sums in fp32; what lies between the
- * two products is held to 2^-18 for bf16 outputs, in all its 24 bits for fp32 ones.  A row's result depends on its own adapter alone; where
- * that or x holds an infinity or a NaN, it has infinities or NaN. */
+ * and without the middle term for a row that has none.  base is what anszp_linear gives without its epilogue.  Sums in fp32, and what lies between the
+ * two products, too, with all its 24 bits.  A row's result depends on its own adapter alone; where that or x holds an infinity or a NaN, it has
+ * infinities or NaN. */
 typedef struct {
     const void*    x;             /* [device] rows x k of x_dtype                                    */
     const void*    a;             /* [device] adapters x rank x k, bf16                              */

@@ -4,8 +4,8 @@
 //
 // Rows come in tiles of 64, and a tile is worked through once for each adapter that its rows have: one for a prompt, up to 64 for a step of as
 // many requests.  What a row has from other rows' adapters is never selected, so that nothing in them, an infinity or a NaN, reaches it.  x and a are bf16
-// (8-bit rows are exact in it), their sums in 32 bits.  h goes into the second product as two bf16 numbers, to 2^-18 of it, for bf16 outputs, and as three,
-// all of it, for fp32 ones: a number rounded to bf16 leaves a rest that is exact.
+// (8-bit rows are exact in it), their sums in 32 bits.  h goes into the second product as three bf16 numbers of 8 bits each, which are all
+// of it.  (Two, rounded, are up to 2^-18 off, and where base or residual cancels the sum that is several steps of a bf16 output.)
 //
 // Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h
 // 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 134 (4.1 TB/s, the vector unit busy 56 % of the time; torch's product of two such matrices,
@@ -37,12 +37,14 @@ struct AdaptParams {
     uint64_t rows, cols;
     uint32_t adapters, k, rank, rank_room, activation;
     uint32_t slots, groups, parts;      // workgroups that share a tile's rows, groups of ranks, parts of k
-    uint32_t blocks, terms;             // blocks of 8 ranks a term of h has, terms
+    uint32_t blocks;                    // of 8 ranks that a term of h has
     uint32_t across, width;             // workgroups that a row's columns take; a row of h's terms
     const uint8_t* x_last;              // where the last 16 bytes of each begin
     const uint8_t* a_last;
     const uint8_t* b_last;
 };
+
+constexpr uint32_t kTerms = 3;          // bf16 numbers that are one of h
 
 __device__ __forceinline__ bf16x8 as_bf16(words4 w) { return __builtin_bit_cast(bf16x8, w); }
 
@@ -223,11 +225,6 @@ __global__ __launch_bounds__(256, 3) void adapt_down_kernel(AdaptParams p) {
     }
 }
 
-// The nearest bf16 (of a number that would become infinite the one below it, so that what is left is a number).
-__device__ __forceinline__ uint16_t part_of(float h) {
-    return !(__builtin_fabsf(h) < 0x1p127f) ? uint16_t(__builtin_bit_cast(uint32_t, h) >> 16) | (h != h ? 0x40u : 0u) : to_bf16(h);
-}
-
 // Eight ranks of h of a row, the parts of k added up; what a row without an adapter has there is not looked at.
 template <uint32_t AT_ONCE>
 __device__ __forceinline__ void load_h(const AdaptParams& p, uint64_t row, uint32_t block, float (&h)[8]) {
@@ -253,23 +250,27 @@ __device__ __forceinline__ void load_h(const AdaptParams& p, uint64_t row, uint3
             }
     }
 }
-// Block `block` of a row's terms, [term][block][8] behind `to`, from these ranks; `adapted`: the row has an adapter.
+// Block `block` of a row's terms, [term][block][8] behind `to`, from these ranks; `adapted`: the row has an adapter.  A term is the upper half of what is left of h: 8 of its 24
+// bits (and of an infinity or a NaN all that it says; nothing is left of these).
 __device__ __forceinline__ void write_terms(const AdaptParams& p, bool adapted, uint32_t block, float (&h)[8], uint16_t* to) {
 #pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i) h[i] = adapted && block < p.blocks && block * 8u + i < p.rank ? h[i] : 0.0f;
-    for (uint32_t term = 0; term < (block < p.blocks ? p.terms : 1u); ++term) {
+    for (uint32_t i = 0; i < 8u; ++i) h[i] = __builtin_canonicalizef(adapted && block < p.blocks && block * 8u + i < p.rank ? h[i] : 0.0f);
+#pragma unroll
+    for (uint32_t term = 0; term < kTerms; ++term) {
+        if (term && block >= p.blocks) break;
         words4 w;
 #pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i) {
-            const uint16_t part = part_of(h[i]);
-            w[i >> 1] = i & 1u ? w[i >> 1] | uint32_t(part) << 16 : part;
-            h[i] = __builtin_fabsf(h[i]) < __builtin_inff() ? h[i] - bf16_low(part) : 0.0f;
-        }
+        for (uint32_t i = 0; i < 8u; i += 2u) w[i >> 1] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, h[i + 1u]), __builtin_bit_cast(uint32_t, h[i]), 0x07060302u);
         *reinterpret_cast<words4*>(to + (term * p.blocks + block) * 8u) = w;
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i) {
+            const float left = h[i] - bf16_high(__builtin_bit_cast(uint32_t, h[i]));
+            h[i] = term || __builtin_fabsf(h[i]) < __builtin_inff() ? left : 0.0f;
+        }
     }
 }
 // Which blocks there are to write: each of the first term, which writes the others too, and those behind all terms, which are zeros.
-__device__ __forceinline__ bool writes(const AdaptParams& p, uint32_t block) { return block < p.blocks || block >= p.blocks * p.terms; }
+__device__ __forceinline__ bool writes(const AdaptParams& p, uint32_t block) { return block < p.blocks || block >= p.blocks * kTerms; }
 
 // 8 consecutive elements of an operand that has as many in a row.
 template <uint32_t DTYPE>
@@ -338,11 +339,13 @@ __device__ __forceinline__ words4 ranks_of(const AdaptParams& p, const uint16_t*
     if constexpr (WHOLE) return *reinterpret_cast<const words4_any*>(at);
     else return careful(at, 2 * (int32_t(p.rank) - int32_t(block) * 8), p.b_last);
 }
-// Steps of the second product, each of four blocks of ranks; short terms share one.
-template <uint32_t OUT>
-__device__ __forceinline__ uint32_t steps_of(const AdaptParams& p) {
-    return p.blocks < 4u ? (p.blocks * (OUT == ANSZP_OUT_BF16 ? 2u : 3u) + 3u) / 4u : p.blocks / 4u;
-}
+// Steps of the second product, each of four blocks of a row of b, which meet h's terms one after the other.  Of one or two blocks the four are the same again: they meet
+// several terms at once.
+struct Steps {
+    uint32_t steps, turns, apart;       // turns of a step, and how far apart what they take of h lies
+    __device__ __forceinline__ explicit Steps(const AdaptParams& p)
+        : steps(p.blocks < 4u ? 1u : p.blocks / 4u), turns(p.blocks < 4u ? p.width / 32u : kTerms), apart(p.blocks < 4u ? 32u : p.blocks * 8u) {}
+};
 __device__ __forceinline__ uint32_t block_of(const AdaptParams& p, uint32_t step, uint32_t g) { return p.blocks < 4u ? g & (p.blocks - 1u) : step * 4u + g; }
 
 // The ids of a tile's rows, one a lane; rows that are not there have the last one's.
@@ -370,16 +373,15 @@ __global__ __launch_bounds__(256) void adapt_terms_kernel(AdaptParams p) {
 // bytes of a row (of bf16) at a time.
 template <uint32_t BASE, uint32_t OUT, bool WHOLE>
 __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 && OUT == ANSZP_OUT_BF16 ? 4 : 3) void adapt_up_kernel(AdaptParams p) {
-    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u;
     extern __shared__ __attribute__((aligned(16))) uint16_t b_rows[];                              // [column / 8 in steps of 8][block][8], 8 more behind a row
     const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4, wave = threadIdx.x >> 6;
     const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
     const uint64_t top = uint64_t(tile) * 64u, first = least(top + wave * 16u, p.rows - 1u);
     const int32_t id = tile_ids(p, top, piece == 0u && wave == 0u);
     const Eighth cols(uint64_t(piece) * 128u + c * 8u, p.cols);
-    const uint32_t rows = uint32_t(least(p.rows - top, 64u)), steps = steps_of<OUT>(p), width = p.blocks * 8u + 8u;
+    const uint32_t rows = uint32_t(least(p.rows - top, 64u)), width = p.blocks * 8u + 8u;
+    const Steps of(p);
     const uint16_t* const h_at = p.terms_of_h + least(first + c, p.rows - 1u) * p.width + g * 8u;
-    const uint32_t terms = p.blocks < 4u ? 1u : kTerms, pieces = steps * terms;                     // of h: a step's terms are one each, short ones share one
     uint64_t left = ~0ull >> (64u - rows);
     bool staged = false;
     while (left) {
@@ -422,15 +424,20 @@ __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 && OUT == ANSZP_OUT_BF1
             }
             __syncthreads();
             if (mine) {
-                // (not unrolled: 135 registers instead of 119, and three wavefronts a SIMD instead of four, 140 us instead of 134)
+                // (a step's terms are under way together, 161 us a call of 8192 rows; one after the other 171)
 #pragma unroll 1
-                for (uint32_t n = 0; n < pieces; ++n) {
-                    const uint32_t s = n / terms, term = n - s * terms;
-                    const bf16x8 h = as_bf16(*reinterpret_cast<const words4*>(h_at + s * 32u + term * p.blocks * 8u));
+                for (uint32_t s = 0; s < of.steps; ++s) {
+                    words4 h[kTerms];
+#pragma unroll
+                    for (uint32_t u = 0; u < kTerms; ++u) h[u] = *reinterpret_cast<const words4*>(h_at + s * 32u + (u < of.turns ? u : 0u) * of.apart);
                     const uint16_t* const b_at = b_rows + c * width + block_of(p, s, g) * 8u;
 #pragma unroll
-                    for (uint32_t t = 0; t < 8u; ++t)
-                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, *reinterpret_cast<const bf16x8*>(b_at + t * 16u * width), sum[t], 0, 0, 0);
+                    for (uint32_t t = 0; t < 8u; ++t) {
+                        const bf16x8 b = *reinterpret_cast<const bf16x8*>(b_at + t * 16u * width);
+#pragma unroll
+                        for (uint32_t u = 0; u < kTerms; ++u)
+                            if (u < of.turns) sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(h[u]), b, sum[t], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(256, BASE == ANSZP_OUT_BF16 && OUT == ANSZP_OUT_BF1
 // waits for memory once, not for each.
 template <uint32_t BASE, uint32_t OUT, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
-    constexpr uint32_t kTerms = OUT == ANSZP_OUT_BF16 ? 2u : 3u, kRing = 4u;
+    constexpr uint32_t kRing = 4u;
     extern __shared__ __attribute__((aligned(16))) uint16_t terms_of_h[];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, g = lane >> 4;
     const uint32_t tile = blockIdx.x / p.across, piece = blockIdx.x - tile * p.across;
@@ -476,13 +483,13 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
         uint32_t s;
         uint64_t lanes;
     } ring[kRing];
-    const uint32_t steps = steps_of<OUT>(p);
+    const Steps of(p);
     const uint16_t* const b_at = p.b + (cols_of_b.at + (c & 3u)) * p.b_row_stride;
     Adapters adapters(of_wave == wave ? id : -1);
     int32_t asked = -1;
-    uint32_t asked_at = steps;
+    uint32_t asked_at = of.steps;
     const auto ask = [&](Piece& to) __attribute__((always_inline)) {
-        if (++asked_at >= steps) {
+        if (++asked_at >= of.steps) {
             asked = adapters.next();
             asked_at = 0u;
         }
@@ -522,18 +529,16 @@ __global__ __launch_bounds__(256, 2) void adapt_up_few_kernel(AdaptParams p) {
 #pragma unroll
             for (uint32_t r = 0; r < 4u; ++r) {
                 if (!(now.lanes >> (16u * r) & 0xFFFFu)) continue;
-                const auto multiply = [&](uint32_t behind) __attribute__((always_inline)) {
-                    const bf16x8 h = *reinterpret_cast<const bf16x8*>(h_at + r * 16u * (p.width + 8u) + now.s * 32u + behind);
+                const auto multiply = [&](uint32_t turn) __attribute__((always_inline)) {
+                    const bf16x8 h = *reinterpret_cast<const bf16x8*>(h_at + r * 16u * (p.width + 8u) + now.s * 32u + turn * of.apart);
 #pragma unroll
                     for (uint32_t t = 0; t < 2u; ++t) part[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(now.b[t]), h, part[r][t], 0, 0, 0);
                 };
-                multiply(0u);
-                if (p.blocks >= 4u) {
 #pragma unroll
-                    for (uint32_t u = 1; u < kTerms; ++u) multiply(u * p.blocks * 8u);
-                }
+                for (uint32_t u = 0; u < kTerms; ++u)
+                    if (u < of.turns) multiply(u);
             }
-            if (now.s + 1u == steps) {
+            if (now.s + 1u == of.steps) {
 #pragma unroll
                 for (uint32_t r = 0; r < 4u; ++r) {
                     if (!(now.lanes >> (16u * r) & 0xFFFFu)) continue;
@@ -597,7 +602,7 @@ __global__ __launch_bounds__(256) void adapt_up_any_kernel(AdaptParams p) {
 
 struct Plan {
     uint32_t ranks;                     // 16s of ranks a workgroup of the first product has
-    uint32_t slots, groups, parts, blocks, terms, width;
+    uint32_t slots, groups, parts, blocks, width;
     bool few, any_down, any_up;         // few rows; operands too short for the kernels of tiles
     uint64_t sums, workspace;           // bytes of the sums of k's parts, of all
 };
@@ -620,7 +625,7 @@ uint64_t bytes_of(const anszp_adapt_args_t& a, uint64_t stride, uint64_t rows, u
 Plan plan_of(const anszp_adapt_args_t& a) {
     Plan q = {};
     if (a.adapters == 0u) {
-        q.blocks = q.terms = 1u;
+        q.blocks = 1u;
         q.width = 32u;
         return q;
     }
@@ -646,9 +651,8 @@ Plan plan_of(const anszp_adapt_args_t& a) {
     // adapter 13.7 us, else 14.7; four, mixed, 14.1 to 21.5; 256 rows: 16, mixed, 34 to 46; two, 128 rows each, 26.7 to 18; four, 64 each, 26.6 to 18.  512:
     // eight, 64 each, 43 to 16; 48, mixed, 88 to 100.)
     q.few = q.any_up || a.rows <= 64u || (a.rows <= 256u && a.adapters >= 4u);
-    q.terms = a.out_dtype == ANSZP_OUT_BF16 ? 2u : 3u;
     q.blocks = blocks <= 2u ? blocks : (blocks + 3u) / 4u * 4u;     // (a step of the second product has four blocks: of one term, or of several short ones)
-    q.width = (q.blocks * q.terms + 3u) / 4u * 32u;
+    q.width = (q.blocks * kTerms + 3u) / 4u * 32u;
     q.sums = (q.parts * a.rows * blocks * 32u + 15u) & ~15ull;
     q.workspace = q.sums + (q.few ? 0u : a.rows * q.width * 2u);
     return q;
@@ -718,7 +722,7 @@ extern "C" int anszp_adapt(const anszp_adapt_args_t* a, void* hip_stream) {
     p.rows = a->rows; p.cols = a->cols; p.adapters = a->adapters; p.k = a->k; p.rank = a->rank; p.rank_room = (a->rank + 7u) / 8u * 8u;
     p.activation = a->activation;
     p.slots = q.slots; p.groups = q.groups; p.parts = q.parts;
-    p.blocks = q.blocks; p.terms = q.terms; p.width = q.width;
+    p.blocks = q.blocks; p.width = q.width;
     p.x_last = p.x + bytes_of_x(*a) - 16u;
     p.a_last = reinterpret_cast<const uint8_t*>(p.a) + bytes_of(*a, a->a_stride, a->rank, a->a_row_stride, a->k) - 16u;
     p.b_last = reinterpret_cast<const uint8_t*>(p.b) + bytes_of(*a, a->b_stride, a->cols, a->b_row_stride, a->rank) - 16u;

@@ -150,3 +150,25 @@ def test_into_each_operand_it_may(rows, cols):
         into = dict(o, mul=mul, residual=residual)
         into[which] = into[which].clone()
         assert torch.equal(B.adapt(**into, activation="gelu", out=into[which]), want)
+
+
+@pytest.mark.parametrize("rank", [5, 8, 16, 40, 128])
+@pytest.mark.parametrize("rows", [1, 60, 700])
+def test_a_base_that_cancels_the_adapters(rows, rank):
+    """h in whole numbers of 20 and 21 bits, one of them a column, and a base that leaves quarters: every step is exact in 32 bits, and so is the bf16 output."""
+    k, cols, n = 60, 136, 3
+    g = torch.Generator(device=DEV).manual_seed(rows + rank)
+    whole = lambda lo, hi, *s: torch.randint(lo, hi, s, device=DEV, generator=g)  # noqa: E731
+    x, a = whole(64, 128, rows, k), whole(128, 256, n, rank, k)
+    of_column = torch.arange(cols, device=DEV) % rank
+    b = torch.zeros(n, cols, rank, dtype=BF16, device=DEV)
+    b[:, torch.arange(cols, device=DEV), of_column] = 1.0
+    ids = torch.arange(rows, dtype=torch.int32, device=DEV) % (n + 1) - (0 if rows == 1 else 1)
+    h = torch.stack([(x[r].cpu() * a[max(int(i), 0)].cpu()).sum(-1) for r, i in enumerate(ids.tolist())])[:, of_column.cpu()].to(DEV)
+    left = whole(-64, 64, rows, cols) / 4
+    base = left - h.float()
+    assert h.max() < 2 ** 21 and torch.equal(base.double(), left.double() - h.double())
+    o = dict(base=base, a=a.to(BF16), b=b, ids=ids)
+    for of_x in (x.to(torch.int8), x.to(BF16)):
+        got = B.adapt(**o, x=of_x)
+        assert torch.equal(got, torch.where(ids[:, None] >= 0, left, base).to(BF16))
