@@ -1188,7 +1188,7 @@ def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: in
 def embed(tokens, weight, zero_point: int = 0, row_scales=None, scale: float = 1.0, out_dtype: str = "bf16", out=None, status=None):
     """anszp_embed on torch's current stream: rows scale * row_scales[id] * (weight[id] - zero_point) of the tokens int64 [n], weight uint8 symbols [vocabulary, cols] and
     row_scales fp32 [vocabulary], or scale * weight[id] of a weight in bf16.  Zeros for tokens below 0, and for those beyond the vocabulary, which the
-    status (two int32 words) tells."""
+    status (two int32 words) tells.  No gradient: the result is apart from autograd, whatever the operands ask for."""
     torch = _torch()
     dev = tokens.device
     if out_dtype in _FLOATS:
@@ -1223,7 +1223,8 @@ def adapt(base, x, a, b, ids, x_scales=None, scales=None, activation: str = "non
     """anszp_adapt on torch's current stream: act(base + scales[i] * x_scales[r] * (x[r] @ a[i]^T) @ b[i]^T) * mul + residual with i = ids[r], and nothing added to base
     for ids below 0.  base [rows, cols] fp32 or bf16 (what linear gives without its epilogue), x [rows, k] bf16 or int8, a [adapters, rank, k] and b
     [adapters, cols, rank] bf16, ids int32 [rows], x_scales fp32 [rows], scales fp32 [adapters]; mul and residual [rows, cols] of the output's type (out's own, if it is
-    given).  Returns out (which may be base, of the same type, mul or residual itself).  An id beyond the adapters counts as none, and the status (two int32 words) tells."""
+    given).  Returns out (which may be base, of the same type, mul or residual itself).  An id beyond the adapters counts as none, and the status (two int32 words) tells.  No gradient: the result is
+    apart from autograd, and adapters that ask for a gradient get none here; they are trained by other means."""
     torch = _torch()
     dev = base.device
     if out_dtype in _FLOATS and activation in FN_CODES:
@@ -1274,7 +1275,7 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out
     """anszp_sample on torch's current stream: a token for each row of logits [rows, vocabulary] fp32 or bf16, drawn by uniforms fp32 [rows] from [0, 1) among what
     top_k, top_p and min_p leave, in the order of falling logits; a temperature of 0 takes the largest.  temperature, top_p and min_p are numbers or fp32 [rows], top_k is a
     number or int32 [rows].  Returns (tokens int64 [rows], which is `out` where that is given; chances fp32 [rows], the token's part of what was
-    left); a row that has no token (a NaN, nothing above -infinity) has -1 and 0."""
+    left); a row that has no token (a NaN, nothing above -infinity) has -1 and 0.  No gradient: the chances, too, are apart from autograd."""
     torch = _torch()
     dev = logits.device
     results = _call("anszp_sample", "sample", dev, logits, uniforms, temperature, top_k, top_p, min_p, out, calls=_operator_calls)

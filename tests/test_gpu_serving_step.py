@@ -278,3 +278,14 @@ def test_a_step_of_no_tokens_is_refused_before_it_changes_anything():
     with pytest.raises(ValueError, match="one token at least"):
         serving.step(tokens[:0], _ints([0, 0, 0]), u, ends=_ints([1, 0, 0]))
     assert all(torch.equal(a, b) for a, b in zip(state, (serving.pages, serving.lengths, serving.free, serving.n_free)))
+
+
+def test_operands_that_ask_for_a_gradient_get_none():
+    """As the docstrings say: the results are apart from autograd, and the operands' own gradients stay empty."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    a, b, base = rnd(2, 8, 64).to(torch.bfloat16).requires_grad_(), rnd(2, 40, 8).to(torch.bfloat16).requires_grad_(), rnd(3, 40).requires_grad_()
+    logits, words = rnd(3, 90).requires_grad_(), rnd(9, 40).to(torch.bfloat16).requires_grad_()
+    results = [B.adapt(base, rnd(3, 64).to(torch.bfloat16), a, b, _ints([0, 1, -1])), B.embed(torch.tensor([1, 2], device=DEV), words), *B.sample(logits, torch.rand(3, device=DEV))]
+    assert not any(t.requires_grad for t in results) and all(t.grad is None for t in (a, b, base, logits, words))
+    assert all("No gradient" in function.__doc__ for function in (B.adapt, B.embed, B.sample))
