@@ -563,6 +563,7 @@ typedef struct {
     uint64_t       n_seqs, n_tokens, free_room;           /* < 2^24, < 2^31, < 2^31; may be 0        */
     uint32_t       table_width;   /* >= 1; table_width * page_size <= 2^30                           */
     uint32_t       page_size;     /* a power of two from 16 to 65536                                 */
+    int32_t*       last;          /* [device] n_seqs: which of all new tokens is the sequence's last one, -1 if it has none or gets nothing; or NULL */
 } anszp_place_args_t;
 /* [host only] Bytes of workspace a call takes (0: none); reads sizes, and whether there are `ends`. */
 uint64_t anszp_place_workspace_bytes(const anszp_place_args_t* args);

@@ -103,7 +103,7 @@ class PlaceArgs(C.Structure):
                 ("ends", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p), ("n_free_out", C.c_void_p),
                 ("slots", C.c_void_p), ("owners", C.c_void_p), ("starts", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64), ("n_seqs", C.c_uint64), ("n_tokens", C.c_uint64), ("free_room", C.c_uint64),
-                ("table_width", C.c_uint32), ("page_size", C.c_uint32)]
+                ("table_width", C.c_uint32), ("page_size", C.c_uint32), ("last", C.c_void_p)]
 
 
 class EmbedArgs(C.Structure):
@@ -1139,16 +1139,17 @@ class Placed(NamedTuple):
     n_free: object
 
 
-def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: int, ends=None, lengths_out=None, n_free_out=None, status=None) -> Placed:
+def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: int, ends=None, lengths_out=None, n_free_out=None, status=None, last=None) -> Placed:
     """anszp_place on torch's current stream: sequences that hold lengths[s] tokens get new[s] more, in pages from the end of the stack free[:n_free].  pages int32
     [sequences, width] (contiguous), lengths, new and ends int32 [sequences], free int32 [room for all pages], n_free int32 [1]; n_tokens: as many slots are made, at least
     the sum of new.  A sequence with a number other than 0 in ends gives its pages back first and begins anew.  pages and free are written in place, behind what goes on
     being held; lengths_out and n_free_out may be lengths and n_free themselves, and where they are not, the same call gives the same again, unless a sequence both
     ends and gets tokens, whose row is written from its first page on.  A sequence for which there is no room gets nothing: its slots are -1, its length (0, if it
-    ends) stays, and the status (two int32 words) says so."""
+    ends) stays, and the status (two int32 words) says so.  last int32 [sequences], where it is given, gets which of the tokens is each sequence's last one, -1 for one
+    that has none or gets nothing."""
     torch = _torch()
     dev = pages.device
-    result = _call("anszp_place", "place_tokens", dev, pages, page_size, lengths, new, free, n_free, n_tokens, ends, lengths_out, n_free_out, status, calls=_operator_calls)
+    result = _call("anszp_place", "place_tokens", dev, pages, page_size, lengths, new, free, n_free, n_tokens, ends, lengths_out, n_free_out, status, last, calls=_operator_calls)
     if result is not None:
         return Placed(*result)
     _device_index(torch, dev)
@@ -1172,6 +1173,8 @@ def place_tokens(pages, page_size: int, lengths, new, free, n_free, n_tokens: in
     a.lengths_out, a.n_free_out = _want(lengths_out, "lengths_out", dev, (n,), torch.int32), _want(n_free_out, "n_free_out", dev, (1,), torch.int32)
     if status is not None:
         a.status = _want(status, "status", dev, (2,), torch.int32)
+    if last is not None:
+        a.last = _want(last, "last", dev, (n,), torch.int32)
     slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
     owners, starts = torch.empty(n_tokens, dtype=torch.int32, device=dev), torch.empty(n + 1, dtype=torch.int32, device=dev)
     a.slots, a.owners, a.starts = slots.data_ptr(), owners.data_ptr(), starts.data_ptr()

@@ -35,6 +35,7 @@ struct PlaceParams {
     int32_t* owners;
     int32_t* starts;
     uint32_t* status;
+    int32_t* last;
     Record* records;
     uint32_t n_seqs, n_tokens, free_room, width, page_log;
 };
@@ -197,6 +198,7 @@ __global__ __launch_bounds__(THREADS) void place_sequences_kernel(PlaceParams p)
             }
             p.starts[s] = at;
             p.lengths_out[s] = int32_t(served ? old + more : old);
+            if (p.last) p.last[s] = served && more ? int32_t(start + more - 1) : -1;
         }
     }
     __syncthreads();                                                // (n_free may be its own output)
@@ -265,10 +267,10 @@ extern "C" int anszp_place(const anszp_place_args_t* a, void* hip_stream) {
     // What is written may meet nothing that other threads still read or write: lengths and n_free may be their own outputs.
     const Rows written[] = {{a->pages, 1, 0, a->n_seqs * a->table_width * 4u}, {a->free_pages, 1, 0, a->free_room * 4u}, {a->slots, 1, 0, a->n_tokens * 8u},
                             {a->owners, 1, 0, a->n_tokens * 4u}, {a->starts, 1, 0, (a->n_seqs + 1u) * 4u}, {a->workspace, 1, 0, need},
-                            {a->lengths_out, 1, 0, a->n_seqs * 4u}, {a->n_free_out, 1, 0, 4}};
+                            {a->lengths_out, 1, 0, a->n_seqs * 4u}, {a->n_free_out, 1, 0, 4}, {a->last, 1, 0, a->n_seqs * 4u}};
     const Rows lengths = {a->lengths, 1, 0, a->n_seqs * 4u}, n_free = {a->n_free, 1, 0, 4};
     const Rows read[] = {{a->new_tokens, 1, 0, a->n_seqs * 4u}, {a->ends, 1, 0, a->n_seqs * 4u}};
-    for (uint32_t i = 0; i < 8u; ++i) {
+    for (uint32_t i = 0; i < 9u; ++i) {
         if (written[i].width == 0u) continue;
         for (uint32_t j = 0; j < i; ++j)
             if (written[j].width && meet(written[i], written[j])) return ANSZP_E_RANGE;
@@ -277,7 +279,7 @@ extern "C" int anszp_place(const anszp_place_args_t* a, void* hip_stream) {
         if (lengths.width && (i == 6u ? meet_elsewhere(written[i], lengths) : meet(written[i], lengths))) return ANSZP_E_RANGE;
         if (i == 7u ? meet_elsewhere(written[i], n_free) : meet(written[i], n_free)) return ANSZP_E_RANGE;
     }
-    PlaceParams p = {a->pages, a->lengths, a->lengths_out, a->new_tokens, a->ends, a->free_pages, a->n_free, a->n_free_out, a->slots, a->owners, a->starts, a->status,
+    PlaceParams p = {a->pages, a->lengths, a->lengths_out, a->new_tokens, a->ends, a->free_pages, a->n_free, a->n_free_out, a->slots, a->owners, a->starts, a->status, a->last,
                      static_cast<Record*>(a->workspace), static_cast<uint32_t>(a->n_seqs), static_cast<uint32_t>(a->n_tokens), static_cast<uint32_t>(a->free_room),
                      a->table_width, static_cast<uint32_t>(__builtin_ctz(a->page_size))};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);

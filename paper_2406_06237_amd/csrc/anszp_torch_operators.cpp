@@ -182,14 +182,14 @@ bool ints(const at::Tensor& t, const at::Device& on, int64_t n) { return vector(
 bool floats(const at::Tensor& t, const at::Device& on, int64_t n) { return vector(t, on, n) && t.scalar_type() == at::kFloat; }
 
 py::object place_tokens(const at::Tensor& pages, int64_t page_size, const at::Tensor& lengths, const at::Tensor& fresh, const at::Tensor& free, const at::Tensor& n_free,
-                        int64_t n_tokens, const Maybe& ends, Maybe lengths_out, Maybe n_free_out, const Maybe& status, uint64_t stream) {
+                        int64_t n_tokens, const Maybe& ends, Maybe lengths_out, Maybe n_free_out, const Maybe& status, const Maybe& last, uint64_t stream) {
     const at::Device on = pages.device();
     if (pages.dim() != 2 || pages.scalar_type() != at::kInt || !pages.is_contiguous() || pages.size(1) > 1ll << 30 || page_size < 0 || page_size > 65536 || n_tokens < 0 ||
         n_tokens >= 1ll << 31 || free.dim() != 1 || free.size(0) >= 1ll << 31)
         return none();
     const int64_t n = pages.size(0);
     if (!ints(lengths, on, n) || !ints(fresh, on, n) || !ints(free, on, free.size(0)) || !ints(n_free, on, 1) || (ends && !ints(*ends, on, n)) ||
-        (lengths_out && !ints(*lengths_out, on, n)) || (n_free_out && !ints(*n_free_out, on, 1)) || (status && !ints(*status, on, 2)))
+        (lengths_out && !ints(*lengths_out, on, n)) || (n_free_out && !ints(*n_free_out, on, 1)) || (status && !ints(*status, on, 2)) || (last && !ints(*last, on, n)))
         return none();
     at::Tensor slots, owners, starts;
     const int rc = unlocked([&] {
@@ -202,6 +202,7 @@ py::object place_tokens(const at::Tensor& pages, int64_t page_size, const at::Te
         a.pages = data<int32_t>(pages); a.lengths = data<int32_t>(lengths); a.lengths_out = address<int32_t>(lengths_out); a.new_tokens = data<int32_t>(fresh);
         a.ends = address<int32_t>(ends); a.free_pages = data<int32_t>(free); a.n_free = data<int32_t>(n_free); a.n_free_out = address<int32_t>(n_free_out);
         a.slots = data<int64_t>(slots); a.owners = data<int32_t>(owners); a.starts = data<int32_t>(starts); a.status = address<uint32_t>(status);
+        a.last = address<int32_t>(last);
         a.n_seqs = uint64_t(n); a.n_tokens = uint64_t(n_tokens); a.free_room = uint64_t(free.size(0)); a.table_width = uint32_t(pages.size(1)); a.page_size = uint32_t(page_size);
         at::Tensor workspace;
         a.workspace_bytes = anszp_place_workspace_bytes(&a);

@@ -172,7 +172,6 @@ class Serving:
         self.lengths = torch.zeros(count, dtype=torch.int32, device=device)
         self.free = torch.from_numpy(np.random.default_rng(seed).permutation(n_pages).astype(np.int32)).to(device)
         self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=device)
-        self.places = torch.arange(count, dtype=torch.int32, device=device)
         self.adapter_of = torch.full((count,), -1, dtype=torch.int32, device=device)
 
     def step(self, tokens, new, uniforms, ends=None, **settings):
@@ -180,18 +179,20 @@ class Serving:
         anew.  settings: sample's.  Returns (the next token of each sequence int64, its chance, logits fp32 [sequences, vocabulary]).  A sequence without new tokens, and one that place_tokens
         refuses, as for lack of pages (its length stays, and the cache's status says so), has token -1 and a chance of 0; its logits mean nothing, and no
         token of it is to be given to a later step before those that it was refused."""
+        torch = B._torch()
         if tokens.shape[0] == 0:
             raise ValueError("a step has one token at least")
+        last = torch.empty_like(self.lengths)
         placed = B.place_tokens(self.pages, PAGE_SIZE, self.lengths, new, self.free, self.n_free, tokens.shape[0], ends=ends, lengths_out=self.lengths, n_free_out=self.n_free,
-                                status=self.block.cache.status)
+                                status=self.block.cache.status, last=last)
         x = B.embed(tokens, self.words.symbols, self.words.zero_point, self.words.scales, scale=math.sqrt(self.words.symbols.shape[1]), status=self.block.cache.status)
         ids = self.adapter_of[placed.owners.clamp_min(0)] if self.adapters else None
         y = self.block.run(x, placed.slots, self.pages, placed.lengths, placed.starts, self.adapters, ids)
-        last = (placed.starts[1:] - 1).clamp_min(0)
+        # (a sequence without a token, -1, has some row here)
         n, s, _ = B.rms_norm(y[last], self.block.norms[0], out_dtype="i8")
         logits = self.logits(n, s, out_dtype="f32")
         drawn, chances = B.sample(logits, uniforms, **settings)
-        none = (placed.slots[last] < 0) | (placed.owners[last] != self.places)
+        none = last < 0
         return drawn.masked_fill_(none, -1), chances.masked_fill_(none, 0.0), logits
 
     def captured_step(self, tokens, new, uniforms, ends=None, **settings):

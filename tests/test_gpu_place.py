@@ -122,3 +122,22 @@ def test_a_sequence_that_ends_and_gets_tokens_has_its_new_pages_at_once():
     table, stack = ints([[3, 5, 1]]), ints([-1, -1, -1])
     got = B.place_tokens(table, 16, ints([40]), ints([20]), stack, ints([0]), 20, ends=ints([1]))
     assert table.tolist() == [[1, 5, 1]] and stack.tolist() == [3, 5, 1] and got.n_free.tolist() == [1] and got.slots.tolist() == [*range(16, 32), *range(80, 84)]
+
+
+@pytest.mark.parametrize("n", [1, 7, 60, 300, 1500])
+def test_the_last_tokens_of_sequences(n):
+    """Where each sequence's last new token is; -1 for those without one and for those that get nothing.  Nothing else is changed by asking for it."""
+    for seed in range(3):
+        rng = random.Random(seed * 100 + n)
+        pages, lengths, free, n_free = _state(rng, n, 16, 60, (2 * n, n // 3, 0)[seed], 9)
+        new = [rng.choice((0, 1, 25, -1, 10 ** 6 if rng.random() < 0.05 else 3)) for _ in range(n)]
+        ends = None if seed == 0 else [int(rng.random() < 0.3) for _ in range(n)]
+        n_tokens = sum(v for v in new if v < 10 ** 6 and v > 0) * (4 if seed else 1)
+        results = []
+        for last in (None, ints([77] * n)):
+            table, stack = torch.tensor(pages, dtype=torch.int32, device=DEV), ints(free)
+            got = B.place_tokens(table, 16, ints(lengths), ints(new), stack, ints([n_free]), n_tokens, ends=None if ends is None else ints(ends), last=last)
+            results.append([*got, table, stack])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+        slots, starts = got.slots.tolist(), got.starts.tolist()
+        assert last.tolist() == [starts[s] + k - 1 if k > 0 and starts[s] + k <= n_tokens and slots[starts[s]] >= 0 else -1 for s, k in enumerate(new)]

@@ -76,6 +76,13 @@ def test_what_place_writes_meets_nothing(out, other):
     assert B.lib().anszp_place(C.addressof(a), None) == E_RANGE
 
 
+@pytest.mark.parametrize("other", ["pages", "free_pages", "slots", "owners", "starts", "workspace", "lengths_out", "n_free_out", "lengths", "n_free", "new_tokens", "ends"])
+def test_what_place_writes_of_last_tokens_meets_nothing(other):
+    a = _args(B.PlaceArgs, PLACE, {})
+    a.last = getattr(a, other)
+    assert B.lib().anszp_place(C.addressof(a), None) == E_RANGE
+
+
 def test_place_workspace():
     def need(**change):
         a = _args(B.PlaceArgs, PLACE, change)
@@ -247,4 +254,12 @@ def test_sizes_of_32_bits_and_more(calls):
                  lambda: B.sample(on(1, long, dtype=BF16), on(1, dtype=torch.float32))):
         with pytest.raises(ValueError, match="32 bits"):
             call()
+    assert calls == []
+
+
+@pytest.mark.parametrize("last", [_ints(2), _ints(6)[::2], torch.zeros(3, dtype=torch.int64)])
+def test_last_tokens_that_are_refused(calls, last):
+    function, operands = _operands()["place"]
+    with pytest.raises(ValueError, match="last"):
+        function(**operands, last=last)
     assert calls == []
