@@ -8,9 +8,9 @@
 // of it.  (Two, rounded, are up to 2^-18 off, and where base or residual cancels the sum that is several steps of a bf16 output.)
 //
 // Memory bounds it: base and out once, x once, the adapters that are there.  8192 rows of 4096 bytes to 11008 columns in bf16 with rank 64, silu and mul: h
-// 25 us (1.4 TB/s of x, 175 TFLOP/s), its terms 5, the columns 134 (4.1 TB/s, the vector unit busy 56 % of the time; torch's product of two such matrices,
-// which streams as many bytes, 92).  1531 rows from 11008 bf16 to 4096 fp32 with a residual, rank 24: 15, 5 and 19 (4 TB/s).  64 requests with 48 adapters
-// of rank 16: 6.4 and 13 us, most of them waiting for loads.
+// 24 to 27 us (1.3 TB/s of x, 170 TFLOP/s), its terms 5, the columns 134 to 148 (4 TB/s, the vector unit busy 56 % of the time; torch's product of two such
+// matrices, which streams as many bytes, 92).  1531 rows from 11008 bf16 to 4096 fp32 with a residual, rank 24: 15, 5 and 18 (4 TB/s).  64 requests with 48
+// adapters of rank 16: 6.5 and 14 us, most of them waiting for loads: each workgroup of the second product adds up the parts of h of its 64 rows first.
 #include <hip/hip_runtime.h>
 
 #include "anszp_cus.h"

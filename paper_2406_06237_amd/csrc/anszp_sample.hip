@@ -12,7 +12,7 @@
 // listed, a few hundred, and each is compared with all others.  Where they are more than the list holds, each bin is cut by its tokens' own logits, as often
 // as that takes.  A small top_k needs no bins: a list of all tokens that may be kept is found by the threads' own largest.
 //
-// Instructions bound it, not memory: 512 rows of 131072 in bf16 take 88 us, 1.5 TB/s, 36 instructions of the vector unit a logit, half of them for q, with
+// Instructions bound it, not memory: 512 rows of 131072 in bf16 take 87 us, 1.5 TB/s, 30 instructions of the vector unit a logit, about half of them for q, with
 // the unit busy 58 % of the time and LDS 28 (an addition to a bin of each of 64 lanes takes 14 clocks, 8 of them for banks that meet).  One row of 32000
 // takes 15 us: each of three passes waits for its first loads, and the sums between them for each other.
 #include <hip/hip_runtime.h>

@@ -14,8 +14,8 @@ product, and the next tokens are drawn from them.  Nothing of it comes back to t
 adapters (--adapters) each sequence has its own low-rank change to every matrix, added to the products by adapt.
 
 With 4096 / 11008 and 8 heads in the cache (177 M weights in 56 MB) a decode takes 0.13 ms, prompts of 8 sequences with 6252 tokens 1.8 ms, a step of the 8
-sequences 0.2 ms, most of which is the host's: its page lists and 13 calls from Python.  With a vocabulary of 32000 a captured step takes 0.18 ms, with four adapters of
-rank 16 0.28.
+sequences 0.2 ms, most of which is the host's: its page lists and 13 calls from Python.  With a vocabulary of 32000 a captured step takes 0.19 ms, with eight adapters of
+rank 16 0.29.
 
     python -m paper_2406_06237_amd.linear_block [--d-model N] [--d-ff N] [--prompt N] [--sequences N] [--steps N] [--bits 8|4] [--vocabulary N] [--adapters N]
 """
