@@ -289,3 +289,25 @@ def test_operands_that_ask_for_a_gradient_get_none():
     results = [B.adapt(base, rnd(3, 64).to(torch.bfloat16), a, b, _ints([0, 1, -1])), B.embed(torch.tensor([1, 2], device=DEV), words), *B.sample(logits, torch.rand(3, device=DEV))]
     assert not any(t.requires_grad for t in results) and all(t.grad is None for t in (a, b, base, logits, words))
     assert all("No gradient" in function.__doc__ for function in (B.adapt, B.embed, B.sample))
+
+
+@pytest.mark.parametrize("adapted", [False, True])
+def test_a_step_is_what_its_calls_give_one_by_one(adapted):
+    """To the bit: page tables and slots from the host, tokens looked up by the formula, ids row by row, the last rows by their numbers."""
+    workload, serving = _serving(adapted)
+    block, sequences = L.Block(workload, SEQUENCES * -(-200 // L.PAGE_SIZE)), L.Sequences(SEQUENCES, 200)
+    block.decode()
+    g = torch.Generator().manual_seed(31)
+    which = serving.adapter_of.tolist()
+    for new in ([70, 1, 129], [1, 1, 1], [3, 64, 20], [1, 0, 1]):
+        tokens, u = torch.randint(0, VOCABULARY, (sum(new),), generator=g).to(DEV), torch.rand(SEQUENCES, generator=g).to(DEV)
+        drawn, chances, got = serving.step(tokens, _ints(new), u, **SETTINGS)
+        x = P.embed(tokens, serving.words.symbols, serving.words.zero_point, serving.words.scales, math.sqrt(D_MODEL)).to(torch.bfloat16).to(DEV)
+        ids = _ints([which[s] for s, n in enumerate(new) for _ in range(n)])
+        y = block.run(x, *sequences.append(new), serving.adapters, ids)
+        there = [s for s, n in enumerate(new) if n]
+        n, s, _ = B.rms_norm(y[[sum(new[:s + 1]) - 1 for s in there]], block.norms[0], out_dtype="i8")
+        want = serving.logits(n, s, out_dtype="f32")
+        assert torch.equal(got[there], want)
+        tokens, its = B.sample(want, u[there], **SETTINGS)
+        assert torch.equal(drawn[there], tokens) and torch.equal(chances[there], its)
